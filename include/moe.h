@@ -65,6 +65,8 @@ typedef void* moe_stream;            /* hipStream_t */
 #define MOE_MAX_EXPERTS 256
 #define MOE_MAX_TOPK 16
 #define MOE_MAX_ROUTER_EXPERTS 64   /* moe_router_topk */
+#define MOE_FEW_TOKENS 16           /* moe_few_tokens */
+#define MOE_KV8_BLOCK 16            /* tokens of a cache block that share an exponent */
 
 /* ABI version of the loaded library (MOE_ABI_VERSION). */
 int moe_abi_version(void);
@@ -323,6 +325,200 @@ moe_status moe_grouped_ffn_mxfp8_gather(const uint8_t* x_codes, const uint8_t* x
 moe_status moe_combine(const void* y_perm, const int32_t* dest_rows, const float* topk_weights,
                        const void* y_shared, int64_t T, int32_t k, int32_t H, moe_dtype dt, void* y,
                        moe_stream stream);
+
+/*
+ * 4-bit weights with group scales, for products with few rows, whose time is the
+ * read of the weights (the memory-constrained single-GPU setting of Section 7; the
+ * FP8 decoding of a batch's last sequences goes the same way).
+ *
+ *   W[n][k] = scale[n][k / group] * (q[n][k] - zero[n][k / group])
+ *
+ * q and zero are integers 0..15, scale is bf16, group is 32, 64 or 128 and divides K.
+ * Without zero points (NULL) zero is 8.  Two representations:
+ *
+ *   standard  codes u8 [rows, K / 2], the even column in the low nibble; scales bf16
+ *             [rows, K / group]; zeros u8 [rows, K / group]
+ *   packed    what the kernels read, rows padded to 16 and columns to 128: codes u8
+ *             [rows / 16][K / 128][1024], a tile of 16 rows x 128 columns in one piece:
+ *             byte 16 l + 4 j + b of a tile belongs to row l % 16 and holds columns
+ *             32 j + 8 (l / 16) + {2 b, 2 b + 4 ... } in the order
+ *             nibble p = 2 b (+ 1 for the high one): column offset 2 p for p < 4,
+ *             2 (p - 4) + 1 for p >= 4; scales bf16 and zeros u8 [rows / 16][K / group][16]
+ *
+ * moe_int4_code_bytes and moe_int4_groups give the packed sizes of one matrix: bytes of
+ * codes, and scales (= zeros) in number.  An expert tensor [E, N, K] is E packed matrices
+ * one after the other.
+ */
+size_t moe_int4_code_bytes(int64_t rows, int32_t K);
+size_t moe_int4_groups(int64_t rows, int32_t K, int32_t group);
+
+/*
+ * moe_quantize_int4 - bf16 rows to standard 4-bit codes.
+ *
+ *   src     bf16 [rows, K]
+ *   codes, scales, zeros   standard form, out; zeros NULL: symmetric
+ *
+ * Symmetric: scale = bf16(max |v| / 7), q = round(v / scale) + 8.  With zeros: lo = min(v, 0),
+ * hi = max(v, 0), scale = bf16((hi - lo) / 15), zero = round(-lo / scale), q = round(v / scale)
+ * + zero.  Both clamped to 0..15, ties to even, the quotients by the scale as rounded.  A group
+ * of zeros has scale 0.  Inputs are finite (not checked).
+ * Errors: INVALID_ARGUMENT for rows < 0, an unknown group, K not a positive multiple of
+ * the group, null or misaligned pointers; UNSUPPORTED for 2^39 groups or more.
+ */
+moe_status moe_quantize_int4(const void* src, int64_t rows, int32_t K, int32_t group, uint8_t* codes,
+                             uint16_t* scales, uint8_t* zeros, moe_stream stream);
+
+/*
+ * moe_pack_int4 - standard to packed form, of `matrices` matrices of rows x K each.
+ * zeros and out_zeros are both NULL or both given.  Run once when weights are loaded.
+ * Errors: as moe_quantize_int4, plus INVALID_ARGUMENT for matrices < 0, one of the two zeros
+ * without the other; UNSUPPORTED for 2^26 tiles or more.
+ */
+moe_status moe_pack_int4(const uint8_t* codes, const uint16_t* scales, const uint8_t* zeros, int64_t matrices,
+                         int64_t rows, int32_t K, int32_t group, uint8_t* out_codes, uint16_t* out_scales,
+                         uint8_t* out_zeros, moe_stream stream);
+
+/*
+ * moe_matvec_int4 - y = x W^T for a 4-bit W and few rows of x.
+ *
+ *   x       bf16 [T, K]
+ *   codes, scales, zeros   packed W [N, K]; zeros may be NULL
+ *   y       bf16 [T, N]   out
+ *
+ * Codes are multiplied as integers in bf16 (exact) on the matrix cores, sums of a group in
+ * fp32, scaled and added up in fp32, rounded once.  The weights are read once for each 64
+ * rows of x: any T is right, few rows are what it is for.  x finite: an infinite x gives NaN.
+ * Errors: INVALID_ARGUMENT for T < 0, N < 1, an unknown group, K not a positive multiple of
+ * the group, null or misaligned pointers; UNSUPPORTED for T > 2^20, N or K > 2^24.
+ */
+moe_status moe_matvec_int4(const void* x, const uint8_t* codes, const uint16_t* scales, const uint8_t* zeros, int64_t T,
+                           int32_t N, int32_t K, int32_t group, void* y, moe_stream stream);
+
+/*
+ * moe_few_tokens - the whole layer (moe_route, the expert FFNs, the shared expert,
+ * moe_combine) for at most MOE_FEW_TOKENS tokens in two kernels: the step of the few
+ * sequences that a batch ends on (the paper's long tail: at most 8 active sequences).
+ * Nothing is grouped: the layer's time is one read of the chosen experts' weights.
+ *
+ *   x               bf16 [T, H]    T <= 16
+ *   logits          f32  [T, E]
+ *   w_gate, w_up    bf16 [E, F, H];  w_down bf16 [E, H, F]   as moe_grouped_ffn
+ *   ws_gate, ws_up  bf16 [Fs, H];    ws_down bf16 [H, Fs]    shared expert; NULL with Fs = 0
+ *   topk_ids i32, topk_weights f32 [T, k]   out, as moe_route
+ *   y               bf16 [T, H]    out
+ *   ws, ws_bytes    device scratch of at least moe_few_tokens_workspace_bytes(): the rows h
+ *
+ * The gate weight multiplies silu(g) u in fp32 before h is rounded to bf16; all sums are fp32,
+ * y is rounded once.  Deterministic; the order of y's sums depends on the experts that the
+ * batch chose, so a token's y may differ in its last bit with the tokens beside it.
+ * Errors: as moe_route and moe_grouped_ffn, plus INVALID_ARGUMENT for Fs < 0 or not a
+ * multiple of 64, T > 16 (UNSUPPORTED).
+ *
+ * moe_few_tokens_int4 takes 4-bit weights: `weights` is a HOST array of six packed tensors in
+ * the order w_gate, w_up, w_down, ws_gate, ws_up, ws_down, of one group size; either all have
+ * zeros or none.  H and F (and Fs) are multiples of the group.
+ */
+typedef struct {
+    const uint8_t* codes;
+    const uint16_t* scales;
+    const uint8_t* zeros;            /* NULL: 8 */
+} moe_int4;
+size_t moe_few_tokens_workspace_bytes(int64_t T, int32_t k, int32_t F, int32_t Fs);
+moe_status moe_few_tokens(const void* x, const float* logits, int64_t T, int32_t H, int32_t E, int32_t k, int32_t F,
+                          int32_t Fs, int32_t renormalize, const void* w_gate, const void* w_up, const void* w_down,
+                          const void* ws_gate, const void* ws_up, const void* ws_down, int32_t* topk_ids,
+                          float* topk_weights, void* y, void* ws, size_t ws_bytes, moe_stream stream);
+moe_status moe_few_tokens_int4(const void* x, const float* logits, int64_t T, int32_t H, int32_t E, int32_t k,
+                               int32_t F, int32_t Fs, int32_t renormalize, int32_t group, const moe_int4* weights,
+                               int32_t* topk_ids, float* topk_weights, void* y, void* ws, size_t ws_bytes,
+                               moe_stream stream);
+
+/*
+ * The paged 8-bit key-value cache of one attention layer (per-sequence KV quantisation,
+ * Section 4; pages of 64 tokens in the paper's Section 5.6).  Keys and values are E4M3 codes; the
+ * 16 tokens of a block share one exponent byte for each kv head, one for their keys and one
+ * for their values:  value = code * 2^(e - 127).
+ *
+ *   k_codes          u8 [pages, heads, page, dim]
+ *   v_codes          u8 [pages, heads, page / 16, dim, 16]   a block's values transposed
+ *   k_exps, v_exps   u8 [pages, heads, page / 16]
+ *
+ * page is a multiple of 16, dim 64, 128 or 256.
+ *
+ * A batch over it, the same arguments for both calls:
+ *   block_table  i32 [B, table_cols]  page of tokens [page i, page (i + 1)) of each sequence
+ *   seq_lens     i32 [B]     tokens of each sequence, the new ones included
+ *   cu_tokens    i32 [B + 1] rows of the new tokens: sequence b has rows cu[b] .. cu[b + 1] - 1,
+ *                at positions seq_lens[b] - n_b .. seq_lens[b] - 1 (n_b its row count)
+ *   T            rows, cu_tokens[B]
+ * A sequence may have no rows.  Rows at positions below 0 (a slot of a captured graph whose
+ * sequence has ended: seq_lens[b] = 0) are left out: nothing is appended for them, their
+ * attention output is 0.  All of these are device arrays and are not checked beyond what
+ * keeps the kernels inside their buffers: a page outside [0, pages) is not written.
+ */
+typedef struct {
+    uint8_t* k_codes;
+    uint8_t* v_codes;
+    uint8_t* k_exps;
+    uint8_t* v_exps;
+    int64_t pages;
+    int32_t page;
+    int32_t heads;
+    int32_t dim;
+} moe_kv8_cache;
+
+/*
+ * moe_kv8_append - rotate the new tokens' queries and keys by their positions and write
+ * keys and values into the cache.
+ *
+ *   q, k, v     bf16, rows T of q_heads, heads, heads heads of dim; *_stride elements from a
+ *               row to the next (a multiple of 8): slices of one projection's output will do
+ *   cos_sin     f32 [positions, rot]   cos, then sin, of rot / 2 angles of each position
+ *   rot         leading dimensions that are rotated, a multiple of 16, at most dim
+ *   interleaved 0: pairs (i, i + rot / 2);  1: pairs (2 i, 2 i + 1)
+ *   q_out       bf16 [T, q_heads, dim]   out: rotated queries
+ *
+ * (a, b) becomes (a cos - b sin, a sin + b cos), each operation rounded to fp32.  For each block
+ * and kv head that gets tokens:  s = the smallest integer with max |v| <= 448 * 2^s over the new
+ * tokens (-127 for zeros); if the block holds earlier tokens, s = max(s, the block's) and, where
+ * that grew, their codes are rounded again to the new step; places after the last token are
+ * set to 0.  Codes are rounded to nearest even.  An infinity saturates, NaN stays NaN and does
+ * not count in s.  Calling again with the same arguments leaves the cache as it is.  Tokens
+ * at positions of `positions` or more are rotated as the last one.
+ * Errors: INVALID_ARGUMENT for negative sizes, heads not dividing q_heads, a page not a positive
+ * multiple of 16, a bad stride or rot, null or misaligned pointers; UNSUPPORTED for another dim,
+ * T + 2 B of 2^24 or more, heads > 65535.
+ */
+moe_status moe_kv8_append(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                          int64_t v_stride, int64_t T, int32_t q_heads, const float* cos_sin, int64_t positions,
+                          int32_t rot, int32_t interleaved, const moe_kv8_cache* cache, const int32_t* block_table,
+                          int32_t table_cols, const int32_t* seq_lens, const int32_t* cu_tokens, int32_t B,
+                          void* q_out, moe_stream stream);
+
+/*
+ * moe_kv8_attention - causal attention of the new tokens over the cache.
+ *
+ *   q           bf16 [T, q_heads, dim]   rotated queries; head h reads kv head h / (q_heads / heads)
+ *   max_new     at least every sequence's row count: rows beyond it are not computed
+ *   max_len     the longest sequence (for the plan only; any value gives right results)
+ *   window      0, or how many tokens a row sees, itself included
+ *   scale       factor of the scores
+ *   out         bf16 [T, q_heads, dim]   out
+ *   ws, ws_bytes  device scratch of at least moe_kv8_attention_workspace_bytes() for the same sizes
+ *
+ * A row at position p sees tokens 0..p, with a window p - window + 1..p.  Scores, softmax and
+ * sums are fp32, probabilities are rounded to bf16 for the product with the values.  A row that
+ * sees nothing is 0.  Cache contents past a sequence's end are not used, whatever they are.
+ * Deterministic for a given plan (sizes, max_new, max_len, compute-unit budget).
+ * Errors: as moe_kv8_append, plus INVALID_ARGUMENT for max_new < 1, max_len < 0, window < 0;
+ * WORKSPACE_TOO_SMALL.
+ */
+size_t moe_kv8_attention_workspace_bytes(int32_t B, int32_t q_heads, int32_t heads, int32_t dim, int32_t max_new,
+                                         int32_t max_len, int32_t window);
+moe_status moe_kv8_attention(const void* q, int64_t T, int32_t q_heads, const moe_kv8_cache* cache,
+                             const int32_t* block_table, int32_t table_cols, const int32_t* seq_lens,
+                             const int32_t* cu_tokens, int32_t B, int32_t max_new, int32_t max_len, int32_t window,
+                             float scale, void* out, void* ws, size_t ws_bytes, moe_stream stream);
 
 /*
  * Per-kernel timing (a benchmarking aid, not part of the layer).

@@ -22,6 +22,9 @@ __all__ = [
     "moe_mxfp8_scale_bytes", "moe_quantize_mxfp8", "moe_grouped_ffn_mxfp8_workspace_bytes",
     "moe_grouped_ffn_mxfp8", "moe_grouped_ffn_mxfp8_gather", "MXFP8", "quantize_weights_mxfp8",
     "MoELayerMXFP8", "LayerGraph",
+    "Int4", "moe_int4_code_bytes", "moe_int4_groups", "moe_quantize_int4", "moe_pack_int4", "quantize_weights_int4",
+    "moe_matvec_int4", "moe_few_tokens", "moe_few_tokens_workspace_bytes", "MoELayerFew", "FEW_TOKENS",
+    "KVCache8", "KV8_BLOCK", "moe_kv8_append", "moe_kv8_attention", "moe_kv8_attention_workspace_bytes",
     "profiler_start", "profiler_select", "profiler_stop", "profiler_records", "set_cu_budget",
     "DTYPE_F32", "DTYPE_BF16",
 ]
@@ -31,6 +34,8 @@ LIB_PATH = os.path.join(HERE, "libmoe.so")
 HEADER_PATH = os.path.join(os.path.dirname(HERE), "include", "moe.h")
 
 DTYPE_F32, DTYPE_BF16 = 0, 1
+FEW_TOKENS = 16          # MOE_FEW_TOKENS
+KV8_BLOCK = 16           # MOE_KV8_BLOCK
 _STATUS = {0: "MOE_OK", 1: "MOE_ERR_INVALID_ARGUMENT", 2: "MOE_ERR_UNSUPPORTED",
            3: "MOE_ERR_WORKSPACE_TOO_SMALL", 4: "MOE_ERR_HIP"}
 
@@ -47,6 +52,18 @@ _P = ctypes.c_void_p
 _I64 = ctypes.c_int64
 _I32 = ctypes.c_int32
 _SZ = ctypes.c_size_t
+
+
+class _Int4Ref(ctypes.Structure):
+    """moe_int4"""
+    _fields_ = [("codes", _P), ("scales", _P), ("zeros", _P)]
+
+
+class _Kv8Cache(ctypes.Structure):
+    """moe_kv8_cache"""
+    _fields_ = [("k_codes", _P), ("v_codes", _P), ("k_exps", _P), ("v_exps", _P), ("pages", _I64), ("page", _I32),
+                ("heads", _I32), ("dim", _I32)]
+
 
 _SIGNATURES = {
     "moe_abi_version": (ctypes.c_int, []),
@@ -72,6 +89,21 @@ _SIGNATURES = {
                                              _P, _P, _SZ, _P]),
     "moe_grouped_ffn_mxfp8_gather": (ctypes.c_int, [_P, _P, _P, _P, _I64, _I64, _I32, _I32, _I32, _P, _P, _P, _P,
                                                     _P, _P, _P, _P, _SZ, _P]),
+    "moe_int4_code_bytes": (_SZ, [_I64, _I32]),
+    "moe_int4_groups": (_SZ, [_I64, _I32, _I32]),
+    "moe_quantize_int4": (ctypes.c_int, [_P, _I64, _I32, _I32, _P, _P, _P, _P]),
+    "moe_pack_int4": (ctypes.c_int, [_P, _P, _P, _I64, _I64, _I32, _I32, _P, _P, _P, _P]),
+    "moe_matvec_int4": (ctypes.c_int, [_P, _P, _P, _P, _I64, _I32, _I32, _I32, _P, _P]),
+    "moe_few_tokens_workspace_bytes": (_SZ, [_I64, _I32, _I32, _I32]),
+    "moe_few_tokens": (ctypes.c_int, [_P, _P, _I64, _I32, _I32, _I32, _I32, _I32, _I32, _P, _P, _P, _P, _P, _P, _P, _P,
+                                      _P, _P, _SZ, _P]),
+    "moe_few_tokens_int4": (ctypes.c_int, [_P, _P, _I64, _I32, _I32, _I32, _I32, _I32, _I32, _I32,
+                                           ctypes.POINTER(_Int4Ref), _P, _P, _P, _P, _SZ, _P]),
+    "moe_kv8_append": (ctypes.c_int, [_P, _I64, _P, _I64, _P, _I64, _I64, _I32, _P, _I64, _I32, _I32,
+                                      ctypes.POINTER(_Kv8Cache), _P, _I32, _P, _P, _I32, _P, _P]),
+    "moe_kv8_attention_workspace_bytes": (_SZ, [_I32, _I32, _I32, _I32, _I32, _I32, _I32]),
+    "moe_kv8_attention": (ctypes.c_int, [_P, _I64, _I32, ctypes.POINTER(_Kv8Cache), _P, _I32, _P, _P, _I32, _I32, _I32,
+                                         _I32, ctypes.c_float, _P, _P, _SZ, _P]),
     "moe_profiler_start": (ctypes.c_int, [ctypes.c_int]),
     "moe_profiler_select": (ctypes.c_int, [ctypes.c_char_p]),
     "moe_set_cu_budget": (ctypes.c_int, [_I32]),
@@ -365,6 +397,252 @@ def moe_grouped_ffn_mxfp8_gather(x, sorted_token_ids, offsets, w_gate, w_up, w_d
     return y_perm
 
 
+# --------------------------------------------------------------------------- 4-bit weights
+class Int4:
+    """A packed 4-bit matrix, or a tensor [E, N, K] of such matrices (include/moe.h): codes u8,
+    scales bf16 and zero points u8 (or None) in the library's tiled layout."""
+
+    def __init__(self, codes, scales, zeros, shape, group):
+        self.codes, self.scales, self.zeros = codes, scales, zeros
+        self.shape, self.group = tuple(shape), group
+
+
+def moe_int4_code_bytes(rows, K) -> int:
+    return lib().moe_int4_code_bytes(rows, K)
+
+
+def moe_int4_groups(rows, K, group) -> int:
+    return lib().moe_int4_groups(rows, K, group)
+
+
+def moe_quantize_int4(w, group=128, zeros=False, stream=None):
+    """w bf16 [..., K] -> standard form (codes u8 [..., K / 2], scales bf16 [..., K / group], zero points u8
+    like the scales, or None)."""
+    if w.dtype != torch.bfloat16:
+        raise TypeError("moe_quantize_int4 takes bf16 weights")
+    K = w.shape[-1]
+    rows = w.numel() // K if K else 0
+    dev = w.device
+    codes = torch.empty((*w.shape[:-1], K // 2), dtype=torch.uint8, device=dev)
+    scales = torch.empty((*w.shape[:-1], max(1, K // group)), dtype=torch.bfloat16, device=dev)
+    z = torch.empty(scales.shape, dtype=torch.uint8, device=dev) if zeros else None
+    _dev(w, codes, scales, z)
+    _check(lib().moe_quantize_int4(_ptr(w), rows, K, group, _ptr(codes), _ptr(scales), _ptr(z), _stream(stream, dev)))
+    return codes, scales, z
+
+
+def moe_pack_int4(codes, scales, zeros=None, group=128, stream=None):
+    """Standard codes u8 [..., N, K / 2], scales bf16 and zeros u8 [..., N, K / group] -> Int4."""
+    if codes.dtype != torch.uint8 or scales.dtype != torch.bfloat16 or (zeros is not None and
+                                                                        zeros.dtype != torch.uint8):
+        raise TypeError("moe_pack_int4 takes u8 codes, bf16 scales and u8 zeros")
+    *lead, N, half = codes.shape
+    K = 2 * half
+    if tuple(scales.shape) != (*lead, N, K // group) or (zeros is not None and zeros.shape != scales.shape):
+        raise ValueError("scales and zeros are [..., N, K / group]")
+    mats = 1
+    for n in lead:
+        mats *= n
+    dev = codes.device
+    groups = mats * moe_int4_groups(N, K, group)
+    out = Int4(torch.empty(max(1, mats * moe_int4_code_bytes(N, K)), dtype=torch.uint8, device=dev),
+               torch.empty(max(1, groups), dtype=torch.bfloat16, device=dev),
+               None if zeros is None else torch.empty(max(1, groups), dtype=torch.uint8, device=dev), (*lead, N, K),
+               group)
+    _dev(codes, scales, zeros, out.codes)
+    _check(lib().moe_pack_int4(_ptr(codes), _ptr(scales), _ptr(zeros), mats, N, K, group, _ptr(out.codes),
+                               _ptr(out.scales), _ptr(out.zeros), _stream(stream, dev)))
+    return out
+
+
+def quantize_weights_int4(w, group=128, zeros=False, stream=None):
+    """Weights bf16 [..., N, K] -> Int4: moe_quantize_int4, then moe_pack_int4."""
+    return moe_pack_int4(*moe_quantize_int4(w, group, zeros, stream), group, stream)
+
+
+def moe_matvec_int4(x, w, y=None, stream=None):
+    """x bf16 [T, K], w Int4 [N, K] -> y bf16 [T, N]."""
+    T, K = x.shape
+    if x.dtype != torch.bfloat16:
+        raise TypeError("moe_matvec_int4 takes bf16 x")
+    if len(w.shape) != 2 or w.shape[1] != K:
+        raise ValueError(f"w {w.shape} does not fit x [T, {K}]")
+    N = w.shape[0]
+    if y is None:
+        y = torch.empty((T, N), dtype=torch.bfloat16, device=x.device)
+    elif y.dtype != torch.bfloat16 or tuple(y.shape) != (T, N):
+        raise ValueError(f"y must be bf16 [{T}, {N}]")
+    _dev(x, w.codes, y)
+    _check(lib().moe_matvec_int4(_ptr(x), _ptr(w.codes), _ptr(w.scales), _ptr(w.zeros), T, N, K, w.group, _ptr(y),
+                                 _stream(stream, x.device)))
+    return y
+
+
+# --------------------------------------------------------------------------- the layer for few tokens
+def moe_few_tokens_workspace_bytes(T, k, F, Fs=0) -> int:
+    return lib().moe_few_tokens_workspace_bytes(T, k, F, Fs)
+
+
+def _few_weights(x, E, F, Fs, ws):
+    """Checks the layer's three or six weights; whether they are 4-bit."""
+    H = x.shape[1]
+    want = [(E, F, H), (E, F, H), (E, H, F), (1, Fs, H), (1, Fs, H), (1, H, Fs)][:6 if Fs else 3]
+    if len(ws) < len(want) or any(w is None for w in ws[:len(want)]):
+        raise ValueError(f"{len(want)} weights are needed")
+    int4 = isinstance(ws[0], Int4)
+    for w, shape in zip(ws, want):
+        if isinstance(w, Int4) != int4 or (not int4 and w.dtype != torch.bfloat16):
+            raise TypeError("weights are all bf16 or all Int4")
+        if tuple(w.shape) != shape and not (shape[0] == 1 and tuple(w.shape) == shape[1:]):
+            raise ValueError(f"weights of shape {tuple(w.shape)}, {shape} expected")
+        if int4 and w.group != ws[0].group:
+            raise ValueError("4-bit weights of one layer share a group size")
+    return int4
+
+
+def moe_few_tokens(x, logits, k, w_gate, w_up, w_down, ws_gate=None, ws_up=None, ws_down=None, renormalize=1,
+                   topk_ids=None, topk_weights=None, y=None, ws=None, stream=None):
+    """The whole layer for T <= 16 tokens: x bf16 [T, H], logits f32 [T, E], weights as MoELayer's, bf16
+    or Int4 -> (y bf16 [T, H], topk_ids, topk_weights)."""
+    T, H = x.shape
+    E = logits.shape[1]
+    F = w_gate.shape[1]
+    Fs = 0 if ws_gate is None else ws_gate.shape[-2]
+    dev = x.device
+    if x.dtype != torch.bfloat16 or logits.dtype != torch.float32:
+        raise TypeError("moe_few_tokens takes bf16 x and f32 logits")
+    if logits.shape[0] != T:
+        raise ValueError("logits are [T, E]")
+    w = (w_gate, w_up, w_down, ws_gate, ws_up, ws_down)
+    int4 = _few_weights(x, E, F, Fs, w)
+    if topk_ids is None:
+        topk_ids = torch.empty((T, k), dtype=torch.int32, device=dev)
+    if topk_weights is None:
+        topk_weights = torch.empty((T, k), dtype=torch.float32, device=dev)
+    if y is None:
+        y = torch.empty((T, H), dtype=torch.bfloat16, device=dev)
+    if ws is None:
+        ws = torch.empty(max(1, moe_few_tokens_workspace_bytes(T, k, F, Fs)), dtype=torch.uint8, device=dev)
+    _dev(x, logits, topk_ids, topk_weights, y, ws)
+    if int4:
+        refs = (_Int4Ref * 6)(*[(_ptr(t.codes), _ptr(t.scales), _ptr(t.zeros)) if t is not None else (None, None, None)
+                                for t in w])
+        _dev(*(t.codes for t in w if t is not None))
+        _check(lib().moe_few_tokens_int4(_ptr(x), _ptr(logits), T, H, E, k, F, Fs, renormalize, w_gate.group, refs,
+                                         _ptr(topk_ids), _ptr(topk_weights), _ptr(y), _ptr(ws), ws.numel(),
+                                         _stream(stream, dev)))
+    else:
+        _dev(*w)
+        _check(lib().moe_few_tokens(_ptr(x), _ptr(logits), T, H, E, k, F, Fs, renormalize, *[_ptr(t) for t in w],
+                                    _ptr(topk_ids), _ptr(topk_weights), _ptr(y), _ptr(ws), ws.numel(),
+                                    _stream(stream, dev)))
+    return y, topk_ids, topk_weights
+
+
+# --------------------------------------------------------------------------- the 8-bit cache
+class KVCache8:
+    """The paged 8-bit key-value cache of one attention layer (include/moe.h).  Either the four
+    tensors, or the sizes with KVCache8.empty."""
+
+    def __init__(self, k_codes, v_codes, k_exps, v_exps):
+        pages, heads, page, dim = k_codes.shape
+        if tuple(v_codes.shape) != (pages, heads, page // KV8_BLOCK, dim, KV8_BLOCK):
+            raise ValueError("v_codes is [pages, heads, page / 16, dim, 16]")
+        for t in (k_exps, v_exps):
+            if tuple(t.shape) != (pages, heads, page // KV8_BLOCK):
+                raise ValueError("exponents are [pages, heads, page / 16]")
+        for t in (k_codes, v_codes, k_exps, v_exps):
+            if t.dtype != torch.uint8:
+                raise TypeError("the cache's tensors are u8")
+        _dev(k_codes, v_codes, k_exps, v_exps)
+        self.k_codes, self.v_codes, self.k_exps, self.v_exps = k_codes, v_codes, k_exps, v_exps
+        self.pages, self.heads, self.page, self.dim = pages, heads, page, dim
+        self._ref = _Kv8Cache(_ptr(k_codes), _ptr(v_codes), _ptr(k_exps), _ptr(v_exps), pages, page, heads, dim)
+
+    @classmethod
+    def empty(cls, pages, heads, dim, page=64, device="cuda"):
+        u8 = dict(dtype=torch.uint8, device=device)
+        return cls(torch.empty((pages, heads, page, dim), **u8),
+                   torch.empty((pages, heads, page // KV8_BLOCK, dim, KV8_BLOCK), **u8),
+                   torch.empty((pages, heads, page // KV8_BLOCK), **u8),
+                   torch.empty((pages, heads, page // KV8_BLOCK), **u8))
+
+
+def _batch(block_table, seq_lens, cu_tokens):
+    B, cols = block_table.shape
+    if seq_lens.shape != (B,) or cu_tokens.shape != (B + 1,):
+        raise ValueError("seq_lens is [B], cu_tokens [B + 1] for a block_table [B, columns]")
+    for t in (block_table, seq_lens, cu_tokens):
+        if t.dtype != torch.int32:
+            raise TypeError("block_table, seq_lens and cu_tokens are int32")
+    return B, cols
+
+
+def _rows(t, name, heads, dim):
+    """Row stride of a tensor [T, heads, dim] whose rows are in one piece."""
+    if t.dtype != torch.bfloat16:
+        raise TypeError(f"{name} must be bf16")
+    if t.dim() != 3 or t.shape[1:] != (heads, dim):
+        raise ValueError(f"{name} must be [T, {heads}, {dim}]")
+    if not t.is_cuda:
+        raise ValueError("all tensors must be on the GPU")
+    if t.shape[0] and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim)):
+        raise ValueError(f"{name}: the heads of a row must be in one piece")
+    return t.stride(0) if t.shape[0] > 1 else heads * dim
+
+
+def moe_kv8_append(q, k, v, cos_sin, cache, block_table, seq_lens, cu_tokens, interleaved=False, q_out=None,
+                   stream=None):
+    """Rotates q [T, q_heads, dim] and k [T, heads, dim] by their positions and writes k and v into the
+    cache -> rotated q.  cos_sin f32 [positions, rot]: cos, then sin, of rot / 2 angles.  Rows may be
+    strided: slices of one projection's output."""
+    T, q_heads = q.shape[0], q.shape[1]
+    B, cols = _batch(block_table, seq_lens, cu_tokens)
+    dim, heads = cache.dim, cache.heads
+    qs, ks, vs = _rows(q, "q", q_heads, dim), _rows(k, "k", heads, dim), _rows(v, "v", heads, dim)
+    if k.shape[0] != T or v.shape[0] != T:
+        raise ValueError("q, k and v have the same rows")
+    if cos_sin.dtype != torch.float32:
+        raise TypeError("cos_sin must be float32")
+    if q_out is None:
+        q_out = torch.empty((T, q_heads, dim), dtype=torch.bfloat16, device=q.device)
+    elif q_out.dtype != torch.bfloat16 or tuple(q_out.shape) != (T, q_heads, dim):
+        raise ValueError(f"q_out must be bf16 [{T}, {q_heads}, {dim}]")
+    _dev(cos_sin, block_table, seq_lens, cu_tokens, q_out)
+    _check(lib().moe_kv8_append(_ptr(q), qs, _ptr(k), ks, _ptr(v), vs, T, q_heads, _ptr(cos_sin), cos_sin.shape[0],
+                                cos_sin.shape[1], 1 if interleaved else 0, ctypes.byref(cache._ref), _ptr(block_table),
+                                cols, _ptr(seq_lens), _ptr(cu_tokens), B, _ptr(q_out), _stream(stream, q.device)))
+    return q_out
+
+
+def moe_kv8_attention_workspace_bytes(T, B, q_heads, heads, dim, max_new, max_len, window=0) -> int:
+    """Bytes of scratch for T rows of B sequences (T = 0: none)."""
+    return lib().moe_kv8_attention_workspace_bytes(B, q_heads, heads, dim, max_new, max_len, window) if T else 0
+
+
+def moe_kv8_attention(q, cache, block_table, seq_lens, cu_tokens, max_new, max_len, window=0, scale=None, out=None,
+                      ws=None, stream=None):
+    """Causal attention of the rows q [T, q_heads, dim] over the cache -> out.  max_new: the most new rows of
+    a sequence, max_len: the longest sequence; scale: 1 / sqrt(dim) unless given."""
+    T, q_heads = q.shape[0], q.shape[1]
+    B, cols = _batch(block_table, seq_lens, cu_tokens)
+    if q.dtype != torch.bfloat16 or q.shape[2] != cache.dim:
+        raise ValueError(f"q must be bf16 [T, q_heads, {cache.dim}]")
+    if out is None:
+        out = torch.empty_like(q)
+    elif out.dtype != torch.bfloat16 or out.shape != q.shape:
+        raise ValueError("out must be like q")
+    if ws is None:
+        ws = torch.empty(max(1, moe_kv8_attention_workspace_bytes(T, B, q_heads, cache.heads, cache.dim, max_new, max_len,
+                                                                  window)), dtype=torch.uint8, device=q.device)
+    _dev(q, block_table, seq_lens, cu_tokens, out, ws)
+    _check(lib().moe_kv8_attention(_ptr(q), T, q_heads, ctypes.byref(cache._ref), _ptr(block_table), cols,
+                                   _ptr(seq_lens), _ptr(cu_tokens), B, max_new, max_len, window,
+                                   cache.dim ** -0.5 if scale is None else scale, _ptr(out), _ptr(ws), ws.numel(),
+                                   _stream(stream, q.device)))
+    return out
+
+
 # --------------------------------------------------------------------------- scheduling
 def set_cu_budget(n: int = 0):
     """Plan the persistent grids for n compute units (0: the device's count)."""
@@ -542,4 +820,34 @@ class MoELayerMXFP8:
                                   y_perm=self.y_shared, ws=self.ws_shared, stream=stream)
         moe_combine(self.y_perm, self.perm["dest_rows"], self.topk_weights, self.y_shared, y=self.y,
                     stream=stream)
+        return self.y
+
+
+class MoELayerFew:
+    """The layer for up to T <= 16 tokens (FEW_TOKENS) in two kernels, with bf16 or 4-bit (Int4) weights:
+    what a batch's last few sequences run.  Buffers are made once; ``run`` takes any number of tokens
+    up to T, allocates nothing and does not synchronize.  After it, ``y``, ``topk_ids`` and
+    ``topk_weights`` are the step's (of as many rows as it had tokens)."""
+
+    def __init__(self, T, H, E, k, F, Fs=0, device="cuda"):
+        if T > FEW_TOKENS:
+            raise ValueError(f"T={T}: at most {FEW_TOKENS} tokens")
+        self.T, self.H, self.E, self.k, self.F, self.Fs = T, H, E, k, F, Fs
+        dev = torch.device(device)
+        self._ids = torch.empty((T, k), dtype=torch.int32, device=dev)
+        self._weights = torch.empty((T, k), dtype=torch.float32, device=dev)
+        self._y = torch.empty((T, H), dtype=torch.bfloat16, device=dev)
+        self.ws = torch.empty(max(1, moe_few_tokens_workspace_bytes(T, k, F, Fs)), dtype=torch.uint8, device=dev)
+        self.topk_ids, self.topk_weights, self.y = self._ids, self._weights, self._y
+
+    def run(self, x, logits, w_gate, w_up, w_down, ws_gate=None, ws_up=None, ws_down=None, renormalize=1, stream=None):
+        n = x.shape[0]
+        if n > self.T or x.shape[1] != self.H or logits.shape[1] != self.E or w_gate.shape[1] != self.F:
+            raise ValueError(f"x {tuple(x.shape)}, logits {tuple(logits.shape)}: not this layer's sizes")
+        if (0 if ws_gate is None else ws_gate.shape[-2]) != self.Fs:
+            raise ValueError(f"the shared expert must have Fs={self.Fs}")
+        if self.y.shape[0] != n:
+            self.topk_ids, self.topk_weights, self.y = self._ids[:n], self._weights[:n], self._y[:n]
+        moe_few_tokens(x, logits, self.k, w_gate, w_up, w_down, ws_gate, ws_up, ws_down, renormalize,
+                       topk_ids=self.topk_ids, topk_weights=self.topk_weights, y=self.y, ws=self.ws, stream=stream)
         return self.y

@@ -286,4 +286,135 @@ moe_status moe_combine(const void* y_perm, const int32_t* dest_rows, const float
                                         dt == MOE_DTYPE_BF16, y, stream_of(stream)));
 }
 
+// ------------------------------------------------------------------ 4-bit weights
+size_t moe_int4_code_bytes(int64_t rows, int32_t K) { return moe::int4_code_bytes(rows, K); }
+size_t moe_int4_groups(int64_t rows, int32_t K, int32_t group) { return moe::int4_groups(rows, K, group); }
+
+moe_status moe_quantize_int4(const void* src, int64_t rows, int32_t K, int32_t group, uint8_t* codes,
+                             uint16_t* scales, uint8_t* zeros, moe_stream stream) {
+  moe::Check c = moe::validate_quantize_int4(src, rows, K, group, codes, scales, zeros);
+  if (!c.ok() || rows == 0) return finish(c);
+  return hip_status("moe_quantize_int4",
+                    moe::launch_quantize_int4(static_cast<const uint16_t*>(src), rows * (K / group), group, codes,
+                                              scales, zeros, stream_of(stream)));
+}
+
+moe_status moe_pack_int4(const uint8_t* codes, const uint16_t* scales, const uint8_t* zeros, int64_t matrices,
+                         int64_t rows, int32_t K, int32_t group, uint8_t* out_codes, uint16_t* out_scales,
+                         uint8_t* out_zeros, moe_stream stream) {
+  moe::Check c = moe::validate_pack_int4(codes, scales, zeros, matrices, rows, K, group, out_codes, out_scales,
+                                         out_zeros);
+  if (!c.ok() || matrices == 0 || rows == 0) return finish(c);
+  return hip_status("moe_pack_int4", moe::launch_pack_int4(codes, scales, zeros, matrices, rows, K, group, out_codes,
+                                                           out_scales, out_zeros, stream_of(stream)));
+}
+
+moe_status moe_matvec_int4(const void* x, const uint8_t* codes, const uint16_t* scales, const uint8_t* zeros, int64_t T,
+                           int32_t N, int32_t K, int32_t group, void* y, moe_stream stream) {
+  moe::Check c = moe::validate_matvec_int4(x, codes, scales, zeros, T, N, K, group, y);
+  if (!c.ok() || T == 0) return finish(c);
+  hipError_t err;
+  const int ncu = cu_count(&err);
+  if (err != hipSuccess) return hip_status("moe_matvec_int4", err);
+  return hip_status("moe_matvec_int4",
+                    moe::launch_matvec_int4(static_cast<const uint16_t*>(x), moe::Int4Ref{codes, scales, zeros}, int(T),
+                                            N, K, group, static_cast<uint16_t*>(y), ncu, stream_of(stream)));
+}
+
+// ------------------------------------------------------------------ the layer for few tokens
+size_t moe_few_tokens_workspace_bytes(int64_t T, int32_t k, int32_t F, int32_t Fs) {
+  return moe::few_workspace_bytes(T, k, F, Fs);
+}
+
+moe_status moe_few_tokens(const void* x, const float* logits, int64_t T, int32_t H, int32_t E, int32_t k, int32_t F,
+                          int32_t Fs, int32_t renormalize, const void* w_gate, const void* w_up, const void* w_down,
+                          const void* ws_gate, const void* ws_up, const void* ws_down, int32_t* topk_ids,
+                          float* topk_weights, void* y, void* ws, size_t ws_bytes, moe_stream stream) {
+  const void* const w[6] = {w_gate, w_up, w_down, ws_gate, ws_up, ws_down};
+  moe::Check c = moe::validate_few(x, logits, T, H, E, k, F, Fs, renormalize, w, topk_ids, topk_weights, y, ws,
+                                   ws_bytes);
+  if (!c.ok() || T == 0) return finish(c);
+  hipError_t err;
+  const int ncu = cu_count(&err);
+  if (err != hipSuccess) return hip_status("moe_few_tokens", err);
+  const moe::FewShape s = {static_cast<const uint16_t*>(x), logits, int(T), H, E, k, F, Fs, renormalize, topk_ids,
+                           topk_weights, static_cast<uint16_t*>(ws), static_cast<uint16_t*>(y), ncu};
+  const uint16_t* p[6];
+  for (int i = 0; i < 6; ++i) p[i] = static_cast<const uint16_t*>(w[i]);
+  return hip_status("moe_few_tokens", moe::launch_few_bf16(s, p, stream_of(stream)));
+}
+
+moe_status moe_few_tokens_int4(const void* x, const float* logits, int64_t T, int32_t H, int32_t E, int32_t k,
+                               int32_t F, int32_t Fs, int32_t renormalize, int32_t group, const moe_int4* weights,
+                               int32_t* topk_ids, float* topk_weights, void* y, void* ws, size_t ws_bytes,
+                               moe_stream stream) {
+  moe::Check c = moe::validate_few_int4(x, logits, T, H, E, k, F, Fs, renormalize, group, weights, topk_ids,
+                                        topk_weights, y, ws, ws_bytes);
+  if (!c.ok() || T == 0) return finish(c);
+  hipError_t err;
+  const int ncu = cu_count(&err);
+  if (err != hipSuccess) return hip_status("moe_few_tokens_int4", err);
+  const moe::FewShape s = {static_cast<const uint16_t*>(x), logits, int(T), H, E, k, F, Fs, renormalize, topk_ids,
+                           topk_weights, static_cast<uint16_t*>(ws), static_cast<uint16_t*>(y), ncu};
+  moe::Int4Ref p[6] = {};
+  for (int i = 0; i < (Fs ? 6 : 3); ++i) p[i] = {weights[i].codes, weights[i].scales, weights[i].zeros};
+  return hip_status("moe_few_tokens_int4", moe::launch_few_int4(s, p, group, stream_of(stream)));
+}
+
+// ------------------------------------------------------------------ the paged 8-bit cache
+namespace {
+
+moe::Kv8Cache cache_of(const moe_kv8_cache& c) {
+  return {c.k_codes, c.v_codes, c.k_exps, c.v_exps, c.pages, c.page, c.heads, c.dim};
+}
+
+}  // namespace
+
+moe_status moe_kv8_append(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                          int64_t v_stride, int64_t T, int32_t q_heads, const float* cos_sin, int64_t positions,
+                          int32_t rot, int32_t interleaved, const moe_kv8_cache* cache, const int32_t* block_table,
+                          int32_t table_cols, const int32_t* seq_lens, const int32_t* cu_tokens, int32_t B,
+                          void* q_out, moe_stream stream) {
+  moe::Check c = moe::validate_kv8_append(q, q_stride, k, k_stride, v, v_stride, T, q_heads, cos_sin, positions, rot,
+                                          interleaved, cache, block_table, table_cols, seq_lens, cu_tokens, B, q_out);
+  if (!c.ok() || T == 0) return finish(c);
+  const moe::Kv8Batch b = {block_table, seq_lens, cu_tokens, B, table_cols, T};
+  const moe::Kv8Append a = {static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k),
+                            static_cast<const uint16_t*>(v), q_stride, k_stride, v_stride, cos_sin, positions, rot,
+                            interleaved, q_heads, static_cast<uint16_t*>(q_out)};
+  return hip_status("moe_kv8_append", moe::launch_kv8_append(cache_of(*cache), b, a, stream_of(stream)));
+}
+
+size_t moe_kv8_attention_workspace_bytes(int32_t B, int32_t q_heads, int32_t heads, int32_t dim, int32_t max_new,
+                                         int32_t max_len, int32_t window) {
+  if (!moe::kv8_plan_sizes_ok(B, q_heads, heads, dim, max_new, max_len, window)) return 0;
+  hipError_t err;
+  const int ncu = cu_count(&err);
+  if (err != hipSuccess) return 0;
+  return moe::kv8_workspace_bytes(moe::kv8_plan(B, q_heads, heads, dim, max_new, max_len, window, ncu), B, heads, dim);
+}
+
+moe_status moe_kv8_attention(const void* q, int64_t T, int32_t q_heads, const moe_kv8_cache* cache,
+                             const int32_t* block_table, int32_t table_cols, const int32_t* seq_lens,
+                             const int32_t* cu_tokens, int32_t B, int32_t max_new, int32_t max_len, int32_t window,
+                             float scale, void* out, void* ws, size_t ws_bytes, moe_stream stream) {
+  moe::Kv8Plan plan = {};
+  size_t need = 0;
+  if (T > 0 && cache != nullptr &&
+      moe::kv8_plan_sizes_ok(B, q_heads, cache->heads, cache->dim, max_new, max_len, window)) {
+    hipError_t err;
+    const int ncu = cu_count(&err);
+    if (err != hipSuccess) return hip_status("moe_kv8_attention", err);
+    plan = moe::kv8_plan(B, q_heads, cache->heads, cache->dim, max_new, max_len, window, ncu);
+    need = moe::kv8_workspace_bytes(plan, B, cache->heads, cache->dim);
+  }
+  moe::Check c = moe::validate_kv8_attention(q, T, q_heads, cache, block_table, table_cols, seq_lens, cu_tokens, B,
+                                             max_new, max_len, window, out, ws, ws_bytes, need);
+  if (!c.ok() || T == 0) return finish(c);
+  const moe::Kv8Batch b = {block_table, seq_lens, cu_tokens, B, table_cols, T};
+  const moe::Kv8Attend a = {static_cast<const uint16_t*>(q), q_heads, max_new, max_len, window, scale,
+                            static_cast<uint16_t*>(out), static_cast<float*>(ws)};
+  return hip_status("moe_kv8_attention", moe::launch_kv8_attention(cache_of(*cache), b, a, plan, stream_of(stream)));
+}
+
 }  // extern "C"

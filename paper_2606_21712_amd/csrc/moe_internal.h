@@ -94,4 +94,80 @@ hipError_t launch_stream_gemm2_mxfp8(const uint8_t* h, const uint8_t* hs, const 
 hipError_t launch_combine(const void* y_perm, const int32_t* dest, const float* w, const void* y_shared,
                           int64_t T, int k, int H, bool bf16, void* y, hipStream_t s);
 
+// 4-bit matrices (layout in int4.h): standard row-major codes to and from.
+struct Int4Ref {
+  const uint8_t* codes;
+  const uint16_t* scales;
+  const uint8_t* zeros;   // null: 8 everywhere
+};
+hipError_t launch_quantize_int4(const uint16_t* src, int64_t groups, int group, uint8_t* codes, uint16_t* scales,
+                                uint8_t* zeros, hipStream_t s);
+hipError_t launch_pack_int4(const uint8_t* codes, const uint16_t* scales, const uint8_t* zeros, int64_t matrices,
+                            int64_t rows, int K, int group, uint8_t* out_codes, uint16_t* out_scales,
+                            uint8_t* out_zeros, hipStream_t s);
+hipError_t launch_matvec_int4(const uint16_t* x, const Int4Ref& w, int T, int N, int K, int group, uint16_t* y,
+                              int num_cu, hipStream_t s);
+
+// The layer for at most 16 tokens.  Weights in the order gate, up, down, then the shared expert's
+// (null without one).  h: scratch, bf16 [T, k, F] then [T, Fs].
+struct FewShape {
+  const uint16_t* x;
+  const float* logits;
+  int T, H, E, k, F, Fs, renorm;
+  int32_t* ids;
+  float* wts;
+  uint16_t* h;
+  uint16_t* y;
+  int num_cu;
+};
+hipError_t launch_few_bf16(const FewShape& s, const uint16_t* const (&w)[6], hipStream_t stream);
+hipError_t launch_few_int4(const FewShape& s, const Int4Ref (&w)[6], int group, hipStream_t stream);
+
+// The paged 8-bit key-value cache (layout in kv8.h) and a batch of sequences over it.
+struct Kv8Cache {
+  uint8_t* k_codes;
+  uint8_t* v_codes;
+  uint8_t* k_exps;
+  uint8_t* v_exps;
+  int64_t pages;
+  int page;               // tokens of a page, a multiple of 16
+  int heads, dim;         // kv heads, head size
+};
+struct Kv8Batch {
+  const int32_t* table;   // [sequences, table_cols] page of each of a sequence's pages
+  const int32_t* lens;    // [sequences] tokens, the new ones included
+  const int32_t* cu;      // [sequences + 1] rows of the new tokens
+  int sequences, table_cols;
+  int64_t tokens;         // rows of new tokens
+};
+struct Kv8Append {
+  const uint16_t *q, *k, *v;
+  int64_t q_stride, k_stride, v_stride;   // elements from one token to the next
+  const float* cos_sin;                   // [positions, rot]
+  int64_t positions;
+  int rot, interleaved;
+  int q_heads;
+  uint16_t* q_out;                        // [tokens, q_heads, dim]
+};
+hipError_t launch_kv8_append(const Kv8Cache& c, const Kv8Batch& b, const Kv8Append& a, hipStream_t s);
+
+struct Kv8Attend {
+  const uint16_t* q;                      // [tokens, q_heads, dim]
+  int q_heads;
+  int max_new, max_len;
+  int window;                             // 0: none
+  float scale;
+  uint16_t* out;
+  float* ws;
+};
+// How an attention call is cut up: `rows` query rows (token, head of the group) a tile, `tiles`
+// tiles for the sequence with the most new tokens, each tile's tokens in `splits` parts.
+struct Kv8Plan {
+  int rows, tiles, splits;
+};
+Kv8Plan kv8_plan(int sequences, int q_heads, int heads, int dim, int max_new, int max_len, int64_t window, int num_cu);
+size_t kv8_workspace_bytes(const Kv8Plan& p, int sequences, int heads, int dim);
+hipError_t launch_kv8_attention(const Kv8Cache& c, const Kv8Batch& b, const Kv8Attend& a, const Kv8Plan& p,
+                                hipStream_t s);
+
 }  // namespace moe

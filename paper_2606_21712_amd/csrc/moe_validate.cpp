@@ -377,4 +377,269 @@ Check validate_combine(const void* y_perm, const int32_t* dest, const float* w, 
   return Check{};
 }
 
+// ------------------------------------------------------------------ 4-bit weights
+namespace {
+
+constexpr int64_t kInt4MaxDim = int64_t(1) << 24;
+
+bool int4_group_ok(int32_t group) { return group == 32 || group == 64 || group == 128; }
+
+Check int4_dims(const char* fn, int32_t K, int32_t group) {
+  if (!int4_group_ok(group))
+    return fail(MOE_ERR_INVALID_ARGUMENT, fn, "group=%lld must be 32, 64 or 128", group);
+  if (K < 1 || K % group != 0)
+    return fail(MOE_ERR_INVALID_ARGUMENT, fn, "K=%lld must be a positive multiple of group=%lld", K, group);
+  if (K > kInt4MaxDim) return fail(MOE_ERR_UNSUPPORTED, fn, "K=%lld exceeds %lld", K, kInt4MaxDim);
+  return Check{};
+}
+
+size_t up16(int64_t rows) { return size_t(rows + 15) / 16 * 16; }
+size_t up128(int32_t K) { return size_t(int64_t(K) + 127) / 128 * 128; }
+
+}  // namespace
+
+size_t int4_code_bytes(int64_t rows, int32_t K) {
+  if (rows <= 0 || K <= 0 || rows > INT64_MAX / (int64_t(1) << 32)) return 0;
+  return up16(rows) * (up128(K) / 2);
+}
+
+size_t int4_groups(int64_t rows, int32_t K, int32_t group) {
+  if (rows <= 0 || K <= 0 || !int4_group_ok(group) || rows > INT64_MAX / (int64_t(1) << 32)) return 0;
+  return up16(rows) * (up128(K) / size_t(group));
+}
+
+Check validate_quantize_int4(const void* src, int64_t rows, int32_t K, int32_t group, const void* codes,
+                             const void* scales, const void* zeros) {
+  const char* fn = "moe_quantize_int4";
+  MOE_TRY(int4_dims(fn, K, group));
+  if (rows < 0) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "rows=%lld is negative", rows);
+  // one thread a group, fewer than 2^32 threads
+  if (rows > ((int64_t(1) << 31) / (K / group)))
+    return fail(MOE_ERR_UNSUPPORTED, fn, "rows=%lld of %lld groups are too many", rows, K / group);
+  if (rows == 0) return Check{};
+  MOE_TRY(ptr(fn, "src", src));
+  MOE_TRY(ptr(fn, "codes", codes));
+  MOE_TRY(ptr(fn, "scales", scales));
+  if (zeros != nullptr) MOE_TRY(ptr(fn, "zeros", zeros));
+  return Check{};
+}
+
+Check validate_pack_int4(const void* codes, const void* scales, const void* zeros, int64_t matrices, int64_t rows,
+                         int32_t K, int32_t group, const void* out_codes, const void* out_scales,
+                         const void* out_zeros) {
+  const char* fn = "moe_pack_int4";
+  MOE_TRY(int4_dims(fn, K, group));
+  if (matrices < 0) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "matrices=%lld is negative", matrices);
+  if (rows < 0) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "rows=%lld is negative", rows);
+  if ((zeros == nullptr) != (out_zeros == nullptr))
+    return fail(MOE_ERR_INVALID_ARGUMENT, fn, "zeros and out_zeros go together");
+  if (matrices == 0 || rows == 0) return Check{};
+  // one workgroup of 64 threads a tile, fewer than 2^32 threads
+  const int64_t most = int64_t(1) << 26;
+  const int64_t ct = int64_t(up128(K)) / 128;
+  if (rows > most * 16 || int64_t(up16(rows)) / 16 > most / ct ||
+      matrices > most / (int64_t(up16(rows)) / 16 * ct))
+    return fail(MOE_ERR_UNSUPPORTED, fn, "%lld matrices of %lld rows are too many tiles", matrices, rows);
+  MOE_TRY(ptr(fn, "codes", codes));
+  MOE_TRY(ptr(fn, "scales", scales));
+  MOE_TRY(ptr(fn, "out_codes", out_codes));
+  MOE_TRY(ptr(fn, "out_scales", out_scales));
+  if (zeros != nullptr) {
+    MOE_TRY(ptr(fn, "zeros", zeros));
+    MOE_TRY(ptr(fn, "out_zeros", out_zeros));
+  }
+  return Check{};
+}
+
+Check validate_matvec_int4(const void* x, const void* codes, const void* scales, const void* zeros, int64_t T,
+                           int32_t N, int32_t K, int32_t group, const void* y) {
+  const char* fn = "moe_matvec_int4";
+  MOE_TRY(int4_dims(fn, K, group));
+  if (T < 0) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "T=%lld is negative", T);
+  if (N < 1) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "N=%lld must be >= 1", N);
+  if (T > (1 << 20)) return fail(MOE_ERR_UNSUPPORTED, fn, "T=%lld exceeds %lld", T, 1 << 20);
+  if (N > kInt4MaxDim) return fail(MOE_ERR_UNSUPPORTED, fn, "N=%lld exceeds %lld", N, kInt4MaxDim);
+  if (T == 0) return Check{};
+  MOE_TRY(ptr(fn, "x", x));
+  MOE_TRY(ptr(fn, "codes", codes));
+  MOE_TRY(ptr(fn, "scales", scales));
+  if (zeros != nullptr) MOE_TRY(ptr(fn, "zeros", zeros));
+  MOE_TRY(ptr(fn, "y", y));
+  return Check{};
+}
+
+// ------------------------------------------------------------------ the layer for few tokens
+size_t few_workspace_bytes(int64_t T, int32_t k, int32_t F, int32_t Fs) {
+  if (T <= 0 || T > MOE_FEW_TOKENS || k < 1 || k > MOE_MAX_TOPK || F < 1 || Fs < 0) return 0;
+  return align256(size_t(T) * (size_t(k) * size_t(F) + size_t(Fs)) * 2);
+}
+
+namespace {
+
+const char* const kFewNames[6] = {"w_gate", "w_up", "w_down", "ws_gate", "ws_up", "ws_down"};
+
+Check few_sizes(const char* fn, int64_t T, int32_t H, int32_t E, int32_t k, int32_t F, int32_t Fs,
+                int32_t renormalize) {
+  MOE_TRY(experts_topk(fn, E, k));
+  MOE_TRY(tokens(fn, T, k));
+  if (T > MOE_FEW_TOKENS) return fail(MOE_ERR_UNSUPPORTED, fn, "T=%lld exceeds %lld", T, MOE_FEW_TOKENS);
+  MOE_TRY(dim64(fn, "H", H));
+  MOE_TRY(dim64(fn, "F", F));
+  if (Fs != 0) MOE_TRY(dim64(fn, "Fs", Fs));
+  if (H > (1 << 20) || F > (1 << 20) || Fs > (1 << 20))
+    return fail(MOE_ERR_UNSUPPORTED, fn, "H=%lld, F=%lld or Fs exceeds 2^20", H, F);
+  if (renormalize != 0 && renormalize != 1)
+    return fail(MOE_ERR_INVALID_ARGUMENT, fn, "renormalize=%lld must be 0 or 1", renormalize);
+  return Check{};
+}
+
+Check few_buffers(const char* fn, const void* x, const void* logits, int64_t T, int32_t k, int32_t F, int32_t Fs,
+                  const void* ids, const void* wts, const void* y, const void* ws, size_t ws_bytes) {
+  MOE_TRY(ptr(fn, "x", x));
+  MOE_TRY(ptr(fn, "logits", logits));
+  MOE_TRY(ptr(fn, "topk_ids", ids));
+  MOE_TRY(ptr(fn, "topk_weights", wts));
+  MOE_TRY(ptr(fn, "y", y));
+  const size_t need = few_workspace_bytes(T, k, F, Fs);
+  if (ws_bytes < need)
+    return fail(MOE_ERR_WORKSPACE_TOO_SMALL, fn, "workspace %lld bytes < %lld needed",
+                (long long)ws_bytes, (long long)need);
+  return ptr(fn, "ws", ws);
+}
+
+}  // namespace
+
+Check validate_few(const void* x, const void* logits, int64_t T, int32_t H, int32_t E, int32_t k, int32_t F,
+                   int32_t Fs, int32_t renormalize, const void* const (&w)[6], const void* ids, const void* wts,
+                   const void* y, const void* ws, size_t ws_bytes) {
+  const char* fn = "moe_few_tokens";
+  MOE_TRY(few_sizes(fn, T, H, E, k, F, Fs, renormalize));
+  if (T == 0) return Check{};
+  for (int i = 0; i < (Fs ? 6 : 3); ++i) MOE_TRY(ptr(fn, kFewNames[i], w[i]));
+  return few_buffers(fn, x, logits, T, k, F, Fs, ids, wts, y, ws, ws_bytes);
+}
+
+Check validate_few_int4(const void* x, const void* logits, int64_t T, int32_t H, int32_t E, int32_t k, int32_t F,
+                        int32_t Fs, int32_t renormalize, int32_t group, const moe_int4* w, const void* ids,
+                        const void* wts, const void* y, const void* ws, size_t ws_bytes) {
+  const char* fn = "moe_few_tokens_int4";
+  MOE_TRY(few_sizes(fn, T, H, E, k, F, Fs, renormalize));
+  MOE_TRY(int4_dims(fn, H, group));
+  MOE_TRY(int4_dims(fn, F, group));
+  if (Fs) MOE_TRY(int4_dims(fn, Fs, group));
+  if (T == 0) return Check{};
+  if (w == nullptr) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "weights is NULL");
+  for (int i = 0; i < (Fs ? 6 : 3); ++i) {
+    MOE_TRY(ptr(fn, kFewNames[i], w[i].codes));
+    MOE_TRY(ptr(fn, kFewNames[i], w[i].scales));
+    if ((w[i].zeros == nullptr) != (w[0].zeros == nullptr))
+      return fail(MOE_ERR_INVALID_ARGUMENT, fn, "zeros: all tensors have them or none");
+    if (w[i].zeros != nullptr) MOE_TRY(ptr(fn, kFewNames[i], w[i].zeros));
+  }
+  return few_buffers(fn, x, logits, T, k, F, Fs, ids, wts, y, ws, ws_bytes);
+}
+
+// ------------------------------------------------------------------ the paged 8-bit cache
+namespace {
+
+Check kv8_sizes(const char* fn, int64_t T, int32_t q_heads, int32_t heads, int32_t dim, int32_t page, int64_t pages,
+                int32_t table_cols, int32_t B) {
+  if (dim != 64 && dim != 128 && dim != 256) return fail(MOE_ERR_UNSUPPORTED, fn, "dim=%lld is not 64, 128 or 256", dim);
+  if (page < MOE_KV8_BLOCK || page % MOE_KV8_BLOCK != 0)
+    return fail(MOE_ERR_INVALID_ARGUMENT, fn, "page=%lld must be a positive multiple of %lld", page, MOE_KV8_BLOCK);
+  if (heads < 1) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "heads=%lld must be >= 1", heads);
+  if (heads > 65535) return fail(MOE_ERR_UNSUPPORTED, fn, "heads=%lld exceeds 65535", heads);
+  if (q_heads < 1 || q_heads % heads != 0)
+    return fail(MOE_ERR_INVALID_ARGUMENT, fn, "q_heads=%lld must be a positive multiple of heads=%lld", q_heads, heads);
+  if (q_heads > 65535) return fail(MOE_ERR_UNSUPPORTED, fn, "q_heads=%lld exceeds 65535", q_heads);
+  if (pages < 1) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "pages=%lld must be >= 1", pages);
+  if (table_cols < 1) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "table_cols=%lld must be >= 1", table_cols);
+  if (pages > (int64_t(1) << 31) || page > (1 << 20))
+    return fail(MOE_ERR_UNSUPPORTED, fn, "%lld pages of %lld tokens are too many", pages, page);
+  if (int64_t(table_cols) * page > INT32_MAX)
+    return fail(MOE_ERR_UNSUPPORTED, fn, "table_cols=%lld times page=%lld exceeds INT32_MAX", table_cols, page);
+  if (T < 0) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "T=%lld is negative", T);
+  if (B < 0) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "B=%lld is negative", B);
+  if (T > 0 && B == 0) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "T=%lld rows but no sequence", T);
+  if (T >= (1 << 24) || T + 2 * int64_t(B) >= (1 << 24))
+    return fail(MOE_ERR_UNSUPPORTED, fn, "T=%lld rows of B=%lld sequences are too many", T, B);
+  return Check{};
+}
+
+Check kv8_buffers(const char* fn, const moe_kv8_cache* c, const void* table, const void* lens, const void* cu) {
+  MOE_TRY(ptr(fn, "k_codes", c->k_codes));
+  MOE_TRY(ptr(fn, "v_codes", c->v_codes));
+  MOE_TRY(ptr(fn, "k_exps", c->k_exps));
+  MOE_TRY(ptr(fn, "v_exps", c->v_exps));
+  MOE_TRY(ptr(fn, "block_table", table));
+  MOE_TRY(ptr(fn, "seq_lens", lens));
+  return ptr(fn, "cu_tokens", cu);
+}
+
+Check row_stride(const char* fn, const char* what, int64_t stride, int64_t width) {
+  if (stride >= width && stride % 8 == 0 && stride < (int64_t(1) << 32)) return Check{};
+  Check c = fail(MOE_ERR_INVALID_ARGUMENT, fn, "row stride %lld must be a multiple of 8, at least %lld", stride, width);
+  c.msg += std::string(" (") + what + ")";
+  return c;
+}
+
+}  // namespace
+
+Check validate_kv8_append(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                          int64_t v_stride, int64_t T, int32_t q_heads, const void* cos_sin, int64_t positions,
+                          int32_t rot, int32_t interleaved, const moe_kv8_cache* cache, const void* table,
+                          int32_t table_cols, const void* lens, const void* cu, int32_t B, const void* q_out) {
+  const char* fn = "moe_kv8_append";
+  if (cache == nullptr) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "cache is NULL");
+  MOE_TRY(kv8_sizes(fn, T, q_heads, cache->heads, cache->dim, cache->page, cache->pages, table_cols, B));
+  if (rot < 0 || rot > cache->dim || rot % 16 != 0)
+    return fail(MOE_ERR_INVALID_ARGUMENT, fn, "rot=%lld must be a multiple of 16, at most dim=%lld", rot, cache->dim);
+  if (interleaved != 0 && interleaved != 1)
+    return fail(MOE_ERR_INVALID_ARGUMENT, fn, "interleaved=%lld must be 0 or 1", interleaved);
+  if (T == 0) return Check{};
+  if (rot > 0 && positions < 1) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "positions=%lld must be >= 1", positions);
+  MOE_TRY(row_stride(fn, "q", q_stride, int64_t(q_heads) * cache->dim));
+  MOE_TRY(row_stride(fn, "k", k_stride, int64_t(cache->heads) * cache->dim));
+  MOE_TRY(row_stride(fn, "v", v_stride, int64_t(cache->heads) * cache->dim));
+  MOE_TRY(ptr(fn, "q", q));
+  MOE_TRY(ptr(fn, "k", k));
+  MOE_TRY(ptr(fn, "v", v));
+  if (rot > 0) MOE_TRY(ptr(fn, "cos_sin", cos_sin));
+  MOE_TRY(kv8_buffers(fn, cache, table, lens, cu));
+  return ptr(fn, "q_out", q_out);
+}
+
+bool kv8_plan_sizes_ok(int32_t B, int32_t q_heads, int32_t heads, int32_t dim, int32_t max_new, int32_t max_len,
+                       int32_t window) {
+  if (B < 1 || heads < 1 || heads > 65535 || q_heads < 1 || q_heads > 65535 || q_heads % heads != 0) return false;
+  if (dim != 64 && dim != 128 && dim != 256) return false;
+  if (max_new < 1 || max_len < 0 || window < 0 || max_new >= (1 << 24)) return false;
+  // a tile's rows are counted in 32 bits, and so are the workgroups
+  const int64_t rows = int64_t(max_new) * (q_heads / heads);
+  return rows <= INT32_MAX - 64 && (rows + 15) / 16 <= INT32_MAX / 256 / (int64_t(B) * heads);
+}
+
+Check validate_kv8_attention(const void* q, int64_t T, int32_t q_heads, const moe_kv8_cache* cache, const void* table,
+                             int32_t table_cols, const void* lens, const void* cu, int32_t B, int32_t max_new,
+                             int32_t max_len, int32_t window, const void* out, const void* ws, size_t ws_bytes,
+                             size_t need) {
+  const char* fn = "moe_kv8_attention";
+  if (cache == nullptr) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "cache is NULL");
+  MOE_TRY(kv8_sizes(fn, T, q_heads, cache->heads, cache->dim, cache->page, cache->pages, table_cols, B));
+  if (max_len < 0) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "max_len=%lld is negative", max_len);
+  if (window < 0) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "window=%lld is negative", window);
+  if (T == 0) return Check{};
+  if (max_new < 1) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "max_new=%lld must be >= 1", max_new);
+  if (!kv8_plan_sizes_ok(B, q_heads, cache->heads, cache->dim, max_new, max_len, window))
+    return fail(MOE_ERR_UNSUPPORTED, fn, "max_new=%lld rows of B=%lld sequences are too many", max_new, B);
+  MOE_TRY(ptr(fn, "q", q));
+  MOE_TRY(kv8_buffers(fn, cache, table, lens, cu));
+  MOE_TRY(ptr(fn, "out", out));
+  if (ws_bytes < need)
+    return fail(MOE_ERR_WORKSPACE_TOO_SMALL, fn, "workspace %lld bytes < %lld needed",
+                (long long)ws_bytes, (long long)need);
+  if (need > 0) MOE_TRY(ptr(fn, "ws", ws));
+  return Check{};
+}
+
 }  // namespace moe

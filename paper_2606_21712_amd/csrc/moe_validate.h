@@ -66,4 +66,34 @@ Check validate_ffn_mxfp8_gather(const void* x, const void* xs, const int32_t* so
 Check validate_combine(const void* y_perm, const int32_t* dest, const float* w, const void* y_shared,
                        int64_t T, int32_t k, int32_t H, int dt, const void* y);
 
+// 4-bit weights: packed sizes of one matrix
+size_t int4_code_bytes(int64_t rows, int32_t K);
+size_t int4_groups(int64_t rows, int32_t K, int32_t group);
+Check validate_quantize_int4(const void* src, int64_t rows, int32_t K, int32_t group, const void* codes,
+                             const void* scales, const void* zeros);
+Check validate_pack_int4(const void* codes, const void* scales, const void* zeros, int64_t matrices, int64_t rows,
+                         int32_t K, int32_t group, const void* out_codes, const void* out_scales,
+                         const void* out_zeros);
+Check validate_matvec_int4(const void* x, const void* codes, const void* scales, const void* zeros, int64_t T,
+                           int32_t N, int32_t K, int32_t group, const void* y);
+// The layer for few tokens: weights in the order gate, up, down, shared gate, up, down; workspace h
+size_t few_workspace_bytes(int64_t T, int32_t k, int32_t F, int32_t Fs);
+Check validate_few(const void* x, const void* logits, int64_t T, int32_t H, int32_t E, int32_t k, int32_t F,
+                   int32_t Fs, int32_t renormalize, const void* const (&w)[6], const void* ids, const void* wts,
+                   const void* y, const void* ws, size_t ws_bytes);
+Check validate_few_int4(const void* x, const void* logits, int64_t T, int32_t H, int32_t E, int32_t k, int32_t F,
+                        int32_t Fs, int32_t renormalize, int32_t group, const moe_int4* w, const void* ids,
+                        const void* wts, const void* y, const void* ws, size_t ws_bytes);
+// The paged 8-bit cache
+Check validate_kv8_append(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                          int64_t v_stride, int64_t T, int32_t q_heads, const void* cos_sin, int64_t positions,
+                          int32_t rot, int32_t interleaved, const moe_kv8_cache* cache, const void* table,
+                          int32_t table_cols, const void* lens, const void* cu, int32_t B, const void* q_out);
+Check validate_kv8_attention(const void* q, int64_t T, int32_t q_heads, const moe_kv8_cache* cache, const void* table,
+                             int32_t table_cols, const void* lens, const void* cu, int32_t B, int32_t max_new,
+                             int32_t max_len, int32_t window, const void* out, const void* ws, size_t ws_bytes,
+                             size_t need);
+bool kv8_plan_sizes_ok(int32_t B, int32_t q_heads, int32_t heads, int32_t dim, int32_t max_new, int32_t max_len,
+                       int32_t window);
+
 }  // namespace moe
