@@ -339,18 +339,18 @@ moe_status moe_combine(const void* y_perm, const int32_t* dest_rows, const float
  *   standard  codes u8 [rows, K / 2], the even column in the low nibble; scales bf16
  *             [rows, K / group]; zeros u8 [rows, K / group]
  *   packed    what the kernels read, rows padded to 16 and columns to 128: codes u8
- *             [rows / 16][K / 128][1024], a tile of 16 rows x 128 columns in one piece:
- *             byte 16 l + 4 j + b of a tile belongs to row l % 16 and holds columns
- *             32 j + 8 (l / 16) + {2 b, 2 b + 4 ... } in the order
- *             nibble p = 2 b (+ 1 for the high one): column offset 2 p for p < 4,
- *             2 (p - 4) + 1 for p >= 4; scales bf16 and zeros u8 [rows / 16][K / group][16]
+ *             [rows / 16][K / 128][1024], a tile of 16 rows x 128 columns in one piece.
+ *             Word j of the four words 16 l .. 16 l + 15 of a tile holds row l % 16, columns
+ *             32 j + 8 (l / 16) + 0..7: nibble p column 2 p for p < 4, 2 (p - 4) + 1 for
+ *             p >= 4.  Scales [rows / 16][K / 128][4][128 / group][4], the last for rows
+ *             4 a + 0..3: bf16; with zero points 32-bit words, the upper half the scale, the
+ *             lower half 128 + zero, both bf16.
  *
- * moe_int4_code_bytes and moe_int4_groups give the packed sizes of one matrix: bytes of
- * codes, and scales (= zeros) in number.  An expert tensor [E, N, K] is E packed matrices
- * one after the other.
+ * moe_int4_code_bytes and moe_int4_scale_bytes (zeros: 0 or 1) give the packed sizes of one
+ * matrix.  An expert tensor [E, N, K] is E packed matrices one after the other.
  */
 size_t moe_int4_code_bytes(int64_t rows, int32_t K);
-size_t moe_int4_groups(int64_t rows, int32_t K, int32_t group);
+size_t moe_int4_scale_bytes(int64_t rows, int32_t K, int32_t group, int32_t zeros);
 
 /*
  * moe_quantize_int4 - bf16 rows to standard 4-bit codes.
@@ -363,35 +363,36 @@ size_t moe_int4_groups(int64_t rows, int32_t K, int32_t group);
  * + zero.  Both clamped to 0..15, ties to even, the quotients by the scale as rounded.  A group
  * of zeros has scale 0.  Inputs are finite (not checked).
  * Errors: INVALID_ARGUMENT for rows < 0, an unknown group, K not a positive multiple of
- * the group, null or misaligned pointers; UNSUPPORTED for 2^39 groups or more.
+ * the group, null or misaligned pointers; UNSUPPORTED for 2^31 groups or more.
  */
 moe_status moe_quantize_int4(const void* src, int64_t rows, int32_t K, int32_t group, uint8_t* codes,
                              uint16_t* scales, uint8_t* zeros, moe_stream stream);
 
 /*
- * moe_pack_int4 - standard to packed form, of `matrices` matrices of rows x K each.
- * zeros and out_zeros are both NULL or both given.  Run once when weights are loaded.
- * Errors: as moe_quantize_int4, plus INVALID_ARGUMENT for matrices < 0, one of the two zeros
- * without the other; UNSUPPORTED for 2^26 tiles or more.
+ * moe_pack_int4 - standard to packed form, of `matrices` matrices of rows x K each; zeros may be
+ * NULL (out_scales then without them).  Run once when weights are loaded.
+ * Errors: as moe_quantize_int4, plus INVALID_ARGUMENT for matrices < 0; UNSUPPORTED for 2^26
+ * tiles or more.
  */
 moe_status moe_pack_int4(const uint8_t* codes, const uint16_t* scales, const uint8_t* zeros, int64_t matrices,
-                         int64_t rows, int32_t K, int32_t group, uint8_t* out_codes, uint16_t* out_scales,
-                         uint8_t* out_zeros, moe_stream stream);
+                         int64_t rows, int32_t K, int32_t group, uint8_t* out_codes, uint8_t* out_scales,
+                         moe_stream stream);
 
 /*
  * moe_matvec_int4 - y = x W^T for a 4-bit W and few rows of x.
  *
  *   x       bf16 [T, K]
- *   codes, scales, zeros   packed W [N, K]; zeros may be NULL
+ *   codes, scales   packed W [N, K], zeros 1 where it has zero points, else 0
  *   y       bf16 [T, N]   out
  *
  * Codes are multiplied as integers in bf16 (exact) on the matrix cores, sums of a group in
  * fp32, scaled and added up in fp32, rounded once.  The weights are read once for each 64
  * rows of x: any T is right, few rows are what it is for.  x finite: an infinite x gives NaN.
  * Errors: INVALID_ARGUMENT for T < 0, N < 1, an unknown group, K not a positive multiple of
- * the group, null or misaligned pointers; UNSUPPORTED for T > 2^20, N or K > 2^24.
+ * the group, null or misaligned pointers; UNSUPPORTED for T > 2^20, K > 2^23 or 2 GiB of
+ * codes or scales.
  */
-moe_status moe_matvec_int4(const void* x, const uint8_t* codes, const uint16_t* scales, const uint8_t* zeros, int64_t T,
+moe_status moe_matvec_int4(const void* x, const uint8_t* codes, const uint8_t* scales, int32_t zeros, int64_t T,
                            int32_t N, int32_t K, int32_t group, void* y, moe_stream stream);
 
 /*
@@ -407,29 +408,30 @@ moe_status moe_matvec_int4(const void* x, const uint8_t* codes, const uint16_t* 
  *   topk_ids i32, topk_weights f32 [T, k]   out, as moe_route
  *   y               bf16 [T, H]    out
  *   ws, ws_bytes    device scratch of at least moe_few_tokens_workspace_bytes(): the rows h
+ *                   and the parts of y's sums; not to be shared by calls that overlap
  *
- * The gate weight multiplies silu(g) u in fp32 before h is rounded to bf16; all sums are fp32,
- * y is rounded once.  Deterministic; the order of y's sums depends on the experts that the
+ * The gate weight multiplies silu(g) u in fp32; h is kept to 16 significant bits (two bf16
+ * numbers), all sums are fp32, y is rounded once.  Deterministic; the order of y's sums depends on the experts that the
  * batch chose, so a token's y may differ in its last bit with the tokens beside it.
  * Errors: as moe_route and moe_grouped_ffn, plus INVALID_ARGUMENT for Fs < 0 or not a
- * multiple of 64, T > 16 (UNSUPPORTED).
+ * multiple of 64; UNSUPPORTED for T > 16.
  *
  * moe_few_tokens_int4 takes 4-bit weights: `weights` is a HOST array of six packed tensors in
- * the order w_gate, w_up, w_down, ws_gate, ws_up, ws_down, of one group size; either all have
- * zeros or none.  H and F (and Fs) are multiples of the group.
+ * the order w_gate, w_up, w_down, ws_gate, ws_up, ws_down, of one group size, all with zero
+ * points (zeros = 1) or all without (0).  H and F (and Fs) are multiples of the group.
  */
 typedef struct {
     const uint8_t* codes;
-    const uint16_t* scales;
-    const uint8_t* zeros;            /* NULL: 8 */
+    const uint8_t* scales;
 } moe_int4;
-size_t moe_few_tokens_workspace_bytes(int64_t T, int32_t k, int32_t F, int32_t Fs);
+size_t moe_few_tokens_workspace_bytes(int64_t T, int32_t H, int32_t k, int32_t F, int32_t Fs);
 moe_status moe_few_tokens(const void* x, const float* logits, int64_t T, int32_t H, int32_t E, int32_t k, int32_t F,
                           int32_t Fs, int32_t renormalize, const void* w_gate, const void* w_up, const void* w_down,
                           const void* ws_gate, const void* ws_up, const void* ws_down, int32_t* topk_ids,
                           float* topk_weights, void* y, void* ws, size_t ws_bytes, moe_stream stream);
 moe_status moe_few_tokens_int4(const void* x, const float* logits, int64_t T, int32_t H, int32_t E, int32_t k,
-                               int32_t F, int32_t Fs, int32_t renormalize, int32_t group, const moe_int4* weights,
+                               int32_t F, int32_t Fs, int32_t renormalize, int32_t group, int32_t zeros,
+                               const moe_int4* weights,
                                int32_t* topk_ids, float* topk_weights, void* y, void* ws, size_t ws_bytes,
                                moe_stream stream);
 

@@ -22,7 +22,7 @@ __all__ = [
     "moe_mxfp8_scale_bytes", "moe_quantize_mxfp8", "moe_grouped_ffn_mxfp8_workspace_bytes",
     "moe_grouped_ffn_mxfp8", "moe_grouped_ffn_mxfp8_gather", "MXFP8", "quantize_weights_mxfp8",
     "MoELayerMXFP8", "LayerGraph",
-    "Int4", "moe_int4_code_bytes", "moe_int4_groups", "moe_quantize_int4", "moe_pack_int4", "quantize_weights_int4",
+    "Int4", "moe_int4_code_bytes", "moe_int4_scale_bytes", "moe_quantize_int4", "moe_pack_int4", "quantize_weights_int4",
     "moe_matvec_int4", "moe_few_tokens", "moe_few_tokens_workspace_bytes", "MoELayerFew", "FEW_TOKENS",
     "KVCache8", "KV8_BLOCK", "moe_kv8_append", "moe_kv8_attention", "moe_kv8_attention_workspace_bytes",
     "profiler_start", "profiler_select", "profiler_stop", "profiler_records", "set_cu_budget",
@@ -56,7 +56,7 @@ _SZ = ctypes.c_size_t
 
 class _Int4Ref(ctypes.Structure):
     """moe_int4"""
-    _fields_ = [("codes", _P), ("scales", _P), ("zeros", _P)]
+    _fields_ = [("codes", _P), ("scales", _P)]
 
 
 class _Kv8Cache(ctypes.Structure):
@@ -90,14 +90,14 @@ _SIGNATURES = {
     "moe_grouped_ffn_mxfp8_gather": (ctypes.c_int, [_P, _P, _P, _P, _I64, _I64, _I32, _I32, _I32, _P, _P, _P, _P,
                                                     _P, _P, _P, _P, _SZ, _P]),
     "moe_int4_code_bytes": (_SZ, [_I64, _I32]),
-    "moe_int4_groups": (_SZ, [_I64, _I32, _I32]),
+    "moe_int4_scale_bytes": (_SZ, [_I64, _I32, _I32, _I32]),
     "moe_quantize_int4": (ctypes.c_int, [_P, _I64, _I32, _I32, _P, _P, _P, _P]),
-    "moe_pack_int4": (ctypes.c_int, [_P, _P, _P, _I64, _I64, _I32, _I32, _P, _P, _P, _P]),
-    "moe_matvec_int4": (ctypes.c_int, [_P, _P, _P, _P, _I64, _I32, _I32, _I32, _P, _P]),
-    "moe_few_tokens_workspace_bytes": (_SZ, [_I64, _I32, _I32, _I32]),
+    "moe_pack_int4": (ctypes.c_int, [_P, _P, _P, _I64, _I64, _I32, _I32, _P, _P, _P]),
+    "moe_matvec_int4": (ctypes.c_int, [_P, _P, _P, _I32, _I64, _I32, _I32, _I32, _P, _P]),
+    "moe_few_tokens_workspace_bytes": (_SZ, [_I64, _I32, _I32, _I32, _I32]),
     "moe_few_tokens": (ctypes.c_int, [_P, _P, _I64, _I32, _I32, _I32, _I32, _I32, _I32, _P, _P, _P, _P, _P, _P, _P, _P,
                                       _P, _P, _SZ, _P]),
-    "moe_few_tokens_int4": (ctypes.c_int, [_P, _P, _I64, _I32, _I32, _I32, _I32, _I32, _I32, _I32,
+    "moe_few_tokens_int4": (ctypes.c_int, [_P, _P, _I64, _I32, _I32, _I32, _I32, _I32, _I32, _I32, _I32,
                                            ctypes.POINTER(_Int4Ref), _P, _P, _P, _P, _SZ, _P]),
     "moe_kv8_append": (ctypes.c_int, [_P, _I64, _P, _I64, _P, _I64, _I64, _I32, _P, _I64, _I32, _I32,
                                       ctypes.POINTER(_Kv8Cache), _P, _I32, _P, _P, _I32, _P, _P]),
@@ -399,11 +399,11 @@ def moe_grouped_ffn_mxfp8_gather(x, sorted_token_ids, offsets, w_gate, w_up, w_d
 
 # --------------------------------------------------------------------------- 4-bit weights
 class Int4:
-    """A packed 4-bit matrix, or a tensor [E, N, K] of such matrices (include/moe.h): codes u8,
-    scales bf16 and zero points u8 (or None) in the library's tiled layout."""
+    """A packed 4-bit matrix, or a tensor [E, N, K] of such matrices (include/moe.h): codes and scales u8
+    in the library's tiled layout; zeros: whether there are zero points."""
 
     def __init__(self, codes, scales, zeros, shape, group):
-        self.codes, self.scales, self.zeros = codes, scales, zeros
+        self.codes, self.scales, self.zeros = codes, scales, bool(zeros)
         self.shape, self.group = tuple(shape), group
 
 
@@ -411,8 +411,8 @@ def moe_int4_code_bytes(rows, K) -> int:
     return lib().moe_int4_code_bytes(rows, K)
 
 
-def moe_int4_groups(rows, K, group) -> int:
-    return lib().moe_int4_groups(rows, K, group)
+def moe_int4_scale_bytes(rows, K, group, zeros=False) -> int:
+    return lib().moe_int4_scale_bytes(rows, K, group, 1 if zeros else 0)
 
 
 def moe_quantize_int4(w, group=128, zeros=False, stream=None):
@@ -444,14 +444,13 @@ def moe_pack_int4(codes, scales, zeros=None, group=128, stream=None):
     for n in lead:
         mats *= n
     dev = codes.device
-    groups = mats * moe_int4_groups(N, K, group)
+    z = zeros is not None
     out = Int4(torch.empty(max(1, mats * moe_int4_code_bytes(N, K)), dtype=torch.uint8, device=dev),
-               torch.empty(max(1, groups), dtype=torch.bfloat16, device=dev),
-               None if zeros is None else torch.empty(max(1, groups), dtype=torch.uint8, device=dev), (*lead, N, K),
-               group)
+               torch.empty(max(1, mats * moe_int4_scale_bytes(N, K, group, z)), dtype=torch.uint8, device=dev), z,
+               (*lead, N, K), group)
     _dev(codes, scales, zeros, out.codes)
     _check(lib().moe_pack_int4(_ptr(codes), _ptr(scales), _ptr(zeros), mats, N, K, group, _ptr(out.codes),
-                               _ptr(out.scales), _ptr(out.zeros), _stream(stream, dev)))
+                               _ptr(out.scales), _stream(stream, dev)))
     return out
 
 
@@ -473,14 +472,14 @@ def moe_matvec_int4(x, w, y=None, stream=None):
     elif y.dtype != torch.bfloat16 or tuple(y.shape) != (T, N):
         raise ValueError(f"y must be bf16 [{T}, {N}]")
     _dev(x, w.codes, y)
-    _check(lib().moe_matvec_int4(_ptr(x), _ptr(w.codes), _ptr(w.scales), _ptr(w.zeros), T, N, K, w.group, _ptr(y),
+    _check(lib().moe_matvec_int4(_ptr(x), _ptr(w.codes), _ptr(w.scales), w.zeros, T, N, K, w.group, _ptr(y),
                                  _stream(stream, x.device)))
     return y
 
 
 # --------------------------------------------------------------------------- the layer for few tokens
-def moe_few_tokens_workspace_bytes(T, k, F, Fs=0) -> int:
-    return lib().moe_few_tokens_workspace_bytes(T, k, F, Fs)
+def moe_few_tokens_workspace_bytes(T, H, k, F, Fs=0) -> int:
+    return lib().moe_few_tokens_workspace_bytes(T, H, k, F, Fs)
 
 
 def _few_weights(x, E, F, Fs, ws):
@@ -495,8 +494,8 @@ def _few_weights(x, E, F, Fs, ws):
             raise TypeError("weights are all bf16 or all Int4")
         if tuple(w.shape) != shape and not (shape[0] == 1 and tuple(w.shape) == shape[1:]):
             raise ValueError(f"weights of shape {tuple(w.shape)}, {shape} expected")
-        if int4 and w.group != ws[0].group:
-            raise ValueError("4-bit weights of one layer share a group size")
+        if int4 and (w.group != ws[0].group or w.zeros != ws[0].zeros):
+            raise ValueError("4-bit weights of one layer share a group size, and have zero points or not")
     return int4
 
 
@@ -522,13 +521,12 @@ def moe_few_tokens(x, logits, k, w_gate, w_up, w_down, ws_gate=None, ws_up=None,
     if y is None:
         y = torch.empty((T, H), dtype=torch.bfloat16, device=dev)
     if ws is None:
-        ws = torch.empty(max(1, moe_few_tokens_workspace_bytes(T, k, F, Fs)), dtype=torch.uint8, device=dev)
+        ws = torch.empty(max(1, moe_few_tokens_workspace_bytes(T, H, k, F, Fs)), dtype=torch.uint8, device=dev)
     _dev(x, logits, topk_ids, topk_weights, y, ws)
     if int4:
-        refs = (_Int4Ref * 6)(*[(_ptr(t.codes), _ptr(t.scales), _ptr(t.zeros)) if t is not None else (None, None, None)
-                                for t in w])
+        refs = (_Int4Ref * 6)(*[(_ptr(t.codes), _ptr(t.scales)) if t is not None else (None, None) for t in w])
         _dev(*(t.codes for t in w if t is not None))
-        _check(lib().moe_few_tokens_int4(_ptr(x), _ptr(logits), T, H, E, k, F, Fs, renormalize, w_gate.group, refs,
+        _check(lib().moe_few_tokens_int4(_ptr(x), _ptr(logits), T, H, E, k, F, Fs, renormalize, w_gate.group, w_gate.zeros, refs,
                                          _ptr(topk_ids), _ptr(topk_weights), _ptr(y), _ptr(ws), ws.numel(),
                                          _stream(stream, dev)))
     else:
@@ -837,7 +835,7 @@ class MoELayerFew:
         self._ids = torch.empty((T, k), dtype=torch.int32, device=dev)
         self._weights = torch.empty((T, k), dtype=torch.float32, device=dev)
         self._y = torch.empty((T, H), dtype=torch.bfloat16, device=dev)
-        self.ws = torch.empty(max(1, moe_few_tokens_workspace_bytes(T, k, F, Fs)), dtype=torch.uint8, device=dev)
+        self.ws = torch.empty(max(1, moe_few_tokens_workspace_bytes(T, H, k, F, Fs)), dtype=torch.uint8, device=dev)
         self.topk_ids, self.topk_weights, self.y = self._ids, self._weights, self._y
 
     def run(self, x, logits, w_gate, w_up, w_down, ws_gate=None, ws_up=None, ws_down=None, renormalize=1, stream=None):

@@ -9,14 +9,15 @@
 //
 //   few_up    every workgroup selects all tokens' experts from the logits (16 x E values), lists
 //             the experts that got a token, and computes 16 features of one of them:
-//             h[t, j] = w_tj silu(Wg x_t) (Wu x_t), rounded to bf16.  The gate weight goes in here,
-//             in fp32, before h is rounded: the second kernel is then one plain sum.
+//             h[t, j] = w_tj silu(Wg x_t) (Wu x_t).  The gate weight goes in here: the second
+//             kernel is then one plain sum.
 //   few_down  16 columns of y for all tokens: the sum over all listed experts of Wd h, along one
 //             long k axis (expert after expert, the shared expert last), dealt to the
 //             wavefronts of the workgroup, whose sums are added in LDS in their order.
 //
-// Weights are the A operand of the products and go straight from memory into the registers
-// that the matrix cores read: nothing is shared between wavefronts, so nothing passes through LDS.
+// h goes between the kernels as two bf16 numbers, the rounded value and the rounded rest (16
+// significant bits), so that y carries one rounding to bf16, its own.  Up to eight tokens the rest
+// takes the other eight columns of the same products; more tokens take a second product.
 #include <algorithm>
 
 #include "int4.h"
@@ -26,24 +27,38 @@ namespace moe {
 namespace {
 
 constexpr int kFewT = 16;             // tokens
-constexpr int kFewWaves = 8;          // wavefronts of a workgroup
+constexpr int kUpWaves = 8;           // wavefronts of a workgroup of few_up
 constexpr int kMaxPairs = kFewT * kMaxTopK;
 
 // The experts that got a token, ascending, and which slot of each token is theirs.
 struct Chosen {
-  int n;                              // experts
+  uint64_t mask[kMaxExperts / 64];
   int16_t expert[kMaxPairs];
   int8_t slot[kMaxPairs][kFewT];      // -1: the token did not choose it
   int16_t ids[kFewT][kMaxTopK];
   float w[kFewT][kMaxTopK];
-  int16_t place[kMaxExperts];
 };
+
+// Maximum over the wavefront: inside the rows of 16 lanes by lane permutes, then over the rows.
+template <int CTRL>
+__device__ __forceinline__ uint32_t permuted(uint32_t v) {
+  return uint32_t(__builtin_amdgcn_update_dpp(0, int(v), CTRL, 0xF, 0xF, false));
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  v = max(v, permuted<0xB1>(v));                          // quad_perm [1, 0, 3, 2]
+  v = max(v, permuted<0x4E>(v));                          // quad_perm [2, 3, 0, 1]
+  v = max(v, permuted<0x141>(v));                         // mirrored halves of a row
+  v = max(v, permuted<0x140>(v));                         // mirrored row
+  const uint32_t a = __builtin_amdgcn_readlane(v, 0), b = __builtin_amdgcn_readlane(v, 16);
+  const uint32_t c = __builtin_amdgcn_readlane(v, 32), d = __builtin_amdgcn_readlane(v, 48);
+  return max(max(a, b), max(c, d));
+}
 
 // Top-k of one token by one wavefront, as moe_route selects: larger logit first, equal ones to
 // the lower expert.  Lane l holds experts l V .. l V + V - 1.
 template <int V>
-__device__ __forceinline__ void select(const float* __restrict__ logits, int E, int k, int renorm, int lane,
-                                       int16_t* ids, float* w) {
+__device__ __forceinline__ void select(Chosen& ch, int t, const float* __restrict__ logits, int E, int k, int renorm,
+                                       int lane) {
   float l[V];
   uint32_t key[V];
 #pragma unroll
@@ -55,27 +70,29 @@ __device__ __forceinline__ void select(const float* __restrict__ logits, int E, 
     key[v] = e < E ? max(orderable(l[v]), 1u) : 0u;
   }
   float lmax = 0.f, denom = 0.f, mine = 0.f;
+  int id = 0;
   for (int j = 0; j < k; ++j) {
     uint32_t m = key[0];
 #pragma unroll
     for (int v = 1; v < V; ++v) m = max(m, key[v]);
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) m = max(m, uint32_t(__shfl_xor(int(m), d)));
+    m = wave_max(m);
     int has = V;
 #pragma unroll
     for (int v = V - 1; v >= 0; --v) has = key[v] == m ? v : has;
     const int owner = __builtin_ctzll(__ballot(has < V));
-    const int v0 = __builtin_amdgcn_readlane(has, owner);
+    const int v0 = V == 1 ? 0 : __builtin_amdgcn_readlane(has, owner);
 #pragma unroll
     for (int v = 0; v < V; ++v)
       if (lane == owner && v == v0) key[v] = 0u;
     const float x = from_orderable(m);
     if (j == 0) lmax = x;
-    const float p = expf(x - lmax);
-    denom += p;                                               // slot order
-    if (lane == j) mine = p;
-    if (lane == 0) ids[j] = int16_t(owner * V + v0);
+    if (lane == j) {
+      mine = x;
+      id = owner * V + v0;
+    }
   }
+  mine = expf(mine - lmax);
+  for (int j = 0; j < k; ++j) denom += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(mine), j));  // slot order
   if (!renorm) {
     denom = 0.f;
 #pragma unroll
@@ -84,246 +101,413 @@ __device__ __forceinline__ void select(const float* __restrict__ logits, int E, 
 #pragma unroll
     for (int d = 1; d < kWave; d <<= 1) denom += __shfl_xor(denom, d);
   }
-  if (lane < k) w[lane] = mine / denom;
-}
-
-// ch.ids (and ch.w) are in place: lists the experts.  All threads of the workgroup call it.
-__device__ __forceinline__ void list_experts(Chosen& ch, int T, int E, int k) {
-  const int tid = threadIdx.x, lane = tid & 63;
-  for (int e = tid; e < E; e += int(blockDim.x)) ch.place[e] = 0;
-  __syncthreads();
-  if (tid < T * k) ch.place[ch.ids[tid / k][tid % k]] = 1;
-  __syncthreads();
-  if (tid < kWave) {
-    int n = 0;
-    for (int e0 = 0; e0 < E; e0 += kWave) {
-      const int e = e0 + lane;
-      const bool on = e < E && ch.place[e] != 0;
-      const uint64_t b = __ballot(on);
-      const int a = n + __popcll(b & ((uint64_t(1) << lane) - 1));
-      if (on) {
-        ch.place[e] = int16_t(a);
-        ch.expert[a] = int16_t(e);
-      }
-      n += __popcll(b);
-    }
-    if (lane == 0) ch.n = n;
+  if (lane < k) {
+    ch.ids[t][lane] = int16_t(id);
+    ch.w[t][lane] = mine / denom;
+    atomicOr(reinterpret_cast<unsigned long long*>(&ch.mask[id >> 6]), 1ull << (id & 63));
   }
-  __syncthreads();
-  const int n = ch.n;
-  for (int i = tid; i < n * kFewT; i += int(blockDim.x)) ch.slot[i / kFewT][i % kFewT] = -1;
-  __syncthreads();
-  if (tid < T * k) ch.slot[ch.place[ch.ids[tid / k][tid % k]]][tid / k] = int8_t(tid % k);
-  __syncthreads();
 }
 
-__device__ __forceinline__ bf16x8 load_row8(const uint16_t* p, bool on) {
-  u32x4 v = {0u, 0u, 0u, 0u};
-  if (on) v = *reinterpret_cast<const u32x4*>(p);
-  return __builtin_bit_cast(bf16x8, v);
+// Before and after the experts are in ch.ids and ch.mask, each between barriers of the caller's.
+__device__ __forceinline__ void clear_list(Chosen& ch, int T, int E, int k) {
+  const int tid = threadIdx.x;
+  if (tid < kMaxExperts / 64) ch.mask[tid] = 0;
+  const int most = min(T * k, E);
+  for (int i = tid; i < most; i += int(blockDim.x)) *reinterpret_cast<u32x4*>(ch.slot[i]) = u32x4{~0u, ~0u, ~0u, ~0u};
 }
-
-__device__ __forceinline__ bf16x8 load_weight8(const uint16_t* p) {
-  return __builtin_bit_cast(bf16x8, __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)));
+__device__ __forceinline__ void fill_list(Chosen& ch, int T, int k) {
+  const int tid = threadIdx.x;
+  if (tid < T * k) {
+    const int t = tid / k, j = tid - t * k;
+    const int e = ch.ids[t][j];
+    int a = __popcll(ch.mask[e >> 6] & ((uint64_t(1) << (e & 63)) - 1));
+    for (int i = 0; i < (e >> 6); ++i) a += __popcll(ch.mask[i]);
+    ch.slot[a][t] = int8_t(j);
+    ch.expert[a] = int16_t(e);
+  }
 }
-
-// Weights of one step along k: 64 columns of 16 bf16 rows, or a tile of 128 columns of 4-bit
-// ones.  `mat` is the matrix (expert), `rt` its tile of 16 rows.
-struct Bf16Weights {
-  static constexpr int kCols = 64;
-  static constexpr int kParts = 2;            // products of 32 columns
-  const uint16_t* w;
-  struct Step {
-    bf16x8 a[kParts];
-  };
-  struct Sums {};
-  __device__ __forceinline__ void load(Step& s, int mat, int rt, int64_t rows, int K, int kt, int lane) const {
-    const uint16_t* p = w + (mat * rows + rt * 16 + (lane & 15)) * K + kt * kCols + 8 * (lane >> 4);
+__device__ __forceinline__ int listed(const Chosen& ch) {
+  int n = 0;
 #pragma unroll
-    for (int j = 0; j < kParts; ++j) s.a[j] = load_weight8(p + 32 * j);
-  }
-  static __device__ __forceinline__ void sums(Sums&, const bf16x8 (&)[kParts]) {}
-  static __device__ __forceinline__ void add(f32x4& acc, const Step& s, const bf16x8 (&xb)[kParts], const Sums&) {
-#pragma unroll
-    for (int j = 0; j < kParts; ++j) acc = mfma16(s.a[j], xb[j], acc);
-  }
-};
-
-template <int GPT, bool ZEROS>
-struct Int4Weights {
-  static constexpr int kCols = kInt4Cols;
-  static constexpr int kParts = 4;
-  const uint8_t* codes;
-  const uint16_t* scales;
-  const uint8_t* zeros;
-  using Step = Int4Tile<GPT, ZEROS>;
-  struct Sums {
-    float x[GPT];
-  };
-  __device__ __forceinline__ void load(Step& s, int mat, int rt, int64_t rows, int K, int kt, int lane) const {
-    int4_load(s, codes, scales, zeros, (mat * int4_row_tiles(rows) + rt) * int4_col_tiles(K) + kt, lane);
-  }
-  static __device__ __forceinline__ void sums(Sums& t, const bf16x8 (&xb)[kParts]) { int4_group_sums<GPT>(t.x, xb); }
-  static __device__ __forceinline__ void add(f32x4& acc, const Step& s, const bf16x8 (&xb)[kParts], const Sums& t) {
-    int4_accumulate<GPT, ZEROS>(acc, s, xb, t.x);
-  }
-};
+  for (int i = 0; i < kMaxExperts / 64; ++i) n += __popcll(ch.mask[i]);
+  return __builtin_amdgcn_readfirstlane(n);
+}
 
 // ------------------------------------------------------------------ gate, up and SwiGLU
-// Unit u: 16 features of one listed expert (then of the shared one); KS wavefronts deal its k
-// steps among themselves.  h: routed rows [T, k, F], then the shared expert's [T, Fs].
-template <typename W, int KS, int V>
-__global__ __launch_bounds__(64 * kFewWaves) void few_up_kernel(const uint16_t* __restrict__ x,
-                                                                const float* __restrict__ logits, int T, int H, int E,
-                                                                int k, int F, int Fs, int renorm, W wg, W wu, W sg,
-                                                                W su, int32_t* __restrict__ ids,
-                                                                float* __restrict__ wts, uint16_t* __restrict__ h) {
-  constexpr int kUnits = kFewWaves / KS;
+// Unit u: 16 NU features of one listed expert (then of the shared one); KS wavefronts deal its k
+// steps among themselves, P steps of weights and PX of activations in flight.  C operands hold the
+// tokens' activations.  h: routed rows [T, k][2][F], then the shared expert's [T][2][Fs].
+template <typename W, int NU, int C, int KS, int V, int P, int PX>
+__global__ __launch_bounds__(64 * kUpWaves, 4) void few_up_kernel(const uint16_t* __restrict__ x,
+                                                                  const float* __restrict__ logits, int T, int H,
+                                                                  int E, int k, int F, int Fs, int renorm, W wg, W wu,
+                                                                  W sg, W su, int32_t* __restrict__ ids,
+                                                                  float* __restrict__ wts, uint16_t* __restrict__ h) {
+  constexpr int kUnits = kUpWaves / KS, kAcc = W::kAcc, kSums = NU * 2 * C * kAcc;
   __shared__ Chosen ch;
-  __shared__ f32x4 part[KS > 1 ? kFewWaves : 1][2][64];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  for (int t = wave; t < T; t += kFewWaves) select<V>(logits + int64_t(t) * E, E, k, renorm, lane, ch.ids[t], ch.w[t]);
+  __shared__ f32x4 part[KS > 1 ? kUpWaves : 1][kSums][64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  clear_list(ch, T, E, k);
   __syncthreads();
+  for (int t = wave; t < T; t += kUpWaves) select<V>(ch, t, logits + int64_t(t) * E, E, k, renorm, lane);
+  __syncthreads();
+  fill_list(ch, T, k);
   if (blockIdx.x == 0 && tid < T * k) {
     ids[tid] = ch.ids[tid / k][tid % k];
     wts[tid] = ch.w[tid / k][tid % k];
   }
-  list_experts(ch, T, E, k);
+  __syncthreads();
 
+  const int n = listed(ch);
   const int ks = wave % KS;
   const int u = int(blockIdx.x) * kUnits + wave / KS;
-  const int per = F / 16;                      // units of an expert
+  const int per = F / (16 * NU);               // units of an expert
   const int a = u / per;
-  const bool shared = a >= ch.n;
-  const int rt = shared ? u - ch.n * per : u % per;
-  const bool on = !shared || rt < Fs / 16;
-  const int col = lane & 15, g4 = lane >> 4;
-  const int slot = !on || col >= T ? -1 : shared ? 0 : ch.slot[a][col];
-  f32x4 ag = {0.f, 0.f, 0.f, 0.f}, au = ag;
-  if (on) {
-    const W& g = shared ? sg : wg;
-    const W& up = shared ? su : wu;
-    const int mat = shared ? 0 : ch.expert[a];
-    const int64_t rows = shared ? Fs : F;
-    const int steps = (H + W::kCols - 1) / W::kCols;
-    const uint16_t* xr = x + int64_t(col) * H + 8 * g4;
-    for (int s = ks; s < steps; s += KS) {
-      typename W::Step wsg, wsu;
-      g.load(wsg, mat, rt, rows, H, s, lane);
-      up.load(wsu, mat, rt, rows, H, s, lane);
-      bf16x8 xb[W::kParts];
+  const bool shared = a >= n;
+  const int rt = shared ? u - n * per : u % per;
+  const bool on = !shared || rt < Fs / (16 * NU);
+  f32x4 acc[NU][2][C][kAcc];                   // gate and up
+  f32x4* flat = &acc[0][0][0][0];
 #pragma unroll
-      for (int j = 0; j < W::kParts; ++j) {
-        const int k0 = s * W::kCols + 32 * j;
-        xb[j] = load_row8(xr + k0, slot >= 0 && k0 + 8 * g4 < H);
+  for (int q = 0; q < kSums; ++q) flat[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+  int slot[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int t = c * W::kTok + W::token(lane);
+    slot[c] = !on || t >= T ? -1 : shared ? 0 : ch.slot[a][t];
+  }
+  if (on) {
+    const int mat = shared ? 0 : __builtin_amdgcn_readfirstlane(ch.expert[a]);
+    const int64_t rows = shared ? Fs : F;
+    const auto vg = W::pick(shared, sg, wg).view(mat, rows, H, lane);
+    const auto vu = W::pick(shared, su, wu).view(mat, rows, H, lane);
+    const auto bx = buffer_of(x, int64_t(T) * H * 2);
+    int xat[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+      xat[c] = slot[c] >= 0 ? (c * W::kTok + W::token(lane)) * H * 2 + W::x_at(lane) : kPast;
+    const int steps = (H + W::kCols - 1) / W::kCols;
+    const int mine = (steps - ks + KS - 1) / KS;
+    // units start at different columns: their rows lie at equal distances, and the same column of
+    // all rows in flight would ask the same few memory channels
+    const int turn = u * 5 % steps;
+    auto place = [&](int i) {
+      const int s = ks + i * KS + turn;
+      return s >= steps ? s - steps : s;
+    };
+    typename W::Step wsg[P][NU], wsu[P][NU];
+    u32x4 xb[PX][C][W::kXRegs];
+    auto load_w = [&](int p, int i) {
+      const int s = place(i);
+#pragma unroll
+      for (int r = 0; r < NU; ++r) {
+        W::load(wsg[p][r], vg, rt * NU + r, s, i < mine);
+        W::load(wsu[p][r], vu, rt * NU + r, s, i < mine);
       }
-      typename W::Sums sums;
-      W::sums(sums, xb);
-      W::add(ag, wsg, xb, sums);
-      W::add(au, wsu, xb, sums);
+    };
+    auto load_x = [&](int p, int i) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) W::load_x(xb[p][c], bx, xat[c], place(i), H, i < mine);
+    };
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      if (p < PX) load_x(p, p);
+      load_w(p, p);
+    }
+    for (int i = 0; i < mine; i += P) {
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        typename W::template Sums<C> sums;
+        W::template sums<C>(sums, xb[p % PX], lane);
+#pragma unroll
+        for (int r = 0; r < NU; ++r) {
+          W::template add<C>(acc[r][0], wsg[p][r], xb[p % PX], sums);
+          W::template add<C>(acc[r][1], wsu[p][r], xb[p % PX], sums);
+        }
+        load_x(p % PX, i + p + PX);
+        load_w(p, i + p + P);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
   }
   if (KS > 1) {
-    part[wave][0][lane] = ag;
-    part[wave][1][lane] = au;
+#pragma unroll
+    for (int q = 0; q < kSums; ++q) part[wave][q][lane] = flat[q];
     __syncthreads();
     if (ks != 0) return;
+#pragma unroll 1
+    for (int i = 1; i < KS; ++i)
 #pragma unroll
-    for (int i = 1; i < KS; ++i) {
-      ag += part[wave + i][0][lane];
-      au += part[wave + i][1][lane];
-    }
+      for (int q = 0; q < kSums; ++q) flat[q] += part[wave + i][q][lane];
   }
-  if (slot < 0) return;
-  const float w = shared ? 1.0f : ch.w[col][slot];
-  float v[4];
+  const int width = shared ? Fs : F;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = w * silu(ag[i]) * au[i];
-  uint16_t* out = (shared ? h + (int64_t(T) * k * F + int64_t(col) * Fs) : h + (int64_t(col) * k + slot) * F) +
-                  rt * 16 + 4 * g4;
-  *reinterpret_cast<u32x2*>(out) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+  for (int u2 = 0; u2 < NU * C * kAcc; ++u2) {
+    const int i = u2 % kAcc, c = u2 / kAcc % C, r2 = u2 / kAcc / C;
+    const f32x4 g = W::finish(acc[r2][0][c][i]), up = W::finish(acc[r2][1][c][i]);
+    if (slot[c] < 0 || !W::holds(lane)) continue;
+    const int t = c * W::kTok + W::token(lane);
+    const float w = shared ? 1.0f : ch.w[t][slot[c]];
+    float v[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = w * silu(g[r]) * up[r];
+    uint16_t* out = h + (shared ? int64_t(T) * k * F * 2 + int64_t(t) * 2 * Fs : (int64_t(t) * k + slot[c]) * 2 * F) +
+                    (rt * NU + r2) * 16 + W::row(i, lane);
+    const u32x2 hi = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+    *reinterpret_cast<u32x2*>(out) = hi;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] -= __uint_as_float(r & 1 ? hi[r / 2] & 0xFFFF0000u : hi[r / 2] << 16);
+    *reinterpret_cast<u32x2*>(out + width) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+  }
 }
 
 // ------------------------------------------------------------------ down and sum
-// Workgroup b: columns 16 b .. 16 b + 15 of y.  The k axis is the listed experts' F columns one
-// after the other, then the shared expert's Fs; wavefront w takes steps w, w + 8, ...
-template <typename W>
-__global__ __launch_bounds__(64 * kFewWaves) void few_down_kernel(const uint16_t* __restrict__ h,
-                                                                  const int32_t* __restrict__ ids, int T, int H,
-                                                                  int E, int k, int F, int Fs, W wd, W sd,
-                                                                  uint16_t* __restrict__ y) {
+// A wavefront's place in the long k axis: step s of listed expert a (a = n: the shared expert).
+template <typename W, int C>
+struct Place {
+  int a, s, steps, cols;
+  typename W::View v;
+  int xat[C];
+};
+
+// Workgroup (g, p): columns 16 NT g .. 16 NT g + 16 NT - 1 of y, part p of the k axis, which is the
+// listed experts' F columns one after the other, then the shared expert's Fs.  All wavefronts of the
+// parts deal its steps among themselves in turn.  Rows of h pass through the caches for every
+// step, zeros included; NT tiles of weights share them.  TS operands hold the tokens, once with
+// h's rounded values and once with the rests; FOLD: one operand of 16 columns holds up to eight
+// tokens and their rests.
+//
+// One part writes y; several write their sums to `partial` [parts, T, H], for few_join.
+template <typename W, int NT, int WAVES, int TS, bool FOLD, int P, int PX>
+__global__ __launch_bounds__(64 * WAVES, 4) void few_down_kernel(const uint16_t* __restrict__ h,
+                                                                 const int32_t* __restrict__ ids, int T, int H, int E,
+                                                                 int k, int F, int Fs, int parts, W wd, W sd,
+                                                                 float* __restrict__ partial,
+                                                                 uint16_t* __restrict__ y) {
+  constexpr int C = FOLD ? 1 : 2 * TS, kAcc = W::kAcc, kSums = NT * TS * kAcc;
   __shared__ Chosen ch;
-  __shared__ f32x4 part[kFewWaves][64];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  if (tid < T * k) ch.ids[tid / k][tid % k] = int16_t(ids[tid]);
+  __shared__ f32x4 part[WAVES][kSums][64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  clear_list(ch, T, E, k);
   __syncthreads();
-  list_experts(ch, T, E, k);
-  const int col = lane & 15, g4 = lane >> 4;
-  const int rt = blockIdx.x;
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  auto walk = [&](const W& w, int mat, int cols, int first, const uint16_t* row, bool on) {
-    const int steps = (cols + W::kCols - 1) / W::kCols;
-    for (int s = first; s < steps; s += kFewWaves) {
-      typename W::Step ws;
-      w.load(ws, mat, rt, H, cols, s, lane);
-      bf16x8 xb[W::kParts];
+  if (tid < T * k) {
+    const int e = ids[tid];
+    ch.ids[tid / k][tid % k] = int16_t(e);
+    atomicOr(reinterpret_cast<unsigned long long*>(&ch.mask[e >> 6]), 1ull << (e & 63));
+  }
+  __syncthreads();
+  fill_list(ch, T, k);
+  __syncthreads();
+  const int rg = blockIdx.x / parts, pt = blockIdx.x - rg * parts;
+  const int n = listed(ch);
+  const int fsteps = (F + W::kCols - 1) / W::kCols, ssteps = (Fs + W::kCols - 1) / W::kCols;
+  const int total = n * fsteps + ssteps;
+  const int stride = parts * WAVES, begin = pt * WAVES + wave;
+  const int mine = (total - begin + stride - 1) / stride;
+  const auto bh = buffer_of(h, int64_t(T) * (int64_t(k) * F + Fs) * 4);
+
+  using At = Place<W, C>;
+  auto enter = [&](At& p) {                     // sets what goes with p.a
+    const bool shared = p.a >= n;
+    const int mat = shared ? 0 : __builtin_amdgcn_readfirstlane(ch.expert[p.a]);
+    p.steps = shared ? ssteps : fsteps;
+    p.cols = shared ? Fs : F;
+    p.v = W::pick(shared, sd, wd).view(mat, H, p.cols, lane);
 #pragma unroll
-      for (int j = 0; j < W::kParts; ++j) {
-        const int k0 = s * W::kCols + 32 * j + 8 * g4;
-        xb[j] = load_row8(row + k0, on && k0 < cols);
-      }
-      typename W::Sums sums;
-      W::sums(sums, xb);
-      W::add(acc, ws, xb, sums);
+    for (int c = 0; c < C; ++c) {
+      const int col = W::token(lane);
+      const int t = FOLD ? col & 7 : (c >> 1) * W::kTok + col, rest = FOLD ? col >> 3 : c & 1;
+      const int slot = t >= T ? -1 : shared ? 0 : ch.slot[p.a][t];
+      const int row = shared ? T * k * F * 2 + (2 * t + rest) * Fs : ((t * k + slot) * 2 + rest) * F;
+      p.xat[c] = slot >= 0 ? row * 2 + W::x_at(lane) : kPast;
     }
   };
-  const int steps = (F + W::kCols - 1) / W::kCols;
-  const int n = ch.n;
-  int first = wave;                           // of the wavefront's steps in the expert
-  for (int a = 0; a < n; ++a) {
-    const int slot = col < T ? ch.slot[a][col] : -1;
-    walk(wd, ch.expert[a], F, first, h + (int64_t(col) * k + max(slot, 0)) * F, slot >= 0);
-    first = (first - steps % kFewWaves + kFewWaves) % kFewWaves;
-  }
-  if (Fs) walk(sd, 0, Fs, first, h + (int64_t(T) * k * F + int64_t(col) * Fs), col < T);
-  part[wave][lane] = acc;
-  __syncthreads();
-  if (wave != 0 || col >= T) return;
+  auto carry = [&](At& p) {                     // steps past the end of an expert belong to the next one,
+    while (p.s >= p.steps) {                    // past the last one to the first
+      p.s -= p.steps;
+      p.a = p.a < n ? p.a + 1 : 0;
+      p.steps = p.a < n ? fsteps : ssteps;
+    }
+  };
+  auto advance = [&](At& p) {
+    p.s += stride;
+    if (p.s >= p.steps) {
+      carry(p);
+      enter(p);
+    }
+  };
+  At pw, px;
+  pw.a = 0;
+  pw.s = begin + rg * 5 % total;                // workgroups start at different columns, as in few_up
+  pw.steps = fsteps;                            // T, k >= 1: an expert is listed
+  carry(pw);
+  enter(pw);
+  px = pw;
+
+  f32x4 acc[NT][C][kAcc];
 #pragma unroll
-  for (int w = 1; w < kFewWaves; ++w) acc += part[w][lane];
-  *reinterpret_cast<u32x2*>(y + int64_t(col) * H + rt * 16 + 4 * g4) =
-      u32x2{pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3])};
+  for (int q = 0; q < NT * C * kAcc; ++q) (&acc[0][0][0])[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+  typename W::Step ws[P][NT];
+  u32x4 xb[PX][C][W::kXRegs];
+  auto load_w = [&](int p, int i) {
+#pragma unroll
+    for (int r = 0; r < NT; ++r) W::load(ws[p][r], pw.v, rg * NT + r, pw.s, i < mine);
+    advance(pw);
+  };
+  auto load_x = [&](int p, int i) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) W::load_x(xb[p][c], bh, px.xat[c], px.s, px.cols, i < mine);
+    advance(px);
+  };
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    if (p < PX) load_x(p, p);
+    load_w(p, p);
+  }
+  for (int i = 0; i < mine; i += P) {
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      typename W::template Sums<C> sums;
+      W::template sums<C>(sums, xb[p % PX], lane);
+#pragma unroll
+      for (int r = 0; r < NT; ++r) W::template add<C>(acc[r], ws[p][r], xb[p % PX], sums);
+      load_x(p % PX, i + p + PX);
+      load_w(p, i + p + P);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < kSums; ++q) {
+    const int i = q % kAcc, t = q / kAcc % TS, r = q / kAcc / TS;
+    part[wave][q][lane] = FOLD ? acc[r][t][i] : acc[r][2 * t][i] + acc[r][(2 * t + 1) % C][i];
+  }
+  __syncthreads();
+  for (int q = wave; q < kSums; q += WAVES) {
+    f32x4 s = part[0][q][lane];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) s += part[w][q][lane];
+    s = W::finish(s);
+    if (FOLD) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[i] += __shfl_xor(s[i], 8);
+    }
+    const int t = q / kAcc % TS * W::kTok + W::token(lane);   // FOLD: T <= 8, the rests' columns are past it
+    const int col = (rg * NT + q / kAcc / TS) * 16 + W::row(q % kAcc, lane);
+    if (t >= T || !W::holds(lane)) continue;
+    if (parts == 1)
+      *reinterpret_cast<u32x2*>(y + int64_t(t) * H + col) = u32x2{pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3])};
+    else
+      *reinterpret_cast<f32x4*>(partial + (int64_t(pt) * T + t) * H + col) = s;
+  }
 }
 
-// Units of few_up at most: the experts that T tokens can choose, and the shared one.
-int64_t up_units(int T, int E, int k, int F, int Fs) { return int64_t(std::min(T * k, E)) * (F / 16) + Fs / 16; }
+// y = the parts' sums, in their order.
+__global__ __launch_bounds__(256) void few_join_kernel(const float* __restrict__ partial, int parts, int64_t n4,
+                                                       uint16_t* __restrict__ y) {
+  const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  if (i >= n4) return;
+  const f32x4* p = reinterpret_cast<const f32x4*>(partial) + i;
+  f32x4 s = p[0];
+  for (int q = 1; q < parts; ++q) s += p[q * n4];
+  reinterpret_cast<u32x2*>(y)[i] = u32x2{pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3])};
+}
+
+// Tiles of 16 rows that share a wavefront's activations (of each of gate and up in few_up), and
+// steps in flight: of weights and of activations.
+template <typename W>
+struct Shape;
+template <>
+struct Shape<Bf16Weights> {
+  static constexpr int kUpTiles = 1, kUp = 2, kUpX = 2;
+  static constexpr int kDownTiles = 1, kDownWaves = 8, kDown = 2, kDownX = 2;
+  static constexpr bool kParts = false;
+};
+template <int GPT, bool ZEROS>
+struct Shape<Int4Weights<GPT, ZEROS>> {
+  static constexpr int kUpTiles = 2, kUp = 2, kUpX = 1;
+  static constexpr int kDownTiles = 4, kDownWaves = 8, kDown = 1, kDownX = 1;
+  static constexpr bool kParts = true;
+};
+
+template <typename W, int C, int KS>
+void up_c(const FewShape& s, const W (&w)[6], int64_t units, hipStream_t stream) {
+  using S = Shape<W>;
+  const dim3 grid(unsigned((units * KS + kUpWaves - 1) / kUpWaves)), block(64 * kUpWaves);
+  if (s.E <= 64)
+    MOE_LAUNCH("few_up", (few_up_kernel<W, S::kUpTiles, C, KS, 1, S::kUp, S::kUpX>), grid, block, stream, s.x, s.logits,
+               s.T, s.H, s.E, s.k, s.F, s.Fs, s.renorm, w[0], w[1], w[3], w[4], s.ids, s.wts, s.h);
+  else
+    MOE_LAUNCH("few_up", (few_up_kernel<W, S::kUpTiles, C, KS, 4, S::kUp, S::kUpX>), grid, block, stream, s.x, s.logits,
+               s.T, s.H, s.E, s.k, s.F, s.Fs, s.renorm, w[0], w[1], w[3], w[4], s.ids, s.wts, s.h);
+}
 
 template <typename W, int KS>
-void up_ks(const FewShape& s, W wg, W wu, W sg, W su, hipStream_t stream) {
-  const int64_t units = up_units(s.T, s.E, s.k, s.F, s.Fs);
-  const dim3 grid(unsigned((units * KS + kFewWaves - 1) / kFewWaves)), block(64 * kFewWaves);
-  if (s.E <= 64)
-    MOE_LAUNCH("few_up", (few_up_kernel<W, KS, 1>), grid, block, stream, s.x, s.logits, s.T, s.H, s.E, s.k, s.F, s.Fs,
-               s.renorm, wg, wu, sg, su, s.ids, s.wts, s.h);
-  else
-    MOE_LAUNCH("few_up", (few_up_kernel<W, KS, 4>), grid, block, stream, s.x, s.logits, s.T, s.H, s.E, s.k, s.F, s.Fs,
-               s.renorm, wg, wu, sg, su, s.ids, s.wts, s.h);
+void up_ks(const FewShape& s, const W (&w)[6], int64_t units, hipStream_t stream) {
+  if constexpr (W::kTok < kFewT) {
+    if (s.T > W::kTok) return up_c<W, 2, KS>(s, w, units, stream);
+  }
+  up_c<W, 1, KS>(s, w, units, stream);
+}
+
+template <typename W, int NT, int TS, bool FOLD>
+void down_c(const FewShape& s, const W (&w)[6], hipStream_t stream) {
+  using S = Shape<W>;
+  constexpr int kWaves = S::kDownWaves;
+  static_assert(16 * NT <= kFewMaxCols, "workspace");
+  const int groups = s.H / (16 * NT);
+  // two workgroups a compute unit, where every wavefront then still has two steps
+  const int64_t steps = int64_t(std::min(s.T * s.k, s.E)) * ((s.F + W::kCols - 1) / W::kCols) +
+                        (s.Fs + W::kCols - 1) / W::kCols;
+  const int64_t want = std::min<int64_t>({(kFewParts + groups - 1) / groups, kFewMostParts, steps / (2 * kWaves)});
+  const int parts = S::kParts ? int(std::max<int64_t>(1, want)) : 1;
+  MOE_LAUNCH("few_down", (few_down_kernel<W, NT, kWaves, TS, FOLD, S::kDown, S::kDownX>),
+             dim3(unsigned(groups * parts)), dim3(64 * kWaves), stream, s.h, s.ids, s.T, s.H, s.E, s.k, s.F, s.Fs,
+             parts, w[2], w[5], s.partial, s.y);
+  if (parts == 1) return;
+  const int64_t n4 = int64_t(s.T) * s.H / 4;
+  MOE_LAUNCH("few_join", few_join_kernel, dim3(unsigned((n4 + 255) / 256)), dim3(256), stream, s.partial, parts, n4,
+             s.y);
 }
 
 template <typename W>
 hipError_t launch(const FewShape& s, const W (&w)[6], hipStream_t stream) {
-  up_ks<W, 8>(s, w[0], w[1], w[3], w[4], stream);
+  // units of few_up at most: the experts that T tokens can choose, and the shared one
+  constexpr int kRows = 16 * Shape<W>::kUpTiles;
+  const int64_t units = int64_t(std::min(s.T * s.k, s.E)) * (s.F / kRows) + s.Fs / kRows;
+  if constexpr (W::kTok < kFewT) {
+    up_ks<W, 8>(s, w, units, stream);
+  } else {
+    const int64_t want = 12 * int64_t(s.num_cu);
+    if (units >= want)
+      up_ks<W, 1>(s, w, units, stream);
+    else if (2 * units >= want)
+      up_ks<W, 2>(s, w, units, stream);
+    else if (4 * units >= want)
+      up_ks<W, 4>(s, w, units, stream);
+    else
+      up_ks<W, 8>(s, w, units, stream);
+  }
   hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
-  MOE_LAUNCH("few_down", (few_down_kernel<W>), dim3(unsigned(s.H / 16)), dim3(64 * kFewWaves), stream, s.h, s.ids,
-             s.T, s.H, s.E, s.k, s.F, s.Fs, w[2], w[5], s.y);
+  constexpr bool kFold = W::kTok == kFewT;
+  constexpr int kTiles = Shape<W>::kDownTiles;
+  // bf16: two tiles share the rows of h where that still leaves three quarters of the compute units a
+  // workgroup (DeepSeek shape, 8 tokens, H 7168: 216 us with one tile, 193 with two; Mixtral shape,
+  // 1 token, H 4096: 38 and 61)
+  const bool wide = W::kTok < kFewT && s.H / 32 >= s.num_cu * 3 / 4;
+  if (s.T > 8)
+    down_c<W, kTiles, kFewT / W::kTok, false>(s, w, stream);
+  else if (wide)
+    down_c<W, 2, 1, kFold>(s, w, stream);
+  else
+    down_c<W, kTiles, 1, kFold>(s, w, stream);
   return hipGetLastError();
 }
 
 template <int GPT, bool ZEROS>
 hipError_t launch_int4(const FewShape& s, const Int4Ref (&w)[6], hipStream_t stream) {
   Int4Weights<GPT, ZEROS> v[6];
-  for (int i = 0; i < 6; ++i) v[i] = {w[i].codes, w[i].scales, w[i].zeros};
+  for (int i = 0; i < 6; ++i) v[i] = {w[i].codes, w[i].scales};
   return launch(s, v, stream);
 }
 
@@ -335,11 +519,10 @@ hipError_t launch_few_bf16(const FewShape& s, const uint16_t* const (&w)[6], hip
   return launch(s, v, stream);
 }
 
-hipError_t launch_few_int4(const FewShape& s, const Int4Ref (&w)[6], int group, hipStream_t stream) {
-  const bool z = w[0].zeros != nullptr;
-  if (group == 32) return z ? launch_int4<4, true>(s, w, stream) : launch_int4<4, false>(s, w, stream);
-  if (group == 64) return z ? launch_int4<2, true>(s, w, stream) : launch_int4<2, false>(s, w, stream);
-  return z ? launch_int4<1, true>(s, w, stream) : launch_int4<1, false>(s, w, stream);
+hipError_t launch_few_int4(const FewShape& s, const Int4Ref (&w)[6], int group, bool zeros, hipStream_t stream) {
+  if (group == 32) return zeros ? launch_int4<4, true>(s, w, stream) : launch_int4<4, false>(s, w, stream);
+  if (group == 64) return zeros ? launch_int4<2, true>(s, w, stream) : launch_int4<2, false>(s, w, stream);
+  return zeros ? launch_int4<1, true>(s, w, stream) : launch_int4<1, false>(s, w, stream);
 }
 
 }  // namespace moe

@@ -53,8 +53,7 @@ __global__ __launch_bounds__(64) void pack_int4_kernel(const uint8_t* __restrict
                                                        const uint16_t* __restrict__ scales,
                                                        const uint8_t* __restrict__ zeros, int64_t rows, int K, int g,
                                                        uint8_t* __restrict__ out_codes,
-                                                       uint16_t* __restrict__ out_scales,
-                                                       uint8_t* __restrict__ out_zeros) {
+                                                       uint8_t* __restrict__ out_scales) {
   const int lane = threadIdx.x;
   const int64_t tile = blockIdx.x;
   const int64_t ct = int4_col_tiles(K), rt = int4_row_tiles(rows);
@@ -77,97 +76,114 @@ __global__ __launch_bounds__(64) void pack_int4_kernel(const uint8_t* __restrict
   reinterpret_cast<u32x4*>(out_codes + tile * kInt4TileBytes)[lane] = v;
   const int gpt = kInt4Cols / g;
   for (int i = lane; i < gpt * kInt4Rows; i += 64) {
-    const int64_t r = row0 + i % kInt4Rows;
-    const int grp = kt * gpt + i / kInt4Rows;
+    const int64_t r = row0 + i / (4 * gpt) * 4 + i % 4;
+    const int grp = kt * gpt + i / 4 % gpt;
     const bool in = r < rows && grp < K / g;
     const int64_t at = (mat * rows + r) * (K / g) + grp;
-    out_scales[tile * gpt * kInt4Rows + i] = in ? scales[at] : uint16_t(0);
-    if (out_zeros) out_zeros[tile * gpt * kInt4Rows + i] = in ? zeros[at] : uint8_t(8);
+    const uint16_t sc = in ? scales[at] : uint16_t(0);
+    const int64_t to = tile * gpt * kInt4Rows + i;
+    if (zeros)
+      reinterpret_cast<uint32_t*>(out_scales)[to] = uint32_t(sc) << 16 | 0x4300u | (in ? zeros[at] & 15u : 8u);
+    else
+      reinterpret_cast<uint16_t*>(out_scales)[to] = sc;
   }
 }
 
 // ------------------------------------------------------------------ matrix times a few rows
-// y[t][n] = sum_k W[n][k] x[t][k].  A wavefront multiplies one tile of 16 weight rows with up
-// to 16 C rows of x on the matrix cores: the weights are the A operand, expanded in registers,
-// x the B operand, read from the caches.  The workgroup's wavefronts deal the tiles along k
-// among themselves and add their sums in LDS, in the order of the wavefronts.
-constexpr int kMvWaves = 8;
-
-template <int C, int GPT, bool ZEROS>
-__global__ __launch_bounds__(64 * kMvWaves) void matvec_int4_kernel(const uint16_t* __restrict__ x,
-                                                                    const uint8_t* __restrict__ codes,
-                                                                    const uint16_t* __restrict__ scales,
-                                                                    const uint8_t* __restrict__ zeros, int T, int N,
-                                                                    int K, uint16_t* __restrict__ y) {
-  __shared__ f32x4 part[kMvWaves][C][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// y[t][n] = sum_k W[n][k] x[t][k].  A wavefront multiplies NT tiles of 16 weight rows with up to
+// 16 C rows of x on the matrix cores: the weights are the A operand, expanded in registers, x the B
+// operand, read from the caches.  KS wavefronts deal the tiles along k among themselves and add
+// their sums in LDS, in their order; P steps of weights are in flight.
+template <int NT, int C, int KS, int GPT, bool ZEROS, int P>
+__global__ __launch_bounds__(64 * KS, 4) void matvec_int4_kernel(const uint16_t* __restrict__ x,
+                                                                 Int4Weights<GPT, ZEROS, kCached> w, int T, int N, int K,
+                                                                 uint16_t* __restrict__ y) {
+  using W = Int4Weights<GPT, ZEROS, kCached>;
+  __shared__ f32x4 part[KS][NT * C][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g4 = lane >> 4, col = lane & 15;
   const int t0 = int(blockIdx.y) * 16 * C;
-  const int ct = int4_col_tiles(K);
-  f32x4 acc[C];
+  const int steps = int4_col_tiles(K);
+  const int mine = (steps - wave + KS - 1) / KS;
+  const auto v = w.view(0, N, K, lane);
+  const int tiles = int(int4_row_tiles(N)), rt = int(blockIdx.x) * NT;
+  const auto bx = buffer_of(x + int64_t(t0) * K, int64_t(min(T - t0, 16 * C)) * K * 2);
+  int xat[C];
 #pragma unroll
-  for (int c = 0; c < C; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int kt = wave; kt < ct; kt += kMvWaves) {
-    Int4Tile<GPT, ZEROS> w;
-    int4_load(w, codes, scales, zeros, int64_t(blockIdx.x) * ct + kt, lane);
+  for (int c = 0; c < C; ++c) xat[c] = (16 * c + W::token(lane)) * K * 2 + W::x_at(lane);   // past the last row: zeros
+  f32x4 acc[NT][C][1];
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      bf16x8 xb[4];
-      const int t = t0 + 16 * c + col;
+  for (int r = 0; r < NT; ++r)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int k = kt * kInt4Cols + 32 * j + 8 * g4;
-        u32x4 v = {0u, 0u, 0u, 0u};
-        if (t < T && k < K) v = *reinterpret_cast<const u32x4*>(x + int64_t(t) * K + k);
-        xb[j] = __builtin_bit_cast(bf16x8, v);
-      }
-      float xs[GPT];
-      int4_group_sums<GPT>(xs, xb);
-      int4_accumulate<GPT, ZEROS>(acc[c], w, xb, xs);
+    for (int c = 0; c < C; ++c) acc[r][c][0] = f32x4{0.f, 0.f, 0.f, 0.f};
+  typename W::Step ws[P][NT];
+  u32x4 xb[C][W::kXRegs];
+  auto load_w = [&](int p, int i) {
+#pragma unroll
+    for (int r = 0; r < NT; ++r) W::load(ws[p][r], v, rt + r, wave + i * KS, i < mine && rt + r < tiles);
+  };
+  auto load_x = [&](int i) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) W::load_x(xb[c], bx, xat[c], wave + i * KS, K, i < mine);
+  };
+#pragma unroll
+  for (int p = 0; p < P; ++p) load_w(p, p);
+  load_x(0);
+  for (int i = 0; i < mine; i += P) {
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      typename W::template Sums<C> sums;
+      W::template sums<C>(sums, xb, lane);
+#pragma unroll
+      for (int r = 0; r < NT; ++r) W::template add<C>(acc[r], ws[p][r], xb, sums);
+      load_x(i + p + 1);
+      load_w(p, i + p + P);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
 #pragma unroll
-  for (int c = 0; c < C; ++c) part[wave][c][lane] = acc[c];
-  __syncthreads();
-  for (int c = wave; c < C; c += kMvWaves) {
-    f32x4 s = part[0][c][lane];
+  for (int r = 0; r < NT; ++r)
 #pragma unroll
-    for (int w = 1; w < kMvWaves; ++w) s += part[w][c][lane];
-    const int t = t0 + 16 * c + col;
-    const int n = int(blockIdx.x) * kInt4Rows + 4 * g4;
+    for (int c = 0; c < C; ++c) part[wave][r * C + c][lane] = acc[r][c][0];
+  __syncthreads();
+  for (int q = wave; q < NT * C; q += KS) {
+    f32x4 s = part[0][q][lane];
+#pragma unroll
+    for (int i = 1; i < KS; ++i) s += part[i][q][lane];
+    const int t = t0 + 16 * (q % C) + col;
+    const int n = (int(blockIdx.x) * NT + q / C) * kInt4Rows + 4 * g4;
     if (t < T) {
       uint16_t* out = y + int64_t(t) * N + n;
       const uint32_t a = pack_bf16x2(s[0], s[1]), b = pack_bf16x2(s[2], s[3]);
       if (n + 4 <= N && (N & 3) == 0) {
         *reinterpret_cast<u32x2*>(out) = u32x2{a, b};
       } else {
-        const uint16_t v[4] = {uint16_t(a), uint16_t(a >> 16), uint16_t(b), uint16_t(b >> 16)};
+        const uint16_t e[4] = {uint16_t(a), uint16_t(a >> 16), uint16_t(b), uint16_t(b >> 16)};
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (n + i < N) out[i] = v[i];
+          if (n + i < N) out[i] = e[i];
       }
     }
   }
 }
 
-template <int C, int GPT>
-hipError_t launch_mv(const uint16_t* x, const uint8_t* codes, const uint16_t* scales, const uint8_t* zeros, int T,
-                     int N, int K, uint16_t* y, hipStream_t s) {
-  const dim3 grid(unsigned(int4_row_tiles(N)), unsigned((T + 16 * C - 1) / (16 * C)));
-  const dim3 block(64 * kMvWaves);
-  if (zeros)
-    MOE_LAUNCH("matvec_int4", (matvec_int4_kernel<C, GPT, true>), grid, block, s, x, codes, scales, zeros, T, N, K, y);
-  else
-    MOE_LAUNCH("matvec_int4", (matvec_int4_kernel<C, GPT, false>), grid, block, s, x, codes, scales, zeros, T, N, K, y);
-  return hipGetLastError();
+template <int NT, int C, int KS, int GPT, bool ZEROS, int P>
+void mv(const uint16_t* x, const Int4Ref& w, int T, int N, int K, uint16_t* y, hipStream_t s) {
+  const dim3 grid(unsigned((int4_row_tiles(N) + NT - 1) / NT), unsigned((T + 16 * C - 1) / (16 * C)));
+  const Int4Weights<GPT, ZEROS, kCached> v = {w.codes, w.scales};
+  MOE_LAUNCH("matvec_int4", (matvec_int4_kernel<NT, C, KS, GPT, ZEROS, P>), grid, dim3(64 * KS), s, x, v, T, N, K, y);
 }
 
-template <int C>
-hipError_t launch_mv_g(const uint16_t* x, const uint8_t* codes, const uint16_t* scales, const uint8_t* zeros, int T,
-                       int N, int K, int group, uint16_t* y, hipStream_t s) {
-  if (group == 32) return launch_mv<C, 4>(x, codes, scales, zeros, T, N, K, y, s);
-  if (group == 64) return launch_mv<C, 2>(x, codes, scales, zeros, T, N, K, y, s);
-  return launch_mv<C, 1>(x, codes, scales, zeros, T, N, K, y, s);
+template <int GPT, bool ZEROS>
+hipError_t mv_group(const uint16_t* x, const Int4Ref& w, int T, int N, int K, uint16_t* y, int num_cu, hipStream_t s) {
+  const bool wide = int4_row_tiles(N) >= 4 * int64_t(num_cu);
+  if (T <= 16)
+    wide ? mv<4, 1, 8, GPT, ZEROS, 1>(x, w, T, N, K, y, s) : mv<1, 1, 8, GPT, ZEROS, 4>(x, w, T, N, K, y, s);
+  else if (T <= 32)
+    mv<1, 2, 8, GPT, ZEROS, 2>(x, w, T, N, K, y, s);
+  else
+    mv<1, 4, 8, GPT, ZEROS, 1>(x, w, T, N, K, y, s);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -185,20 +201,20 @@ hipError_t launch_quantize_int4(const uint16_t* src, int64_t groups, int group, 
 }
 
 hipError_t launch_pack_int4(const uint8_t* codes, const uint16_t* scales, const uint8_t* zeros, int64_t matrices,
-                            int64_t rows, int K, int group, uint8_t* out_codes, uint16_t* out_scales,
-                            uint8_t* out_zeros, hipStream_t s) {
+                            int64_t rows, int K, int group, uint8_t* out_codes, uint8_t* out_scales, hipStream_t s) {
   const dim3 grid(unsigned(matrices * int4_row_tiles(rows) * int4_col_tiles(K)));
   MOE_LAUNCH("pack_int4", pack_int4_kernel, grid, dim3(64), s, codes, scales, zeros, rows, K, group, out_codes,
-             out_scales, out_zeros);
+             out_scales);
   return hipGetLastError();
 }
 
-hipError_t launch_matvec_int4(const uint16_t* x, const Int4Ref& w, int T, int N, int K, int group, uint16_t* y,
-                              int num_cu, hipStream_t s) {
-  (void)num_cu;
-  if (T <= 16) return launch_mv_g<1>(x, w.codes, w.scales, w.zeros, T, N, K, group, y, s);
-  if (T <= 32) return launch_mv_g<2>(x, w.codes, w.scales, w.zeros, T, N, K, group, y, s);
-  return launch_mv_g<4>(x, w.codes, w.scales, w.zeros, T, N, K, group, y, s);
+hipError_t launch_matvec_int4(const uint16_t* x, const Int4Ref& w, int T, int N, int K, int group, bool zeros,
+                              uint16_t* y, int num_cu, hipStream_t s) {
+  if (group == 32)
+    return zeros ? mv_group<4, true>(x, w, T, N, K, y, num_cu, s) : mv_group<4, false>(x, w, T, N, K, y, num_cu, s);
+  if (group == 64)
+    return zeros ? mv_group<2, true>(x, w, T, N, K, y, num_cu, s) : mv_group<2, false>(x, w, T, N, K, y, num_cu, s);
+  return zeros ? mv_group<1, true>(x, w, T, N, K, y, num_cu, s) : mv_group<1, false>(x, w, T, N, K, y, num_cu, s);
 }
 
 }  // namespace moe

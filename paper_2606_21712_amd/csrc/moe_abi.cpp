@@ -288,7 +288,9 @@ moe_status moe_combine(const void* y_perm, const int32_t* dest_rows, const float
 
 // ------------------------------------------------------------------ 4-bit weights
 size_t moe_int4_code_bytes(int64_t rows, int32_t K) { return moe::int4_code_bytes(rows, K); }
-size_t moe_int4_groups(int64_t rows, int32_t K, int32_t group) { return moe::int4_groups(rows, K, group); }
+size_t moe_int4_scale_bytes(int64_t rows, int32_t K, int32_t group, int32_t zeros) {
+  return moe::int4_scale_bytes(rows, K, group, zeros);
+}
 
 moe_status moe_quantize_int4(const void* src, int64_t rows, int32_t K, int32_t group, uint8_t* codes,
                              uint16_t* scales, uint8_t* zeros, moe_stream stream) {
@@ -300,16 +302,15 @@ moe_status moe_quantize_int4(const void* src, int64_t rows, int32_t K, int32_t g
 }
 
 moe_status moe_pack_int4(const uint8_t* codes, const uint16_t* scales, const uint8_t* zeros, int64_t matrices,
-                         int64_t rows, int32_t K, int32_t group, uint8_t* out_codes, uint16_t* out_scales,
-                         uint8_t* out_zeros, moe_stream stream) {
-  moe::Check c = moe::validate_pack_int4(codes, scales, zeros, matrices, rows, K, group, out_codes, out_scales,
-                                         out_zeros);
+                         int64_t rows, int32_t K, int32_t group, uint8_t* out_codes, uint8_t* out_scales,
+                         moe_stream stream) {
+  moe::Check c = moe::validate_pack_int4(codes, scales, zeros, matrices, rows, K, group, out_codes, out_scales);
   if (!c.ok() || matrices == 0 || rows == 0) return finish(c);
   return hip_status("moe_pack_int4", moe::launch_pack_int4(codes, scales, zeros, matrices, rows, K, group, out_codes,
-                                                           out_scales, out_zeros, stream_of(stream)));
+                                                           out_scales, stream_of(stream)));
 }
 
-moe_status moe_matvec_int4(const void* x, const uint8_t* codes, const uint16_t* scales, const uint8_t* zeros, int64_t T,
+moe_status moe_matvec_int4(const void* x, const uint8_t* codes, const uint8_t* scales, int32_t zeros, int64_t T,
                            int32_t N, int32_t K, int32_t group, void* y, moe_stream stream) {
   moe::Check c = moe::validate_matvec_int4(x, codes, scales, zeros, T, N, K, group, y);
   if (!c.ok() || T == 0) return finish(c);
@@ -317,14 +318,26 @@ moe_status moe_matvec_int4(const void* x, const uint8_t* codes, const uint16_t* 
   const int ncu = cu_count(&err);
   if (err != hipSuccess) return hip_status("moe_matvec_int4", err);
   return hip_status("moe_matvec_int4",
-                    moe::launch_matvec_int4(static_cast<const uint16_t*>(x), moe::Int4Ref{codes, scales, zeros}, int(T),
-                                            N, K, group, static_cast<uint16_t*>(y), ncu, stream_of(stream)));
+                    moe::launch_matvec_int4(static_cast<const uint16_t*>(x), moe::Int4Ref{codes, scales}, int(T),
+                                            N, K, group, zeros != 0, static_cast<uint16_t*>(y), ncu, stream_of(stream)));
 }
 
 // ------------------------------------------------------------------ the layer for few tokens
-size_t moe_few_tokens_workspace_bytes(int64_t T, int32_t k, int32_t F, int32_t Fs) {
-  return moe::few_workspace_bytes(T, k, F, Fs);
+size_t moe_few_tokens_workspace_bytes(int64_t T, int32_t H, int32_t k, int32_t F, int32_t Fs) {
+  return moe::few_workspace_bytes(T, H, k, F, Fs);
 }
+
+namespace {
+
+moe::FewShape few_shape(const void* x, const float* logits, int64_t T, int32_t H, int32_t E, int32_t k, int32_t F,
+                        int32_t Fs, int32_t renormalize, int32_t* ids, float* wts, void* ws, void* y, int ncu) {
+  auto* base = static_cast<uint8_t*>(ws);
+  return {static_cast<const uint16_t*>(x), logits, int(T), H, E, k, F, Fs, renormalize, ids, wts,
+          reinterpret_cast<uint16_t*>(base), reinterpret_cast<float*>(base + moe::few_partial_offset(T, k, F, Fs)),
+          static_cast<uint16_t*>(y), ncu};
+}
+
+}  // namespace
 
 moe_status moe_few_tokens(const void* x, const float* logits, int64_t T, int32_t H, int32_t E, int32_t k, int32_t F,
                           int32_t Fs, int32_t renormalize, const void* w_gate, const void* w_up, const void* w_down,
@@ -337,28 +350,27 @@ moe_status moe_few_tokens(const void* x, const float* logits, int64_t T, int32_t
   hipError_t err;
   const int ncu = cu_count(&err);
   if (err != hipSuccess) return hip_status("moe_few_tokens", err);
-  const moe::FewShape s = {static_cast<const uint16_t*>(x), logits, int(T), H, E, k, F, Fs, renormalize, topk_ids,
-                           topk_weights, static_cast<uint16_t*>(ws), static_cast<uint16_t*>(y), ncu};
+  const moe::FewShape s = few_shape(x, logits, T, H, E, k, F, Fs, renormalize, topk_ids, topk_weights, ws, y, ncu);
   const uint16_t* p[6];
   for (int i = 0; i < 6; ++i) p[i] = static_cast<const uint16_t*>(w[i]);
   return hip_status("moe_few_tokens", moe::launch_few_bf16(s, p, stream_of(stream)));
 }
 
 moe_status moe_few_tokens_int4(const void* x, const float* logits, int64_t T, int32_t H, int32_t E, int32_t k,
-                               int32_t F, int32_t Fs, int32_t renormalize, int32_t group, const moe_int4* weights,
+                               int32_t F, int32_t Fs, int32_t renormalize, int32_t group, int32_t zeros,
+                               const moe_int4* weights,
                                int32_t* topk_ids, float* topk_weights, void* y, void* ws, size_t ws_bytes,
                                moe_stream stream) {
-  moe::Check c = moe::validate_few_int4(x, logits, T, H, E, k, F, Fs, renormalize, group, weights, topk_ids,
+  moe::Check c = moe::validate_few_int4(x, logits, T, H, E, k, F, Fs, renormalize, group, zeros, weights, topk_ids,
                                         topk_weights, y, ws, ws_bytes);
   if (!c.ok() || T == 0) return finish(c);
   hipError_t err;
   const int ncu = cu_count(&err);
   if (err != hipSuccess) return hip_status("moe_few_tokens_int4", err);
-  const moe::FewShape s = {static_cast<const uint16_t*>(x), logits, int(T), H, E, k, F, Fs, renormalize, topk_ids,
-                           topk_weights, static_cast<uint16_t*>(ws), static_cast<uint16_t*>(y), ncu};
+  const moe::FewShape s = few_shape(x, logits, T, H, E, k, F, Fs, renormalize, topk_ids, topk_weights, ws, y, ncu);
   moe::Int4Ref p[6] = {};
-  for (int i = 0; i < (Fs ? 6 : 3); ++i) p[i] = {weights[i].codes, weights[i].scales, weights[i].zeros};
-  return hip_status("moe_few_tokens_int4", moe::launch_few_int4(s, p, group, stream_of(stream)));
+  for (int i = 0; i < (Fs ? 6 : 3); ++i) p[i] = {weights[i].codes, weights[i].scales};
+  return hip_status("moe_few_tokens_int4", moe::launch_few_int4(s, p, group, zeros != 0, stream_of(stream)));
 }
 
 // ------------------------------------------------------------------ the paged 8-bit cache

@@ -97,19 +97,17 @@ hipError_t launch_combine(const void* y_perm, const int32_t* dest, const float* 
 // 4-bit matrices (layout in int4.h): standard row-major codes to and from.
 struct Int4Ref {
   const uint8_t* codes;
-  const uint16_t* scales;
-  const uint8_t* zeros;   // null: 8 everywhere
+  const uint8_t* scales;
 };
 hipError_t launch_quantize_int4(const uint16_t* src, int64_t groups, int group, uint8_t* codes, uint16_t* scales,
                                 uint8_t* zeros, hipStream_t s);
 hipError_t launch_pack_int4(const uint8_t* codes, const uint16_t* scales, const uint8_t* zeros, int64_t matrices,
-                            int64_t rows, int K, int group, uint8_t* out_codes, uint16_t* out_scales,
-                            uint8_t* out_zeros, hipStream_t s);
-hipError_t launch_matvec_int4(const uint16_t* x, const Int4Ref& w, int T, int N, int K, int group, uint16_t* y,
-                              int num_cu, hipStream_t s);
+                            int64_t rows, int K, int group, uint8_t* out_codes, uint8_t* out_scales, hipStream_t s);
+hipError_t launch_matvec_int4(const uint16_t* x, const Int4Ref& w, int T, int N, int K, int group, bool zeros,
+                              uint16_t* y, int num_cu, hipStream_t s);
 
 // The layer for at most 16 tokens.  Weights in the order gate, up, down, then the shared expert's
-// (null without one).  h: scratch, bf16 [T, k, F] then [T, Fs].
+// (null without one).  h: scratch, bf16 [T, k, 2, F] then [T, 2, Fs].
 struct FewShape {
   const uint16_t* x;
   const float* logits;
@@ -117,11 +115,12 @@ struct FewShape {
   int32_t* ids;
   float* wts;
   uint16_t* h;
+  float* partial;      // parts of the down projection (tiling.h)
   uint16_t* y;
   int num_cu;
 };
 hipError_t launch_few_bf16(const FewShape& s, const uint16_t* const (&w)[6], hipStream_t stream);
-hipError_t launch_few_int4(const FewShape& s, const Int4Ref (&w)[6], int group, hipStream_t stream);
+hipError_t launch_few_int4(const FewShape& s, const Int4Ref (&w)[6], int group, bool zeros, hipStream_t stream);
 
 // The paged 8-bit key-value cache (layout in kv8.h) and a batch of sequences over it.
 struct Kv8Cache {

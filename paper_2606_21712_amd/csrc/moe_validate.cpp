@@ -380,7 +380,7 @@ Check validate_combine(const void* y_perm, const int32_t* dest, const float* w, 
 // ------------------------------------------------------------------ 4-bit weights
 namespace {
 
-constexpr int64_t kInt4MaxDim = int64_t(1) << 24;
+constexpr int64_t kInt4MaxDim = int64_t(1) << 23;
 
 bool int4_group_ok(int32_t group) { return group == 32 || group == 64 || group == 128; }
 
@@ -390,6 +390,11 @@ Check int4_dims(const char* fn, int32_t K, int32_t group) {
   if (K < 1 || K % group != 0)
     return fail(MOE_ERR_INVALID_ARGUMENT, fn, "K=%lld must be a positive multiple of group=%lld", K, group);
   if (K > kInt4MaxDim) return fail(MOE_ERR_UNSUPPORTED, fn, "K=%lld exceeds %lld", K, kInt4MaxDim);
+  return Check{};
+}
+
+Check zeros_flag(const char* fn, int32_t zeros) {
+  if (zeros != 0 && zeros != 1) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "zeros=%lld must be 0 or 1", zeros);
   return Check{};
 }
 
@@ -403,9 +408,9 @@ size_t int4_code_bytes(int64_t rows, int32_t K) {
   return up16(rows) * (up128(K) / 2);
 }
 
-size_t int4_groups(int64_t rows, int32_t K, int32_t group) {
-  if (rows <= 0 || K <= 0 || !int4_group_ok(group) || rows > INT64_MAX / (int64_t(1) << 32)) return 0;
-  return up16(rows) * (up128(K) / size_t(group));
+size_t int4_scale_bytes(int64_t rows, int32_t K, int32_t group, int zeros) {
+  if (rows <= 0 || K <= 0 || !int4_group_ok(group) || rows > INT64_MAX / (int64_t(1) << 34)) return 0;
+  return up16(rows) * (up128(K) / size_t(group)) * (zeros ? 4 : 2);
 }
 
 Check validate_quantize_int4(const void* src, int64_t rows, int32_t K, int32_t group, const void* codes,
@@ -425,14 +430,11 @@ Check validate_quantize_int4(const void* src, int64_t rows, int32_t K, int32_t g
 }
 
 Check validate_pack_int4(const void* codes, const void* scales, const void* zeros, int64_t matrices, int64_t rows,
-                         int32_t K, int32_t group, const void* out_codes, const void* out_scales,
-                         const void* out_zeros) {
+                         int32_t K, int32_t group, const void* out_codes, const void* out_scales) {
   const char* fn = "moe_pack_int4";
   MOE_TRY(int4_dims(fn, K, group));
   if (matrices < 0) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "matrices=%lld is negative", matrices);
   if (rows < 0) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "rows=%lld is negative", rows);
-  if ((zeros == nullptr) != (out_zeros == nullptr))
-    return fail(MOE_ERR_INVALID_ARGUMENT, fn, "zeros and out_zeros go together");
   if (matrices == 0 || rows == 0) return Check{};
   // one workgroup of 64 threads a tile, fewer than 2^32 threads
   const int64_t most = int64_t(1) << 26;
@@ -444,34 +446,39 @@ Check validate_pack_int4(const void* codes, const void* scales, const void* zero
   MOE_TRY(ptr(fn, "scales", scales));
   MOE_TRY(ptr(fn, "out_codes", out_codes));
   MOE_TRY(ptr(fn, "out_scales", out_scales));
-  if (zeros != nullptr) {
-    MOE_TRY(ptr(fn, "zeros", zeros));
-    MOE_TRY(ptr(fn, "out_zeros", out_zeros));
-  }
+  if (zeros != nullptr) MOE_TRY(ptr(fn, "zeros", zeros));
   return Check{};
 }
 
-Check validate_matvec_int4(const void* x, const void* codes, const void* scales, const void* zeros, int64_t T,
-                           int32_t N, int32_t K, int32_t group, const void* y) {
+Check validate_matvec_int4(const void* x, const void* codes, const void* scales, int32_t zeros, int64_t T, int32_t N,
+                           int32_t K, int32_t group, const void* y) {
   const char* fn = "moe_matvec_int4";
   MOE_TRY(int4_dims(fn, K, group));
+  MOE_TRY(zeros_flag(fn, zeros));
   if (T < 0) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "T=%lld is negative", T);
   if (N < 1) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "N=%lld must be >= 1", N);
   if (T > (1 << 20)) return fail(MOE_ERR_UNSUPPORTED, fn, "T=%lld exceeds %lld", T, 1 << 20);
-  if (N > kInt4MaxDim) return fail(MOE_ERR_UNSUPPORTED, fn, "N=%lld exceeds %lld", N, kInt4MaxDim);
+  // the kernel addresses codes, scales and 64 rows of x with 32-bit byte offsets
+  if (int4_code_bytes(N, K) >= (size_t(1) << 31) || int4_scale_bytes(N, K, group, zeros) >= (size_t(1) << 31))
+    return fail(MOE_ERR_UNSUPPORTED, fn, "N=%lld x K=%lld matrix reaches 2 GiB", N, K);
   if (T == 0) return Check{};
   MOE_TRY(ptr(fn, "x", x));
   MOE_TRY(ptr(fn, "codes", codes));
   MOE_TRY(ptr(fn, "scales", scales));
-  if (zeros != nullptr) MOE_TRY(ptr(fn, "zeros", zeros));
   MOE_TRY(ptr(fn, "y", y));
   return Check{};
 }
 
 // ------------------------------------------------------------------ the layer for few tokens
-size_t few_workspace_bytes(int64_t T, int32_t k, int32_t F, int32_t Fs) {
-  if (T <= 0 || T > MOE_FEW_TOKENS || k < 1 || k > MOE_MAX_TOPK || F < 1 || Fs < 0) return 0;
-  return align256(size_t(T) * (size_t(k) * size_t(F) + size_t(Fs)) * 2);
+size_t few_partial_offset(int64_t T, int32_t k, int32_t F, int32_t Fs) {
+  return align256(size_t(T) * (size_t(k) * size_t(F) + size_t(Fs)) * 4);
+}
+
+size_t few_workspace_bytes(int64_t T, int32_t H, int32_t k, int32_t F, int32_t Fs) {
+  if (T <= 0 || T > MOE_FEW_TOKENS || H < 1 || k < 1 || k > MOE_MAX_TOPK || F < 1 || Fs < 0) return 0;
+  // parts of [T, H] fp32 sums: ceil(kFewParts / groups) at most, of H / columns groups
+  const size_t most = size_t(H) * kFewMostParts, some = size_t(kFewParts) * kFewMaxCols + size_t(H);
+  return few_partial_offset(T, k, F, Fs) + align256(size_t(T) * (most < some ? most : some) * sizeof(float));
 }
 
 namespace {
@@ -488,19 +495,22 @@ Check few_sizes(const char* fn, int64_t T, int32_t H, int32_t E, int32_t k, int3
   if (Fs != 0) MOE_TRY(dim64(fn, "Fs", Fs));
   if (H > (1 << 20) || F > (1 << 20) || Fs > (1 << 20))
     return fail(MOE_ERR_UNSUPPORTED, fn, "H=%lld, F=%lld or Fs exceeds 2^20", H, F);
+  // one expert's matrix is addressed with 32-bit byte offsets
+  if (int64_t(H) * (F > Fs ? F : Fs) * 2 >= (int64_t(1) << 31))
+    return fail(MOE_ERR_UNSUPPORTED, fn, "H=%lld x F=%lld (or Fs) expert matrix reaches 2 GiB", H, F);
   if (renormalize != 0 && renormalize != 1)
     return fail(MOE_ERR_INVALID_ARGUMENT, fn, "renormalize=%lld must be 0 or 1", renormalize);
   return Check{};
 }
 
-Check few_buffers(const char* fn, const void* x, const void* logits, int64_t T, int32_t k, int32_t F, int32_t Fs,
-                  const void* ids, const void* wts, const void* y, const void* ws, size_t ws_bytes) {
+Check few_buffers(const char* fn, const void* x, const void* logits, int64_t T, int32_t H, int32_t k, int32_t F,
+                  int32_t Fs, const void* ids, const void* wts, const void* y, const void* ws, size_t ws_bytes) {
   MOE_TRY(ptr(fn, "x", x));
   MOE_TRY(ptr(fn, "logits", logits));
   MOE_TRY(ptr(fn, "topk_ids", ids));
   MOE_TRY(ptr(fn, "topk_weights", wts));
   MOE_TRY(ptr(fn, "y", y));
-  const size_t need = few_workspace_bytes(T, k, F, Fs);
+  const size_t need = few_workspace_bytes(T, H, k, F, Fs);
   if (ws_bytes < need)
     return fail(MOE_ERR_WORKSPACE_TOO_SMALL, fn, "workspace %lld bytes < %lld needed",
                 (long long)ws_bytes, (long long)need);
@@ -516,27 +526,25 @@ Check validate_few(const void* x, const void* logits, int64_t T, int32_t H, int3
   MOE_TRY(few_sizes(fn, T, H, E, k, F, Fs, renormalize));
   if (T == 0) return Check{};
   for (int i = 0; i < (Fs ? 6 : 3); ++i) MOE_TRY(ptr(fn, kFewNames[i], w[i]));
-  return few_buffers(fn, x, logits, T, k, F, Fs, ids, wts, y, ws, ws_bytes);
+  return few_buffers(fn, x, logits, T, H, k, F, Fs, ids, wts, y, ws, ws_bytes);
 }
 
 Check validate_few_int4(const void* x, const void* logits, int64_t T, int32_t H, int32_t E, int32_t k, int32_t F,
-                        int32_t Fs, int32_t renormalize, int32_t group, const moe_int4* w, const void* ids,
+                        int32_t Fs, int32_t renormalize, int32_t group, int32_t zeros, const moe_int4* w, const void* ids,
                         const void* wts, const void* y, const void* ws, size_t ws_bytes) {
   const char* fn = "moe_few_tokens_int4";
   MOE_TRY(few_sizes(fn, T, H, E, k, F, Fs, renormalize));
   MOE_TRY(int4_dims(fn, H, group));
   MOE_TRY(int4_dims(fn, F, group));
   if (Fs) MOE_TRY(int4_dims(fn, Fs, group));
+  MOE_TRY(zeros_flag(fn, zeros));
   if (T == 0) return Check{};
   if (w == nullptr) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "weights is NULL");
   for (int i = 0; i < (Fs ? 6 : 3); ++i) {
     MOE_TRY(ptr(fn, kFewNames[i], w[i].codes));
     MOE_TRY(ptr(fn, kFewNames[i], w[i].scales));
-    if ((w[i].zeros == nullptr) != (w[0].zeros == nullptr))
-      return fail(MOE_ERR_INVALID_ARGUMENT, fn, "zeros: all tensors have them or none");
-    if (w[i].zeros != nullptr) MOE_TRY(ptr(fn, kFewNames[i], w[i].zeros));
   }
-  return few_buffers(fn, x, logits, T, k, F, Fs, ids, wts, y, ws, ws_bytes);
+  return few_buffers(fn, x, logits, T, H, k, F, Fs, ids, wts, y, ws, ws_bytes);
 }
 
 // ------------------------------------------------------------------ the paged 8-bit cache

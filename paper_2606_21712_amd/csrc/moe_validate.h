@@ -68,21 +68,22 @@ Check validate_combine(const void* y_perm, const int32_t* dest, const float* w, 
 
 // 4-bit weights: packed sizes of one matrix
 size_t int4_code_bytes(int64_t rows, int32_t K);
-size_t int4_groups(int64_t rows, int32_t K, int32_t group);
+size_t int4_scale_bytes(int64_t rows, int32_t K, int32_t group, int zeros);
 Check validate_quantize_int4(const void* src, int64_t rows, int32_t K, int32_t group, const void* codes,
                              const void* scales, const void* zeros);
 Check validate_pack_int4(const void* codes, const void* scales, const void* zeros, int64_t matrices, int64_t rows,
-                         int32_t K, int32_t group, const void* out_codes, const void* out_scales,
-                         const void* out_zeros);
-Check validate_matvec_int4(const void* x, const void* codes, const void* scales, const void* zeros, int64_t T,
-                           int32_t N, int32_t K, int32_t group, const void* y);
-// The layer for few tokens: weights in the order gate, up, down, shared gate, up, down; workspace h
-size_t few_workspace_bytes(int64_t T, int32_t k, int32_t F, int32_t Fs);
+                         int32_t K, int32_t group, const void* out_codes, const void* out_scales);
+Check validate_matvec_int4(const void* x, const void* codes, const void* scales, int32_t zeros, int64_t T, int32_t N,
+                           int32_t K, int32_t group, const void* y);
+// The layer for few tokens: weights in the order gate, up, down, shared gate, up, down.
+// Workspace: [h | parts of the down projection]
+size_t few_workspace_bytes(int64_t T, int32_t H, int32_t k, int32_t F, int32_t Fs);
+size_t few_partial_offset(int64_t T, int32_t k, int32_t F, int32_t Fs);
 Check validate_few(const void* x, const void* logits, int64_t T, int32_t H, int32_t E, int32_t k, int32_t F,
                    int32_t Fs, int32_t renormalize, const void* const (&w)[6], const void* ids, const void* wts,
                    const void* y, const void* ws, size_t ws_bytes);
 Check validate_few_int4(const void* x, const void* logits, int64_t T, int32_t H, int32_t E, int32_t k, int32_t F,
-                        int32_t Fs, int32_t renormalize, int32_t group, const moe_int4* w, const void* ids,
+                        int32_t Fs, int32_t renormalize, int32_t group, int32_t zeros, const moe_int4* w, const void* ids,
                         const void* wts, const void* y, const void* ws, size_t ws_bytes);
 // The paged 8-bit cache
 Check validate_kv8_append(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,

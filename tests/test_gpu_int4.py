@@ -43,9 +43,14 @@ def pack_plain(q, s, z, g):
     def spread(v, fill):
         out = torch.full((Np, Kp // g), fill, dtype=v.dtype)
         out[:N, :K // g] = v
-        return out.reshape(Np // 16, 16, Kp // g).transpose(1, 2).reshape(-1)
+        return out.reshape(Np // 16, 4, 4, Kp // 128, 128 // g).permute(0, 3, 1, 4, 2).reshape(-1)
 
-    return codes, spread(s, 0), None if z is None else spread(z, 8)
+    s = spread(s, 0).view(torch.int16).int()
+    if z is not None:                                # words: the scale above, 128 + z in bf16 below
+        s = (s << 16) | (spread(z, 8).float() + 128).to(torch.bfloat16).view(torch.int16).int()
+    else:
+        s = s.to(torch.int16)
+    return codes, s.view(torch.uint8)
 
 
 def random_int4(N, K, g, zeros, seed):
@@ -90,14 +95,14 @@ def test_pack(N, K, g, zeros):
     log(f"[gpu] pack int4 {N}x{K} g={g} zeros={zeros}")
     q, s, z = random_int4(N, K, g, zeros, N + K)
     w = on_gpu(q, s, z, g)
-    codes, scales, zz = pack_plain(q, s, z, g)
+    codes, scales = pack_plain(q, s, z, g)
     assert torch.equal(w.codes.cpu(), codes)
-    assert torch.equal(w.scales.cpu().view(torch.int16), scales.view(torch.int16))
-    assert zz is None if not zeros else torch.equal(w.zeros.cpu(), zz)
+    assert torch.equal(w.scales.cpu(), scales)
     # a tensor of several matrices is the matrices one after the other
     w2 = moe.moe_pack_int4(torch.stack([standard(q)] * 3).cuda(), torch.stack([s] * 3).cuda(),
                            None if z is None else torch.stack([z] * 3).cuda(), g)
-    assert torch.equal(w2.codes, w.codes.repeat(3)) and w2.shape == (3, N, K)
+    assert torch.equal(w2.codes, w.codes.repeat(3)) and torch.equal(w2.scales, w.scales.repeat(3))
+    assert w2.shape == (3, N, K)
 
 
 @pytest.mark.parametrize("T", [1, 2, 5, 15, 16, 17, 31, 33, 48, 64, 65, 130])
