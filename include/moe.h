@@ -504,7 +504,7 @@ moe_status moe_kv8_append(const void* q, int64_t q_stride, const void* k, int64_
  *   max_new     at least every sequence's row count: rows beyond it are not computed
  *   max_len     the longest sequence (for the plan only; any value gives right results)
  *   window      0, or how many tokens a row sees, itself included
- *   scale       factor of the scores
+ *   scale       factor of the scores, positive
  *   out         bf16 [T, q_heads, dim]   out
  *   ws, ws_bytes  device scratch of at least moe_kv8_attention_workspace_bytes() for the same sizes
  *
@@ -515,8 +515,8 @@ moe_status moe_kv8_append(const void* q, int64_t q_stride, const void* k, int64_
  * Errors: as moe_kv8_append, plus INVALID_ARGUMENT for max_new < 1, max_len < 0, window < 0;
  * WORKSPACE_TOO_SMALL.
  */
-size_t moe_kv8_attention_workspace_bytes(int32_t B, int32_t q_heads, int32_t heads, int32_t dim, int32_t max_new,
-                                         int32_t max_len, int32_t window);
+size_t moe_kv8_attention_workspace_bytes(int64_t T, int32_t B, int32_t q_heads, int32_t heads, int32_t dim,
+                                         int32_t max_new, int32_t max_len, int32_t window);
 moe_status moe_kv8_attention(const void* q, int64_t T, int32_t q_heads, const moe_kv8_cache* cache,
                              const int32_t* block_table, int32_t table_cols, const int32_t* seq_lens,
                              const int32_t* cu_tokens, int32_t B, int32_t max_new, int32_t max_len, int32_t window,

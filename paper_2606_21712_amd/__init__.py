@@ -101,7 +101,7 @@ _SIGNATURES = {
                                            ctypes.POINTER(_Int4Ref), _P, _P, _P, _P, _SZ, _P]),
     "moe_kv8_append": (ctypes.c_int, [_P, _I64, _P, _I64, _P, _I64, _I64, _I32, _P, _I64, _I32, _I32,
                                       ctypes.POINTER(_Kv8Cache), _P, _I32, _P, _P, _I32, _P, _P]),
-    "moe_kv8_attention_workspace_bytes": (_SZ, [_I32, _I32, _I32, _I32, _I32, _I32, _I32]),
+    "moe_kv8_attention_workspace_bytes": (_SZ, [_I64, _I32, _I32, _I32, _I32, _I32, _I32, _I32]),
     "moe_kv8_attention": (ctypes.c_int, [_P, _I64, _I32, ctypes.POINTER(_Kv8Cache), _P, _I32, _P, _P, _I32, _I32, _I32,
                                          _I32, ctypes.c_float, _P, _P, _SZ, _P]),
     "moe_profiler_start": (ctypes.c_int, [ctypes.c_int]),
@@ -614,8 +614,8 @@ def moe_kv8_append(q, k, v, cos_sin, cache, block_table, seq_lens, cu_tokens, in
 
 
 def moe_kv8_attention_workspace_bytes(T, B, q_heads, heads, dim, max_new, max_len, window=0) -> int:
-    """Bytes of scratch for T rows of B sequences (T = 0: none)."""
-    return lib().moe_kv8_attention_workspace_bytes(B, q_heads, heads, dim, max_new, max_len, window) if T else 0
+    """Bytes of scratch for T rows of B sequences."""
+    return lib().moe_kv8_attention_workspace_bytes(T, B, q_heads, heads, dim, max_new, max_len, window)
 
 
 def moe_kv8_attention(q, cache, block_table, seq_lens, cu_tokens, max_new, max_len, window=0, scale=None, out=None,

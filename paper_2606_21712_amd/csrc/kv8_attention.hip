@@ -15,9 +15,15 @@
 //                  two products; B operand: the probabilities, which lane group g already
 //                  holds for block g.  No score moves between lanes.
 //
-// Codes are expanded to bf16 exactly (E4M3 has four significant bits); the keys' exponent goes
-// into the scores and the values' into the probabilities, both powers of two.  Scores, maxima,
-// sums and outputs are fp32; probabilities are rounded to bf16 (2^-9 relative) for the product.
+// Codes times their block's power of two are expanded to bf16 exactly (E4M3 has four significant
+// bits), in one instruction for two.  Scores, maxima and outputs are fp32; probabilities are rounded to
+// bf16 (2^-9 relative) for the product.  Their sum is one more row of that product, of ones: fp32
+// sums of the rounded probabilities, which is what the values are weighted with.
+//
+// Work is dealt by what the sequences hold, which only the device knows: every workgroup adds up the
+// batch's chunks and takes the quota that gives `target` workgroups; a tile that spans more is
+// cut into parts of equal length.  Parts write their sums, maxima and outputs to scratch, and
+// kv8_join adds them up, in order.
 #include <algorithm>
 
 #include "kv8.h"
@@ -26,193 +32,262 @@ namespace moe {
 namespace {
 
 constexpr int kAttWaves = 4;
-constexpr int kChunk = 64;                    // tokens that a wavefront takes at a time
+constexpr int kChunk = 64;                    // tokens: the unit in which work is dealt
+constexpr int kMinChunks = 2 * kAttWaves;     // of a part: a tile is not cut below this
 constexpr float kLow = -1e30f;                // below every score: the maximum before any token
-
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
-// Eight E4M3 codes -> bf16, exact.
-__device__ __forceinline__ bf16x8 expand8(uint32_t lo, uint32_t hi) {
+// Eight E4M3 codes times a power of two -> bf16, exact down to bf16's smallest values.
+__device__ __forceinline__ bf16x8 expand8(uint32_t lo, uint32_t hi, float scale) {
   u32x4 v;
-  v[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false));
-  v[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true));
-  v[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false));
-  v[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true));
+  v[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false));
+  v[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true));
+  v[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false));
+  v[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true));
   return __builtin_bit_cast(bf16x8, v);
 }
 
-__device__ __forceinline__ float exp2_of(uint32_t e) {        // 2^(e - 127), 0 for e = 0
+__device__ __forceinline__ float exp2_of(uint32_t e) {        // 2^(e - 127); the conversion reads the exponent
   return __uint_as_float(e << 23);
 }
 
-// What a tile sees: the rows and the chunks of tokens of one part of it.
-struct Span {
-  int row0, fresh, len;     // the sequence's first row, new tokens and tokens
-  int rows;                 // query rows of the tile (of 16 R)
-  int begin, end;           // chunks
-};
-
-__device__ __forceinline__ Span span_of(const Kv8Batch& b, int seq, int G, int tile, int tile_rows, int split,
-                                        int splits, int64_t window, int64_t capacity) {
-  Span s;
-  s.row0 = b.cu[seq];
-  s.fresh = b.cu[seq + 1] - s.row0;
-  s.len = int(min(int64_t(b.lens[seq]), capacity));
-  const int first = tile * tile_rows;
-  s.rows = int(min(int64_t(tile_rows), int64_t(s.fresh) * G - first));
-  s.begin = s.end = 0;
-  if (s.rows <= 0) return s;
-  const int64_t past = int64_t(s.len) - s.fresh;
-  const int64_t last = past + (first + s.rows - 1) / G;       // position of the last row
-  const int64_t low = window > 0 ? max(past + first / G - window + 1, int64_t(0)) : 0;
-  const int c0 = int(low / kChunk), c1 = last < 0 ? 0 : int(last / kChunk) + 1;
-  if (c1 <= c0) return s;
-  const int each = (c1 - c0 + splits - 1) / splits;
-  s.begin = min(c0 + split * each, c1);
-  s.end = min(s.begin + each, c1);
-  return s;
+// Maximum over the four lanes l, l ^ 16, l ^ 32, l ^ 48: exchanges of rows of 16 and of halves.
+__device__ __forceinline__ float max_of_groups(float v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-template <int D, int R>
-__global__ __launch_bounds__(64 * kAttWaves) void kv8_attention_kernel(Kv8Cache c, Kv8Batch b, Kv8Attend a,
-                                                                       Kv8Plan plan) {
+__device__ __forceinline__ int wave_sum(int v) {
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) v += __shfl_xor(v, d);
+  return v;
+}
+__device__ __forceinline__ int wave_scan(int v, int lane) {   // inclusive
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) {
+    const int u = __shfl_up(v, d);
+    v += lane >= d ? u : 0;
+  }
+  return v;
+}
+
+// A sequence's first row, new tokens and tokens; its tiles, and the most chunks that one of them spans.
+struct Cut {
+  int row0, fresh, len, tiles, chunks;
+};
+__device__ __forceinline__ Cut cut_of(const Kv8Batch& b, const Kv8Attend& a, const Kv8Plan& p, int G, int seq) {
+  Cut c = {0, 0, 0, 0, 0};
+  if (seq >= b.sequences) return c;
+  c.row0 = b.cu[seq];
+  c.fresh = b.cu[seq + 1] - c.row0;
+  c.len = min(b.lens[seq], p.capacity);
+  if (c.fresh <= 0) return c;
+  c.tiles = int(min((int64_t(c.fresh) * G + p.rows - 1) / p.rows, int64_t(p.tiles)));
+  c.chunks = (max(c.len, 0) + kChunk - 1) / kChunk;
+  if (a.window > 0) c.chunks = min(c.chunks, int((int64_t(a.window) + p.rows) / kChunk + 2));
+  return c;
+}
+
+// Which tile, and part of it, workgroup `id` is; seq < 0: none.  Workgroups of a sequence follow one
+// another, its heads fastest: they go round the XCDs, and with as many heads as XCDs a head's
+// tiles share one L2.  Later tiles, which see more, come first.
+struct Work {
+  int seq, row0, fresh, len, head, tile, part, parts;
+};
+__device__ __forceinline__ Work find_work(const Kv8Batch& b, const Kv8Attend& a, const Kv8Plan& p, int heads, int G,
+                                          int id, int lane) {
+  Cut c = cut_of(b, a, p, G, lane);
+  int quota = 1 << 30;
+  if (p.target > 0) {
+    int sum = c.tiles * c.chunks;
+    for (int s0 = kWave; s0 < b.sequences; s0 += kWave) {
+      const Cut d = cut_of(b, a, p, G, s0 + lane);
+      sum += d.tiles * d.chunks;
+    }
+    const int64_t total = int64_t(wave_sum(sum)) * heads;
+    quota = int(max(int64_t(kMinChunks), (total + p.target - 1) / p.target));
+  }
+  int before = 0;
+  for (int s0 = 0; s0 < b.sequences; s0 += kWave) {
+    if (s0 > 0) c = cut_of(b, a, p, G, s0 + lane);
+    const int parts = max(1, (c.chunks + quota - 1) / quota);
+    const int n = c.tiles * parts * heads;
+    const int upto = before + wave_scan(n, lane);
+    const uint64_t m = __ballot(upto > id);
+    if (m != 0) {
+      const int at = __builtin_ctzll(m);
+      Work w;
+      w.seq = s0 + at;
+      w.row0 = __builtin_amdgcn_readlane(c.row0, at);
+      w.fresh = __builtin_amdgcn_readlane(c.fresh, at);
+      w.len = __builtin_amdgcn_readlane(c.len, at);
+      w.parts = __builtin_amdgcn_readlane(parts, at);
+      const int local = id - __builtin_amdgcn_readlane(upto - n, at);
+      w.head = local % heads;
+      w.part = local / heads % w.parts;
+      w.tile = __builtin_amdgcn_readlane(c.tiles, at) - 1 - local / heads / w.parts;
+      return w;
+    }
+    before = __builtin_amdgcn_readlane(upto, kWave - 1);
+  }
+  return Work{-1, 0, 0, 0, 0, 0, 0, 1};
+}
+
+// What kv8_join has to know of a row: the workgroup of its first part (the others follow a head count
+// apart), and its parts times 64 plus its place in the tile.
+struct RowParts {
+  int first, parts64;
+};
+
+// R: 16 query rows each.  A wavefront takes 16 NW tokens at a time (NW = 4 or 2); a lane group has 4 NW of
+// them, a block or half of one.  UNIFORM: a page holds whole steps, so that a step's page is one number.
+template <int D, int R, int NW, int OCC, bool UNIFORM>
+__global__ __launch_bounds__(64 * kAttWaves, OCC) void kv8_attention_kernel(Kv8Cache c, Kv8Batch b, Kv8Attend a, Kv8Plan plan) {
   constexpr int KS = D / 32;                  // products of 32 dimensions
   constexpr int DT = D / 16;                  // tiles of 16 dimensions
+  constexpr int kTok = 16 * NW, kHalf = 4 / NW;   // tokens of a step, lane groups of a block
+  typedef uint32_t vwords __attribute__((ext_vector_type(NW)));
   __shared__ float ml[kAttWaves][2][16 * R];
   __shared__ f32x4 oo[kAttWaves / 2][DT * R][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __shared__ u32x4 ql[R][KS][64];             // the queries, as operands: all wavefronts have the same
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 4, col = lane & 15;
-  int id = blockIdx.x;
-  const int split = id % plan.splits;
-  id /= plan.splits;
-  const int tile = id % plan.tiles;
-  id /= plan.tiles;
-  const int head = id % c.heads, seq = id / c.heads;
   const int G = a.q_heads / c.heads;
-  const int per_page = c.page / kKvBlock;
-  const Span sp = span_of(b, seq, G, tile, 16 * R, split, plan.splits, a.window, int64_t(b.table_cols) * c.page);
-  if (sp.rows <= 0) return;
+  const Work w = find_work(b, a, plan, c.heads, G, blockIdx.x, lane);
+  if (w.seq < 0) return;
+  const int row0 = w.row0, fresh = w.fresh, len = w.len;
+  const int first_row = w.tile * 16 * R;
+  const int rows = min(16 * R, int(min(int64_t(fresh) * G, int64_t(1) << 30)) - first_row);
+  // positions of the first and the last row, and the chunks that they see: this part's share
+  const int first_pos = len - fresh + first_row / G, last_pos = len - fresh + (first_row + rows - 1) / G;
+  const int low = a.window > 0 ? max(first_pos - a.window + 1, 0) : 0;
+  const int c0 = low / kChunk, c1 = last_pos < 0 ? c0 : last_pos / kChunk + 1;
+  const int each = (max(c1 - c0, 0) + w.parts - 1) / w.parts;
+  const int begin = min(c0 + w.part * each, c1) * (kChunk / kTok), end = min(c0 + (w.part + 1) * each, c1) * (kChunk / kTok);
 
   // queries: row r is token r / G, head r % G of the group
-  bf16x8 q[R][KS];
   int pos[R];                                 // position of the column's token; -1: sees nothing
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const int local = 16 * r + col;
-    const int row = tile * 16 * R + local;
-    const int64_t t = int64_t(sp.row0) + row / G;
-    const bool on = local < sp.rows && t < b.tokens;
-    pos[r] = on ? sp.len - sp.fresh + row / G : -1;
-    const uint16_t* p = a.q + (t * a.q_heads + head * G + row % G) * D;
+    const int row = first_row + local;
+    const int64_t t = int64_t(row0) + row / G;
+    const bool on = local < rows && t < b.tokens;
+    pos[r] = on ? len - fresh + row / G : -1;
+    if (r % kAttWaves != wave && R > 1) continue;
+    const uint16_t* p = a.q + (t * a.q_heads + w.head * G + row % G) * D;
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
+      if (R == 1 && s % kAttWaves != wave) continue;
       u32x4 v = {0u, 0u, 0u, 0u};
       if (on) v = *reinterpret_cast<const u32x4*>(p + 64 * (s / 2) + 16 * g + 8 * (s % 2));
-      q[r][s] = __builtin_bit_cast(bf16x8, v);
+      ql[r][s][lane] = v;
     }
   }
-  const int first_pos = sp.len - sp.fresh + tile * 16 * R / G;
-  const int last_pos = sp.len - sp.fresh + (tile * 16 * R + sp.rows - 1) / G;
+  __syncthreads();
 
-  f32x4 o[DT][R];
-  float m[R], l[R];
+  f32x4 o[DT][R], l[R];                       // l: the sum, in every element
+  float m[R];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     m[r] = kLow;
-    l[r] = 0.f;
+    l[r] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[d][r] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   const float scale = a.scale * 1.44269504088896f;            // scores in powers of two
-  const int last_block = (sp.len - 1) / kKvBlock;
 
-  // a block's index in the cache; past the end of the sequence the last block stands in
-  auto locate = [&](int block) {
-    block = min(block, last_block);
-    const int page = b.table[int64_t(seq) * b.table_cols + block / per_page];
-    const int64_t inside = min(max(int64_t(page), int64_t(0)), c.pages - 1);
-    return kv_block(inside, head, block % per_page, c.heads, per_page);
+  // Where a step's blocks are: the lane's of the keys (a row of the first product) and of the values.  A
+  // page is looked up a step ahead of its loads.  Past the end of the sequence the last block stands in,
+  // where a page does not hold the whole step.
+  const int k_of = (col >> 2) / kHalf, v_of = g / kHalf;      // the lane's blocks of a step
+  const int per_page = c.page / kKvBlock, last_block = max(len - 1, 0) / kKvBlock;
+  const int32_t* table = b.table + int64_t(w.seq) * b.table_cols;
+  const uint32_t page_blocks = uint32_t(c.heads) * uint32_t(per_page), head_blocks = uint32_t(w.head) * uint32_t(per_page);
+  struct Block {
+    int page, inside;
+  };
+  struct Place {
+    Block k, v;                               // UNIFORM: k alone, of the step's first block
+  };
+  auto find = [&](int block) {
+    // block / per_page, by the reciprocal rounded down: one too few at most
+    int at = int(__umulhi(uint32_t(block), plan.inverse)), rest = block - at * per_page;
+    const bool more = rest >= per_page;
+    at += more ? 1 : 0;
+    rest -= more ? per_page : 0;
+    return Block{table[at], rest};
+  };
+  auto look_up = [&](int step) {
+    Place x;
+    if (UNIFORM) {
+      x.k = find(NW * step);
+    } else {
+      x.k = find(min(NW * step + k_of, last_block));
+      x.v = find(min(NW * step + v_of, last_block));
+    }
+    return x;
+  };
+  auto block_at = [&](const Block& x) {                       // among the cache's blocks
+    const uint32_t page = min(uint32_t(max(x.page, 0)), uint32_t(c.pages - 1));
+    return uint64_t(page) * page_blocks + (head_blocks + uint32_t(x.inside));
+  };
+  // A read-once load where one tile reads what it sees: its heads share the rows.
+  auto fetch = [&](const auto* p) {
+    if constexpr (R == 1) return __builtin_nontemporal_load(p);
+    else return *p;
   };
 
-  for (int ch = sp.begin + wave; ch < sp.end; ch += kAttWaves) {
-    const int64_t kb = locate(4 * ch + (col >> 2)), vb = locate(4 * ch + g);
-    u32x4 kc[4][D / 64], vc[DT];
+  u32x4 kc[NW][D / 64];
+  vwords vc[DT];
+  uint32_t ke, ve;
+  const uint32_t k_lane = ((col >> 2) % kHalf * (4 * NW) + (col & 3)) * D + 16 * g;   // inside a block
+  const uint32_t v_lane = col * kKvBlock + g % kHalf * (4 * NW);
+  auto load_k = [&](const Place& x) {
+    const uint64_t at = block_at(x.k);
+    const uint8_t* p = c.k_codes + at * (kKvBlock * D) + (UNIFORM ? k_of * (kKvBlock * D) + k_lane : k_lane);
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int t = 0; t < NW; ++t)
 #pragma unroll
-      for (int s = 0; s < D / 64; ++s)
-        kc[t][s] = *reinterpret_cast<const u32x4*>(c.k_codes + kb * (kKvBlock * D) + (4 * t + (col & 3)) * D + 64 * s +
-                                                   16 * g);
+      for (int s = 0; s < D / 64; ++s) kc[t][s] = fetch(reinterpret_cast<const u32x4*>(p + 4 * t * D + 64 * s));
+    ke = c.k_exps[at + (UNIFORM ? k_of : 0)];
+  };
+  auto load_v = [&](const Place& x) {
+    const uint64_t at = block_at(UNIFORM ? x.k : x.v);
+    const uint8_t* p = c.v_codes + at * (kKvBlock * D) + (UNIFORM ? v_of * (kKvBlock * D) + v_lane : v_lane);
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
-      vc[d] = *reinterpret_cast<const u32x4*>(c.v_codes + vb * (kKvBlock * D) + (16 * d + col) * kKvBlock);
-    const float kf = exp2_of(c.k_exps[vb]) * scale, vf = exp2_of(c.v_exps[vb]);
+    for (int d = 0; d < DT; ++d) vc[d] = fetch(reinterpret_cast<const vwords*>(p + 16 * d * kKvBlock));
+    ve = c.v_exps[at + (UNIFORM ? v_of : 0)];
+  };
 
-    const int t0 = ch * kChunk + kKvBlock * g;                // first token of the lane's block
-    if (ch * kChunk + kChunk > sp.len) {                      // codes past the end: anything, NaN too
-      const int n = min(max(sp.len - t0, 0), kKvBlock);
+  auto scores = [&](f32x4 (&s)[NW][R]) {
+    const float kf = exp2_of(ke);
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const int k = min(max(n - 4 * w, 0), 4);
-        const uint32_t keep = k == 4 ? 0xFFFFFFFFu : (1u << (8 * k)) - 1u;
-#pragma unroll
-        for (int d = 0; d < DT; ++d) vc[d][w] &= keep;
-      }
-    }
-    // In a chunk that some row does not see in full, a NaN among the values must not reach the rows
-    // that do not see it, and 0 NaN is NaN: such codes are taken out, and the rows that see
-    // their token get a NaN score instead.
-    const bool edge = ch * kChunk + kChunk - 1 > first_pos || (a.window > 0 && last_pos - ch * kChunk >= a.window);
-    uint32_t bad[4] = {0u, 0u, 0u, 0u};                       // bit 8 i + 7 of word t: token 4 t + i of the block
-    if (edge) {
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-#pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          const uint32_t n = ((vc[d][w] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
-          vc[d][w] &= ~((n >> 7) * 0xFFu);
-          bad[w] |= n;
-        }
-#pragma unroll
-        for (int i = 1; i < 16; i <<= 1) bad[w] |= uint32_t(__shfl_xor(int(bad[w]), i));
-      }
-    }
-    f32x4 s[4][R];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
+    for (int t = 0; t < NW; ++t) {
 #pragma unroll
       for (int r = 0; r < R; ++r) s[t][r] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
-        const bf16x8 ka = expand8(kc[t][k / 2][2 * (k % 2)], kc[t][k / 2][2 * (k % 2) + 1]);
+        const bf16x8 ka = expand8(kc[t][k / 2][2 * (k % 2)], kc[t][k / 2][2 * (k % 2) + 1], kf);
 #pragma unroll
-        for (int r = 0; r < R; ++r) s[t][r] = mfma16(ka, q[r][k], s[t][r]);
+        for (int r = 0; r < R; ++r) s[t][r] = mfma16(ka, __builtin_bit_cast(bf16x8, ql[r][k][lane]), s[t][r]);
       }
     }
-    bf16x8 p[2][R];
+  };
+  // Probabilities of a step as the operands of the second product; masked scores are -infinity.
+  auto softmax = [&](const f32x4 (&s)[NW][R], bf16x8 (&p)[NW / 2][R]) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      float mx = -INFINITY;
+      float mx = fmaxf(fmaxf(s[0][r][0], s[0][r][1]), fmaxf(s[0][r][2], s[0][r][3]));
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float x = s[t][r][i] * kf;
-          if (edge) {
-            const int tok = t0 + 4 * t + i;
-            if ((bad[t] >> (8 * i + 7)) & 1u) x = NAN;
-            if (tok > pos[r] || (a.window > 0 && pos[r] - tok >= a.window)) x = -INFINITY;
-          }
-          s[t][r][i] = x;
-          mx = fmaxf(mx, x);
-        }
-      mx = fmaxf(mx, __shfl_xor(mx, 16));
-      mx = fmaxf(mx, __shfl_xor(mx, 32));
-      const float mn = fmaxf(m[r], mx);
+      for (int t = 1; t < NW; ++t)
+        mx = fmaxf(mx, fmaxf(fmaxf(s[t][r][0], s[t][r][1]), fmaxf(s[t][r][2], s[t][r][3])));
+      const float mn = fmaxf(m[r], max_of_groups(mx) * scale);
       if (__ballot(mn > m[r]) != 0) {
         const float f = __builtin_amdgcn_exp2f(m[r] - mn);
         l[r] *= f;
@@ -220,39 +295,97 @@ __global__ __launch_bounds__(64 * kAttWaves) void kv8_attention_kernel(Kv8Cache 
         for (int d = 0; d < DT; ++d) o[d][r] *= f;
         m[r] = mn;
       }
-      float sum = 0.f;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        u32x4 w;
+      for (int h = 0; h < NW / 2; ++h) {
+        u32x4 v;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float e0 = __builtin_amdgcn_exp2f(s[2 * h + i / 2][r][2 * (i % 2)] - mn);
-          const float e1 = __builtin_amdgcn_exp2f(s[2 * h + i / 2][r][2 * (i % 2) + 1] - mn);
-          sum += e0 + e1;
-          w[i] = pack_bf16x2(e0 * vf, e1 * vf);
-        }
-        p[h][r] = __builtin_bit_cast(bf16x8, w);
+        for (int i = 0; i < 4; ++i)
+          v[i] = pack_bf16x2(
+              __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * h + i / 2][r][2 * (i % 2)], scale, -mn)),
+              __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * h + i / 2][r][2 * (i % 2) + 1], scale, -mn)));
+        p[h][r] = __builtin_bit_cast(bf16x8, v);
       }
-      l[r] += sum;
     }
+  };
+  auto weigh = [&](const bf16x8 (&p)[NW / 2][R]) {
+    const float vf = exp2_of(ve);
+    const u32x4 ones = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
+#pragma unroll
+    for (int h = 0; h < NW / 2; ++h)
+#pragma unroll
+      for (int r = 0; r < R; ++r) l[r] = mfma16(__builtin_bit_cast(bf16x8, ones), p[h][r], l[r]);
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const bf16x8 va = expand8(vc[d][2 * h], vc[d][2 * h + 1]);
+      for (int h = 0; h < NW / 2; ++h) {
+        const bf16x8 va = expand8(vc[d][2 * h], vc[d][2 * h + 1], vf);
 #pragma unroll
         for (int r = 0; r < R; ++r) o[d][r] = mfma16(va, p[h][r], o[d][r]);
       }
+  };
+  // In a chunk that some row does not see in full: codes of values past the end are anything, NaN too,
+  // and so may be those of a token that a row must not see, and 0 NaN is NaN.  Such codes are taken
+  // out, and the rows that do see their token get a NaN score instead.
+  auto mask = [&](int ch, f32x4 (&s)[NW][R]) {
+    const int t0 = ch * kTok + 4 * NW * g;                    // first of the lane's tokens
+    const int n = min(max(len - t0, 0), 4 * NW);
+    uint32_t bad[NW];                                         // bit 8 i + 7 of word t: its token 4 t + i
+#pragma unroll
+    for (int t = 0; t < NW; ++t) {
+      const int k = min(max(n - 4 * t, 0), 4);
+      const uint32_t keep = k == 4 ? 0xFFFFFFFFu : (1u << (8 * k)) - 1u;
+      bad[t] = 0;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        const uint32_t x = vc[d][t] & keep;
+        const uint32_t nan = ((x & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+        vc[d][t] = x & ~(nan | (nan - (nan >> 7)));
+        bad[t] |= nan;
+      }
+#pragma unroll
+      for (int i = 1; i < 16; i <<= 1) bad[t] |= uint32_t(__shfl_xor(int(bad[t]), i));
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int t = 0; t < NW; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int tok = t0 + 4 * t + i;
+          float x = s[t][r][i];
+          x = (bad[t] >> (8 * i + 7)) & 1u ? NAN : x;
+          s[t][r][i] = tok > pos[r] || (a.window > 0 && pos[r] - tok >= a.window) ? -INFINITY : x;
+        }
+  };
+
+  // The loads of the next step are issued as soon as the registers of this one's are free: the keys
+  // after the scores, the values after the second product.
+  const int last = end - 1;
+  if (begin + wave < end) {
+    int ch = begin + wave;
+    Place at = look_up(ch);
+    load_k(at);
+    load_v(at);
+    at = look_up(min(ch + kAttWaves, last));
+    for (; ch < end; ch += kAttWaves) {
+      f32x4 s[NW][R];
+      scores(s);
+      load_k(at);
+      if (ch * kTok + kTok - 1 > first_pos || (a.window > 0 && last_pos - ch * kTok >= a.window)) mask(ch, s);
+      bf16x8 p[NW / 2][R];
+      softmax(s, p);
+      weigh(p);
+      load_v(at);
+      at = look_up(min(ch + 2 * kAttWaves, last));
+    }
   }
 
   // join the wavefronts: all maxima and sums, then the outputs of half the waves at a time
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    l[r] += __shfl_xor(l[r], 16);
-    l[r] += __shfl_xor(l[r], 32);
     if (g == 0) {
       ml[wave][0][16 * r + col] = m[r];
-      ml[wave][1][16 * r + col] = l[r];
+      ml[wave][1][16 * r + col] = l[r][0];
     }
   }
   __syncthreads();
@@ -261,11 +394,11 @@ __global__ __launch_bounds__(64 * kAttWaves) void kv8_attention_kernel(Kv8Cache 
   for (int r = 0; r < R; ++r) {
     top[r] = kLow;
 #pragma unroll
-    for (int w = 0; w < kAttWaves; ++w) top[r] = fmaxf(top[r], ml[w][0][16 * r + col]);
+    for (int v = 0; v < kAttWaves; ++v) top[r] = fmaxf(top[r], ml[v][0][16 * r + col]);
     total[r] = 0.f;
 #pragma unroll
-    for (int w = 0; w < kAttWaves; ++w)
-      total[r] += ml[w][1][16 * r + col] * __builtin_amdgcn_exp2f(ml[w][0][16 * r + col] - top[r]);
+    for (int v = 0; v < kAttWaves; ++v)
+      total[r] += ml[v][1][16 * r + col] * __builtin_amdgcn_exp2f(ml[v][0][16 * r + col] - top[r]);
     const float f = __builtin_amdgcn_exp2f(m[r] - top[r]);
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[d][r] *= f;
@@ -291,20 +424,24 @@ __global__ __launch_bounds__(64 * kAttWaves) void kv8_attention_kernel(Kv8Cache 
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const int local = 16 * r + col;
-    if (local >= sp.rows) continue;
-    const int row = tile * 16 * R + local;
-    const int64_t t = int64_t(sp.row0) + row / G;
+    if (local >= rows) continue;
+    const int row = first_row + local;
+    const int64_t t = int64_t(row0) + row / G;
     if (t >= b.tokens) continue;
-    if (plan.splits == 1) {
-      const float inv = total[r] > 0.f ? 1.0f / total[r] : (total[r] == 0.f ? 0.f : total[r]);
-      uint16_t* out = a.out + (t * a.q_heads + head * G + row % G) * D + 4 * g;
+    if (w.parts == 1) {
+      if (plan.target > 0 && g == 0)
+        reinterpret_cast<RowParts*>(a.ws)[t * a.q_heads + w.head * G + row % G] = RowParts{0, 64};
+      const float inv = total[r] > 0.f ? 1.0f / total[r] : total[r] == 0.f ? 0.f : total[r];
+      uint16_t* out = a.out + (t * a.q_heads + w.head * G + row % G) * D + 4 * g;
 #pragma unroll
       for (int d = 0; d < DT; ++d)
         *reinterpret_cast<u32x2*>(out + 16 * d) =
             u32x2{pack_bf16x2(o[d][r][0] * inv, o[d][r][1] * inv), pack_bf16x2(o[d][r][2] * inv, o[d][r][3] * inv)};
     } else {
-      // [tile][split][row][D + 2]: the sums, then the maximum and the sum of the softmax
-      float* part = a.ws + ((int64_t(blockIdx.x)) * (16 * R) + local) * (D + 4);
+      if (g == 0 && w.part == 0)
+        reinterpret_cast<RowParts*>(a.ws)[t * a.q_heads + w.head * G + row % G] = RowParts{int(blockIdx.x), w.parts * 64 + local};
+      // [workgroup][row][D + 4]: the sums, then the maximum and the sum of the softmax
+      float* part = a.ws + plan.row_words + (int64_t(blockIdx.x) * (16 * R) + local) * (D + 4);
 #pragma unroll
       for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(part + 16 * d + 4 * g) = o[d][r];
       if (g == 0) {
@@ -315,88 +452,132 @@ __global__ __launch_bounds__(64 * kAttWaves) void kv8_attention_kernel(Kv8Cache 
   }
 }
 
-// Joins the parts of each row: one wavefront a row.
+// Joins the parts of a row (token, query head) that has several: one workgroup a row, its wavefronts
+// deal the parts among themselves, eight at a time in flight, and are joined in order.
 template <int D>
 __global__ __launch_bounds__(256) void kv8_join_kernel(Kv8Cache c, Kv8Batch b, Kv8Attend a, Kv8Plan plan) {
-  const int lane = threadIdx.x & 63;
-  const int64_t unit = (int64_t(blockIdx.x) * 256 + threadIdx.x) / 64;
-  const int local = int(unit % plan.rows);
-  int64_t id = unit / plan.rows;
-  const int64_t tile_id = id;
-  const int tile = int(id % plan.tiles);
-  id /= plan.tiles;
-  const int head = int(id % c.heads);
-  const int64_t seq = id / c.heads;
-  if (seq >= b.sequences) return;
-  const int G = a.q_heads / c.heads;
-  const int row0 = b.cu[seq], fresh = b.cu[seq + 1] - row0;
-  const int64_t row = int64_t(tile) * plan.rows + local;
-  if (row >= int64_t(fresh) * G) return;
-  const int64_t t = row0 + row / G;
-  if (t >= b.tokens) return;
-  const float* part = a.ws + (tile_id * plan.splits * plan.rows + local) * (D + 4);
-  const int64_t stride = int64_t(plan.rows) * (D + 4);
-  float top = kLow;
-  for (int s = 0; s < plan.splits; ++s) top = fmaxf(top, part[s * stride + D]);
-  constexpr int kPer = D / 64;
-  float acc[kPer], total = 0.f;
+  constexpr int kPer = D / 64, kAhead = 8;
+  __shared__ float acc4[4][D], ml[4][2];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t unit = blockIdx.x;
+  // rows that no workgroup had (more new tokens than the caller said) have anything here
+  const RowParts rp = reinterpret_cast<const RowParts*>(a.ws)[unit];
+  const int first = rp.first, parts = rp.parts64 >> 6, in_tile = rp.parts64 & 63;
+  if (parts <= 1 || first < 0 || in_tile >= plan.rows ||
+      int64_t(first) + int64_t(parts - 1) * c.heads >= plan.workgroups)
+    return;
+  const float* part = a.ws + plan.row_words + (int64_t(first) * plan.rows + in_tile) * (D + 4);
+  const int64_t stride = int64_t(c.heads) * plan.rows * (D + 4);
+  float acc[kPer], total = 0.f, top = kLow;
 #pragma unroll
   for (int i = 0; i < kPer; ++i) acc[i] = 0.f;
-  for (int s = 0; s < plan.splits; ++s) {
-    const float f = __builtin_amdgcn_exp2f(part[s * stride + D] - top);
-    total += part[s * stride + D + 1] * f;
+  for (int s0 = wave; s0 < parts; s0 += 4 * kAhead) {
+    float m[kAhead], l[kAhead], v[kAhead][kPer];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) acc[i] += part[s * stride + lane * kPer + i] * f;
+    for (int j = 0; j < kAhead; ++j) {
+      const float* p = part + int64_t(min(s0 + 4 * j, parts - 1)) * stride;
+      m[j] = p[D];
+      l[j] = p[D + 1];
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) v[j][i] = p[lane * kPer + i];
+    }
+    __builtin_amdgcn_sched_barrier(0);                        // all loads first
+    float mx = top;
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) mx = fmaxf(mx, s0 + 4 * j < parts ? m[j] : kLow);
+    const float old = __builtin_amdgcn_exp2f(top - mx);
+    total *= old;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) acc[i] *= old;
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const float f = s0 + 4 * j < parts ? __builtin_amdgcn_exp2f(m[j] - mx) : 0.f;
+      total += l[j] * f;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) acc[i] += v[j][i] * f;
+    }
+    top = mx;
   }
-  const float inv = total > 0.f ? 1.0f / total : (total == 0.f ? 0.f : total);
-  uint16_t* out = a.out + (t * a.q_heads + head * G + row % G) * D + lane * kPer;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) out[i] = uint16_t(pack_bf16x2(acc[i] * inv, 0.f));
+  for (int i = 0; i < kPer; ++i) acc4[wave][lane * kPer + i] = acc[i];
+  if (lane == 0) {
+    ml[wave][0] = top;
+    ml[wave][1] = total;
+  }
+  __syncthreads();
+  if (threadIdx.x >= D / 2) return;
+  const int d = 2 * threadIdx.x;
+  float mx = kLow, sum = 0.f, x0 = 0.f, x1 = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) mx = fmaxf(mx, ml[w][0]);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float f = __builtin_amdgcn_exp2f(ml[w][0] - mx);
+    sum += ml[w][1] * f;
+    x0 += acc4[w][d] * f;
+    x1 += acc4[w][d + 1] * f;
+  }
+  const float inv = sum > 0.f ? 1.0f / sum : sum == 0.f ? 0.f : sum;
+  *reinterpret_cast<uint32_t*>(a.out + unit * D + d) = pack_bf16x2(x0 * inv, x1 * inv);
 }
 
-template <int D, int R>
+template <int D, int R, int NW, int OCC>
 hipError_t launch(const Kv8Cache& c, const Kv8Batch& b, const Kv8Attend& a, const Kv8Plan& p, hipStream_t s) {
-  const int64_t tiles = int64_t(b.sequences) * c.heads * p.tiles;
-  MOE_LAUNCH("kv8_attention", (kv8_attention_kernel<D, R>), dim3(unsigned(tiles * p.splits)), dim3(64 * kAttWaves), s,
-             c, b, a, p);
+  const dim3 grid(unsigned(p.workgroups)), block(64 * kAttWaves);
+  if (c.page % (16 * NW) == 0)
+    MOE_LAUNCH("kv8_attention", (kv8_attention_kernel<D, R, NW, OCC, true>), grid, block, s, c, b, a, p);
+  else
+    MOE_LAUNCH("kv8_attention", (kv8_attention_kernel<D, R, NW, OCC, false>), grid, block, s, c, b, a, p);
   hipError_t err = hipGetLastError();
-  if (err != hipSuccess || p.splits == 1) return err;
-  MOE_LAUNCH("kv8_join", (kv8_join_kernel<D>), dim3(unsigned((tiles * p.rows + 3) / 4)), dim3(256), s, c, b, a, p);
+  if (err != hipSuccess || p.target == 0) return err;
+  MOE_LAUNCH("kv8_join", (kv8_join_kernel<D>), dim3(unsigned(b.tokens * a.q_heads)), dim3(256), s, c, b, a, p);
   return hipGetLastError();
 }
 
 template <int D>
 hipError_t launch_rows(const Kv8Cache& c, const Kv8Batch& b, const Kv8Attend& a, const Kv8Plan& p, hipStream_t s) {
-  if (p.rows == 16) return launch<D, 1>(c, b, a, p, s);
-  if constexpr (D <= 128) {
-    if (p.rows == 64) return launch<D, 4>(c, b, a, p, s);
-  }
-  return launch<D, 2>(c, b, a, p, s);
+  if (p.rows == 16) return launch<D, 1, D <= 128 ? 4 : 2, 2>(c, b, a, p, s);
+  return launch<D, 2, 2, D <= 128 ? 2 : 1>(c, b, a, p, s);
 }
 
 }  // namespace
 
-Kv8Plan kv8_plan(int sequences, int q_heads, int heads, int dim, int max_new, int max_len, int64_t window, int num_cu) {
-  Kv8Plan p;
+Kv8Plan kv8_plan(int sequences, int q_heads, int heads, int dim, int max_new, int max_len, int window, int num_cu) {
+  Kv8Plan p = {};
   const int64_t rows = int64_t(max_new) * (q_heads / heads);
-  p.rows = rows <= 16 ? 16 : rows <= 32 || dim > 128 ? 32 : 64;
+  p.rows = rows <= 16 ? 16 : 32;
   p.tiles = int((rows + p.rows - 1) / p.rows);
-  // two workgroups a compute unit, and at least one chunk for each wavefront
+  // four workgroups a compute unit; tiles are not cut where there are twice as many of them, nor
+  // where they are short
   const int64_t tiles = int64_t(sequences) * heads * p.tiles;
-  const int64_t seen = window > 0 ? std::min<int64_t>(max_len, window + max_new) : max_len;
-  const int64_t chunks = (seen + kChunk - 1) / kChunk;
-  const int64_t want = (2 * int64_t(num_cu) + tiles - 1) / std::max<int64_t>(tiles, 1);
-  p.splits = int(std::max<int64_t>(1, std::min(want, chunks / kAttWaves)));
+  const int64_t seen = window > 0 ? std::min<int64_t>(max_len, int64_t(window) + max_new) : max_len;
+  p.target = tiles >= 4 * int64_t(num_cu) || seen <= kMinChunks * kChunk ? 0 : 4 * num_cu;
   return p;
 }
 
-size_t kv8_workspace_bytes(const Kv8Plan& p, int sequences, int heads, int dim) {
-  if (p.splits <= 1) return 0;
-  return size_t(sequences) * heads * p.tiles * p.splits * p.rows * (dim + 4) * sizeof(float);
+// Parts are never more than the tiles and the target together: a part but the last of a tile holds a
+// quota of chunks, and `target` quotas hold them all.
+int64_t kv8_workgroups(const Kv8Plan& p, int sequences, int heads) {
+  return int64_t(sequences) * heads * p.tiles + p.target;
 }
 
-hipError_t launch_kv8_attention(const Kv8Cache& c, const Kv8Batch& b, const Kv8Attend& a, const Kv8Plan& p,
+// [a RowParts for each row | the parts]
+static int64_t row_words(int64_t tokens, int q_heads) { return (tokens * q_heads * 2 + 3) / 4 * 4; }
+
+size_t kv8_workspace_bytes(const Kv8Plan& p, int64_t tokens, int sequences, int q_heads, int heads, int dim) {
+  if (p.target == 0) return 0;
+  return (size_t(row_words(tokens, q_heads)) + size_t(kv8_workgroups(p, sequences, heads)) * p.rows * (dim + 4)) *
+         sizeof(float);
+}
+
+hipError_t launch_kv8_attention(const Kv8Cache& c, const Kv8Batch& b, const Kv8Attend& a, const Kv8Plan& plan,
                                 hipStream_t s) {
+  Kv8Plan p = plan;
+  const uint32_t per_page = uint32_t(c.page / kKvBlock);
+  p.inverse = per_page == 1 ? 0xFFFFFFFFu : uint32_t((uint64_t(1) << 32) / per_page);
+  p.row_words = row_words(b.tokens, a.q_heads);
+  p.workgroups = kv8_workgroups(p, b.sequences, c.heads);
+  p.capacity = int(std::min<int64_t>(int64_t(b.table_cols) * c.page, INT32_MAX));
   if (c.dim == 64) return launch_rows<64>(c, b, a, p, s);
   if (c.dim == 128) return launch_rows<128>(c, b, a, p, s);
   return launch_rows<256>(c, b, a, p, s);

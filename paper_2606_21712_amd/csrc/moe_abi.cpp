@@ -397,13 +397,14 @@ moe_status moe_kv8_append(const void* q, int64_t q_stride, const void* k, int64_
   return hip_status("moe_kv8_append", moe::launch_kv8_append(cache_of(*cache), b, a, stream_of(stream)));
 }
 
-size_t moe_kv8_attention_workspace_bytes(int32_t B, int32_t q_heads, int32_t heads, int32_t dim, int32_t max_new,
+size_t moe_kv8_attention_workspace_bytes(int64_t T, int32_t B, int32_t q_heads, int32_t heads, int32_t dim, int32_t max_new,
                                          int32_t max_len, int32_t window) {
-  if (!moe::kv8_plan_sizes_ok(B, q_heads, heads, dim, max_new, max_len, window)) return 0;
+  if (T < 1 || T >= (1 << 24) || !moe::kv8_plan_sizes_ok(B, q_heads, heads, dim, max_new, max_len, window)) return 0;
   hipError_t err;
   const int ncu = cu_count(&err);
   if (err != hipSuccess) return 0;
-  return moe::kv8_workspace_bytes(moe::kv8_plan(B, q_heads, heads, dim, max_new, max_len, window, ncu), B, heads, dim);
+  return moe::kv8_workspace_bytes(moe::kv8_plan(B, q_heads, heads, dim, max_new, max_len, window, ncu), T, B, q_heads,
+                                  heads, dim);
 }
 
 moe_status moe_kv8_attention(const void* q, int64_t T, int32_t q_heads, const moe_kv8_cache* cache,
@@ -418,10 +419,10 @@ moe_status moe_kv8_attention(const void* q, int64_t T, int32_t q_heads, const mo
     const int ncu = cu_count(&err);
     if (err != hipSuccess) return hip_status("moe_kv8_attention", err);
     plan = moe::kv8_plan(B, q_heads, cache->heads, cache->dim, max_new, max_len, window, ncu);
-    need = moe::kv8_workspace_bytes(plan, B, cache->heads, cache->dim);
+    need = moe::kv8_workspace_bytes(plan, T, B, q_heads, cache->heads, cache->dim);
   }
   moe::Check c = moe::validate_kv8_attention(q, T, q_heads, cache, block_table, table_cols, seq_lens, cu_tokens, B,
-                                             max_new, max_len, window, out, ws, ws_bytes, need);
+                                             max_new, max_len, window, scale, out, ws, ws_bytes, need);
   if (!c.ok() || T == 0) return finish(c);
   const moe::Kv8Batch b = {block_table, seq_lens, cu_tokens, B, table_cols, T};
   const moe::Kv8Attend a = {static_cast<const uint16_t*>(q), q_heads, max_new, max_len, window, scale,

@@ -159,13 +159,18 @@ struct Kv8Attend {
   uint16_t* out;
   float* ws;
 };
-// How an attention call is cut up: `rows` query rows (token, head of the group) a tile, `tiles`
-// tiles for the sequence with the most new tokens, each tile's tokens in `splits` parts.
+// How an attention call is cut up: `rows` query rows (token, head of the group) a tile, at most `tiles`
+// tiles of a sequence; `target`: workgroups to cut long tiles up for, 0: none is cut.
 struct Kv8Plan {
-  int rows, tiles, splits;
+  int rows, tiles, target;
+  int capacity;           // tokens that a row of the block table has place for
+  uint32_t inverse;       // 2^32 / blocks of a page, rounded down
+  int64_t workgroups;
+  int64_t row_words;      // of scratch before the parts
 };
-Kv8Plan kv8_plan(int sequences, int q_heads, int heads, int dim, int max_new, int max_len, int64_t window, int num_cu);
-size_t kv8_workspace_bytes(const Kv8Plan& p, int sequences, int heads, int dim);
+Kv8Plan kv8_plan(int sequences, int q_heads, int heads, int dim, int max_new, int max_len, int window, int num_cu);
+int64_t kv8_workgroups(const Kv8Plan& p, int sequences, int heads);
+size_t kv8_workspace_bytes(const Kv8Plan& p, int64_t tokens, int sequences, int q_heads, int heads, int dim);
 hipError_t launch_kv8_attention(const Kv8Cache& c, const Kv8Batch& b, const Kv8Attend& a, const Kv8Plan& p,
                                 hipStream_t s);
 

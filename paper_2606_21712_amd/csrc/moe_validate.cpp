@@ -629,14 +629,18 @@ bool kv8_plan_sizes_ok(int32_t B, int32_t q_heads, int32_t heads, int32_t dim, i
 
 Check validate_kv8_attention(const void* q, int64_t T, int32_t q_heads, const moe_kv8_cache* cache, const void* table,
                              int32_t table_cols, const void* lens, const void* cu, int32_t B, int32_t max_new,
-                             int32_t max_len, int32_t window, const void* out, const void* ws, size_t ws_bytes,
-                             size_t need) {
+                             int32_t max_len, int32_t window, float scale, const void* out, const void* ws,
+                             size_t ws_bytes, size_t need) {
   const char* fn = "moe_kv8_attention";
   if (cache == nullptr) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "cache is NULL");
   MOE_TRY(kv8_sizes(fn, T, q_heads, cache->heads, cache->dim, cache->page, cache->pages, table_cols, B));
   if (max_len < 0) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "max_len=%lld is negative", max_len);
   if (window < 0) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "window=%lld is negative", window);
+  if (!(scale > 0.f) || scale > 1e30f) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "scale must be positive and finite");
   if (T == 0) return Check{};
+  // one workgroup a row joins what long sequences are cut into
+  if (T * int64_t(q_heads) >= (int64_t(1) << 31))
+    return fail(MOE_ERR_UNSUPPORTED, fn, "T=%lld rows of q_heads=%lld are too many", T, q_heads);
   if (max_new < 1) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "max_new=%lld must be >= 1", max_new);
   if (!kv8_plan_sizes_ok(B, q_heads, cache->heads, cache->dim, max_new, max_len, window))
     return fail(MOE_ERR_UNSUPPORTED, fn, "max_new=%lld rows of B=%lld sequences are too many", max_new, B);

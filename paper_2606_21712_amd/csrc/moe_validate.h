@@ -92,8 +92,8 @@ Check validate_kv8_append(const void* q, int64_t q_stride, const void* k, int64_
                           int32_t table_cols, const void* lens, const void* cu, int32_t B, const void* q_out);
 Check validate_kv8_attention(const void* q, int64_t T, int32_t q_heads, const moe_kv8_cache* cache, const void* table,
                              int32_t table_cols, const void* lens, const void* cu, int32_t B, int32_t max_new,
-                             int32_t max_len, int32_t window, const void* out, const void* ws, size_t ws_bytes,
-                             size_t need);
+                             int32_t max_len, int32_t window, float scale, const void* out, const void* ws,
+                             size_t ws_bytes, size_t need);
 bool kv8_plan_sizes_ok(int32_t B, int32_t q_heads, int32_t heads, int32_t dim, int32_t max_new, int32_t max_len,
                        int32_t window);
 

@@ -335,7 +335,8 @@ def test_attention_splits(B, G):
 
 @pytest.mark.parametrize("D,new", [(64, 20), (128, 5), (256, 20)])
 def test_nan_reaches_those_who_see_it(D, new):
-    """A NaN in a new token's key or value: NaN for the rows that see the token, no change for others."""
+    """A NaN in a new token's key, or in one dimension of its value: NaN (at least there) for the rows that see
+    the token, no change for others."""
     log(f"[gpu] attention NaN D={D} new={new}")
     rng = np.random.default_rng(D)
     lens = [100]
@@ -355,7 +356,7 @@ def test_nan_reaches_those_who_see_it(D, new):
         out = moe.moe_kv8_attention(q, h2.device(), *args)
         seen = new // 2
         assert torch.equal(out[:seen], clean[:seen]), what
-        assert out[seen:].isnan().all(), what
+        assert (out[seen:].isnan() if what == "k" else out[seen:, :, 3].isnan()).all(), what
 
 
 def test_large_offsets():
