@@ -3,8 +3,15 @@
 //
 // One workgroup owns one block of 16 tokens of one kv head that receives new tokens: nothing
 // else writes there, so the block's exponent, the rescaling of what it holds and the new codes
-// need no atomics.  Thread t holds eight neighbouring dimensions of one token: the maximum
-// over the block's new tokens is one reduction, and each value is read once.
+// need no atomics.  One half of its threads has the keys, the other the values: a thread holds
+// 16 dimensions of one token, both halves of its rotation pairs among them, so every value is
+// read once and the block's largest is one reduction.  The same threads rotate the queries of
+// the block's tokens, for all of which their angles are read once.
+//
+// Bound by memory for prompts: 116 us for 23 thousand tokens of 32 query and 8 kv heads of 128
+// (524 MB, 4.5 TB/s; a large copy reaches 4.9).  Eight dimensions a thread, which reads every
+// pair twice and the angles for each head, took 145 us; one query head loaded at a time 136.  A
+// step's few tokens are bound by the launch and the chain lengths - page - rows: 7 us.
 #include "kv8.h"
 #include "mxfp8.h"
 
@@ -34,7 +41,7 @@ __device__ __forceinline__ u32x2 kv_codes(const float (&v)[8], int s) {
     const float x = v[i] * f;
     c[i] = x == x ? __builtin_amdgcn_fmed3f(x, -448.0f, 448.0f) : x;
   }
-  u32x2 r;
+  u32x2 r = {0u, 0u};
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     int w = __builtin_amdgcn_cvt_pk_fp8_f32(c[4 * i], c[4 * i + 1], 0, false);
@@ -53,74 +60,105 @@ __device__ __forceinline__ void kv_values(float (&v)[8], u32x2 c) {
   }
 }
 
-__device__ __forceinline__ void load8(float (&v)[8], const uint16_t* p) {
-  const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+// The two runs of eight dimensions that thread t of a token's D / 16 holds: the halves of pairs
+// (i, i + rot / 2) of the rotated dimensions and 16 neighbours beyond them, or 16 neighbours
+// everywhere where pairs are (2 i, 2 i + 1).  rot is a multiple of 16.  angle: the first of the
+// eight pairs' angles, or -1.
+struct Runs {
+  int a, b, angle;
+};
+template <bool INTERLEAVED>
+__device__ __forceinline__ Runs runs_of(int t, int rot) {
+  const int half = rot / 2;
+  if constexpr (INTERLEAVED) return {16 * t, 16 * t + 8, 16 * t < rot ? 8 * t : -1};
+  if (8 * t < half) return {8 * t, 8 * t + half, 8 * t};
+  return {16 * t, 16 * t + 8, -1};
+}
+
+struct Raw {                                                  // 16 bf16
+  u32x4 a, b;
+};
+__device__ __forceinline__ Raw load_runs(const uint16_t* row, const Runs& r) {   // read once: not kept in L2
+  return {__builtin_nontemporal_load(reinterpret_cast<const u32x4*>(row + r.a)),
+          __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(row + r.b))};
+}
+
+// Rotated values.  Products and sums are rounded one by one (no fused multiply-add), so that the
+// codes are those of the formula in fp32 whatever the compiler.
+template <bool INTERLEAVED>
+__device__ __forceinline__ void rotated(float (&v)[16], const Raw& w, const float (&cs)[16], bool rotates) {
+#pragma clang fp contract(off)
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    v[2 * i] = __uint_as_float(w[i] << 16);
-    v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    v[2 * i] = __uint_as_float(w.a[i] << 16);
+    v[2 * i + 1] = __uint_as_float(w.a[i] & 0xFFFF0000u);
+    v[8 + 2 * i] = __uint_as_float(w.b[i] << 16);
+    v[9 + 2 * i] = __uint_as_float(w.b[i] & 0xFFFF0000u);
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int p = INTERLEAVED ? 2 * i : i, q = INTERLEAVED ? 2 * i + 1 : 8 + i;
+    const float a = v[p], b = v[q];
+    const float ac = a * cs[i], bs = b * cs[8 + i], as = a * cs[8 + i], bc = b * cs[i];
+    const float x = ac - bs, y = as + bc;
+    v[p] = rotates ? x : a;
+    v[q] = rotates ? y : b;
   }
 }
 
-// Dimensions d .. d + 7 of a head's row, rotated: pairs are (i, i + rot / 2), or (2 i, 2 i + 1)
-// where interleaved.  Products and sums are rounded one by one (no fused multiply-add), so that
-// the codes are those of the formula in fp32 whatever the compiler.
-__device__ __forceinline__ void rotated8(float (&v)[8], const uint16_t* row, int d, const float* cs, int rot,
-                                         int interleaved) {
-#pragma clang fp contract(off)
-  load8(v, row + d);
-  if (d >= rot) return;
-  const int half = rot / 2;
-  if (interleaved) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float c = cs[d / 2 + i], s = cs[half + d / 2 + i];
-      const float a = v[2 * i], b = v[2 * i + 1];
-      const float ac = a * c, bs = b * s, as = a * s, bc = b * c;
-      v[2 * i] = ac - bs;
-      v[2 * i + 1] = as + bc;
-    }
-  } else {
-    const bool low = d < half;
-    float o[8];
-    load8(o, row + (low ? d + half : d - half));
-    const float* p = cs + (low ? d : d - half);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float c = p[i], s = p[half + i];
-      const float own = v[i] * c, other = o[i] * s;
-      v[i] = low ? own - other : other + own;
-    }
-  }
+template <int kFrom>
+__device__ __forceinline__ u32x4 pack8(const float (&v)[16]) {
+  return u32x4{pack_bf16x2(v[kFrom], v[kFrom + 1]), pack_bf16x2(v[kFrom + 2], v[kFrom + 3]),
+               pack_bf16x2(v[kFrom + 4], v[kFrom + 5]), pack_bf16x2(v[kFrom + 6], v[kFrom + 7])};
+}
+
+// Codes of eight values, and codes again of codes whose exponent grew by s.
+template <int kFrom>
+__device__ __forceinline__ u32x2 codes8(const float (&v)[16], int s) {
+  const float w[8] = {v[kFrom], v[kFrom + 1], v[kFrom + 2], v[kFrom + 3],
+                      v[kFrom + 4], v[kFrom + 5], v[kFrom + 6], v[kFrom + 7]};
+  return kv_codes(w, s);
+}
+__device__ __forceinline__ u32x2 rescaled(u32x2 c, int s) {
+  float v[8];
+  kv_values(v, c);
+  return kv_codes(v, s);
 }
 
 // Workgroup (slot, head).  Slots are handed out to sequences from their rows alone: sequence b
 // gets those from cu[b] / 16 + 2 b on, which are always enough for the blocks that it touches.
-template <int D>
+template <int D, bool INTERLEAVED>
 __global__ __launch_bounds__(2 * D) void kv8_append_kernel(Kv8Cache c, Kv8Batch b, Kv8Append a) {
-  constexpr int kPer = D / 8;                                 // threads of a token
-  constexpr int kWavesHere = 2 * D / 64;
-  __shared__ uint8_t vt[D][kKvBlock];
-  __shared__ float red[2][kWavesHere];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  constexpr int kPer = D / 16;                                // threads of a token
+  constexpr int kWaves = D / 64;                              // waves of a half
+  constexpr int kQ = 2;                                       // query heads loaded at once
+  __shared__ uint32_t vt[D][5];                               // a dimension's 16 tokens; 5: rows in different banks
+  __shared__ float red[2 * kWaves];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+  const int side = wave / kWaves;                             // 0 keys, 1 values
+  const int tid = threadIdx.x % D;
   const int slot = blockIdx.x, head = blockIdx.y;
   // the last sequence whose slots begin at or before this one
-  int before = 0;
+  int seq = -1, row0 = 0, stop = 0, len = 0;
   for (int s0 = 0; s0 < b.sequences; s0 += kWave) {
-    const int s = s0 + lane;
-    const uint64_t m = __ballot(s < b.sequences && b.cu[min(s, b.sequences - 1)] / kKvBlock + 2 * s <= slot);
-    before += __popcll(m);
+    const int s = min(s0 + lane, b.sequences - 1);
+    const int from = b.cu[s], to = b.cu[s + 1], n = b.lens[s];
+    const uint64_t m = __ballot(s0 + lane < b.sequences && from / kKvBlock + 2 * s <= slot);
+    if (m != 0) {
+      const int last = 63 - __builtin_clzll(m);
+      seq = s0 + last;
+      row0 = __builtin_amdgcn_readlane(from, last);
+      stop = __builtin_amdgcn_readlane(to, last);
+      len = __builtin_amdgcn_readlane(n, last);
+    }
     if (m != ~uint64_t(0)) break;
   }
-  const int seq = before - 1;
   if (seq < 0) return;
-  const int row0 = b.cu[seq], fresh = b.cu[seq + 1] - row0;
-  const int begin = b.lens[seq] - fresh;                      // position of the first new token
+  const int begin = len - (stop - row0);                      // position of the first new token
   const int first = max(begin, 0);                            // tokens before position 0 are not written
   const int blk = first / kKvBlock + (slot - (row0 / kKvBlock + 2 * seq));
-  const int p = blk * kKvBlock + tid / kPer;                  // this thread's token
-  const int d = tid % kPer * 8;
-  if (blk * kKvBlock >= begin + fresh) return;
+  const int p0 = blk * kKvBlock;                              // position of the block
+  if (p0 >= len) return;
   const int per_page = c.page / kKvBlock;
   const int column = blk / per_page;
   if (column >= b.table_cols) return;
@@ -128,99 +166,125 @@ __global__ __launch_bounds__(2 * D) void kv8_append_kernel(Kv8Cache c, Kv8Batch 
   if (page < 0 || page >= c.pages) return;
   const int64_t at = kv_block(page, head, blk % per_page, c.heads, per_page);
 
-  const int64_t row = int64_t(row0) + p - begin;
-  const bool is_new = p >= first && p < begin + fresh && row < b.tokens;
-  const bool is_old = p < first;                              // held before this call
-  const float* cs = a.cos_sin + min(int64_t(max(p, 0)), a.positions - 1) * a.rot;
-  float kv[8], vv[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) kv[i] = vv[i] = 0.f;
-  if (is_new) {
-    rotated8(kv, a.k + row * a.k_stride + int64_t(head) * D, d, cs, a.rot, a.interleaved);
-    load8(vv, a.v + row * a.v_stride + int64_t(head) * D + d);
-    const int G = a.q_heads / c.heads;
-    for (int j = 0; j < G; ++j) {
-      const int qh = head * G + j;
-      float q[8];
-      rotated8(q, a.q + row * a.q_stride + int64_t(qh) * D, d, cs, a.rot, a.interleaved);
-      *reinterpret_cast<u32x4*>(a.q_out + (row * a.q_heads + qh) * D + d) =
-          u32x4{pack_bf16x2(q[0], q[1]), pack_bf16x2(q[2], q[3]), pack_bf16x2(q[4], q[5]), pack_bf16x2(q[6], q[7])};
+  const int fresh0 = max(first - p0, 0), fresh1 = min(len - p0, kKvBlock);   // the new tokens' places in the block
+  const int place = tid / kPer;
+  const int64_t row = int64_t(row0) + p0 - begin + place;
+  const bool is_new = place >= fresh0 && place < fresh1 && row < b.tokens;
+  const Runs r = runs_of<INTERLEAVED>(tid % kPer, a.rot);
+  uint8_t* kc = c.k_codes + at * (kKvBlock * D) + place * D;
+  u32x4* vc = reinterpret_cast<u32x4*>(c.v_codes + at * (kKvBlock * D)) + tid;
+  uint8_t* exps = (side == 0 ? c.k_exps : c.v_exps) + at;
+  u32x4 old = {0u, 0u, 0u, 0u};                               // this token's codes; one dimension's of all 16 tokens
+  int old_e = -127;
+  if (fresh0 > 0) {                                           // the block holds earlier tokens
+    old_e = int(*exps) - 127;
+    if (side == 1) {
+      old = *vc;
+    } else if (place < fresh0) {
+      const u32x2 lo = *reinterpret_cast<const u32x2*>(kc + r.a), hi = *reinterpret_cast<const u32x2*>(kc + r.b);
+      old = u32x4{lo[0], lo[1], hi[0], hi[1]};
     }
   }
-  float mk = 0.f, mv = 0.f;                                   // fmaxf passes over NaN
+  float x[16];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    mk = fmaxf(mk, fabsf(kv[i]));
-    mv = fmaxf(mv, fabsf(vv[i]));
-  }
+  for (int i = 0; i < 16; ++i) x[i] = 0.f;
+  if (is_new) {
+    const int G = a.q_heads / c.heads;
+    const uint16_t* q = a.q + row * a.q_stride + int64_t(head) * G * D;
+    uint16_t* qo = a.q_out + (row * a.q_heads + int64_t(head) * G) * D;
+    Raw w[kQ];
 #pragma unroll
-  for (int s = 1; s < kWave; s <<= 1) {
-    mk = fmaxf(mk, __shfl_xor(mk, s));
-    mv = fmaxf(mv, __shfl_xor(mv, s));
-  }
-  if (lane == 0) {
-    red[0][wave] = mk;
-    red[1][wave] = mv;
-  }
-  __syncthreads();
+    for (int i = 0; i < kQ; ++i) w[i] = load_runs(q + min(side + 2 * i, G - 1) * D, r);
+    const Raw own = load_runs((side == 0 ? a.k + row * a.k_stride : a.v + row * a.v_stride) + int64_t(head) * D, r);
+    float cs[16];
 #pragma unroll
-  for (int w = 0; w < kWavesHere; ++w) {
-    mk = fmaxf(mk, red[0][w]);
-    mv = fmaxf(mv, red[1][w]);
-  }
-  int ek = kv_exponent(mk), ev = kv_exponent(mv);
-  uint8_t* kc = c.k_codes + at * (kKvBlock * D) + (tid / kPer) * D + d;
-  uint8_t* vc = c.v_codes + at * (kKvBlock * D);
-  u32x2 kout = {0u, 0u}, vout = {0u, 0u};
-  if (first > blk * kKvBlock) {                               // the block holds earlier tokens
-    const int ok = int(c.k_exps[at]) - 127, ov = int(c.v_exps[at]) - 127;
-    ek = max(ek, ok);
-    ev = max(ev, ov);
-    if (is_old) {
-      float o[8];
-      kout = *reinterpret_cast<const u32x2*>(kc);
-      if (ek != ok) {
-        kv_values(o, kout);
-        kout = kv_codes(o, ek - ok);
-      }
-      u32x2 w;
+    for (int i = 0; i < 16; ++i) cs[i] = 0.f;
+    const bool rotates = r.angle >= 0;
+    if (rotates) {
+      const float* p = a.cos_sin + min(int64_t(p0 + place), a.positions - 1) * a.rot + r.angle;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const uint32_t byte = vc[(d + i) * kKvBlock + tid / kPer];
-        w[i / 4] = (i % 4 ? w[i / 4] : 0u) | (byte << (8 * (i % 4)));
+        cs[i] = p[i];
+        cs[8 + i] = p[a.rot / 2 + i];
       }
-      vout = w;
-      if (ev != ov) {
-        kv_values(o, vout);
-        vout = kv_codes(o, ev - ov);
+    }
+    rotated<INTERLEAVED>(x, own, cs, rotates && side == 0);
+    for (int j = side; j < G; j += 2 * kQ) {
+      if (j != side) {
+#pragma unroll
+        for (int i = 0; i < kQ; ++i) w[i] = load_runs(q + min(j + 2 * i, G - 1) * D, r);
+      }
+#pragma unroll
+      for (int i = 0; i < kQ; ++i) {
+        if (j + 2 * i >= G) break;
+        float y[16];
+        rotated<INTERLEAVED>(y, w[i], cs, rotates);
+        *reinterpret_cast<u32x4*>(qo + (j + 2 * i) * D + r.a) = pack8<0>(y);
+        *reinterpret_cast<u32x4*>(qo + (j + 2 * i) * D + r.b) = pack8<8>(y);
       }
     }
   }
-  if (is_new) {
-    kout = kv_codes(kv, ek);
-    vout = kv_codes(vv, ev);
-  }
+
+  float m = 0.f;                                              // fmaxf passes over NaN
 #pragma unroll
-  for (int i = 0; i < 8; ++i) vt[d + i][tid / kPer] = uint8_t(vout[i / 4] >> (8 * (i % 4)));
-  __syncthreads();                                            // also: every old byte has been read
-  *reinterpret_cast<u32x2*>(kc) = kout;
-  if (tid < D) reinterpret_cast<u32x4*>(vc)[tid] = reinterpret_cast<const u32x4*>(&vt[tid][0])[0];
-  if (tid == 0) {
-    c.k_exps[at] = uint8_t(ek + 127);
-    c.v_exps[at] = uint8_t(ev + 127);
+  for (int i = 0; i < 16; ++i) m = fmaxf(m, fabsf(x[i]));
+#pragma unroll
+  for (int s = 1; s < kWave; s <<= 1) m = fmaxf(m, __shfl_xor(m, s));
+  if constexpr (kWaves > 1) {
+    if (lane == 0) red[wave] = m;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) m = fmaxf(m, red[side * kWaves + i]);
   }
+  const int e = fresh0 > 0 ? max(kv_exponent(m), old_e) : kv_exponent(m);
+  if (fresh0 > 0 && e != old_e) {
+    const u32x2 lo = rescaled(u32x2{old[0], old[1]}, e - old_e), hi = rescaled(u32x2{old[2], old[3]}, e - old_e);
+    old = u32x4{lo[0], lo[1], hi[0], hi[1]};
+  }
+  const u32x2 lo = codes8<0>(x, e), hi = codes8<8>(x, e);
+  if (side == 0) {
+    *reinterpret_cast<u32x2*>(kc + r.a) = is_new ? lo : u32x2{old[0], old[1]};
+    *reinterpret_cast<u32x2*>(kc + r.b) = is_new ? hi : u32x2{old[2], old[3]};
+  } else {
+    uint8_t* col = reinterpret_cast<uint8_t*>(vt) + place;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      col[(r.a + i) * 20] = uint8_t(lo[i / 4] >> (8 * (i % 4)));
+      col[(r.b + i) * 20] = uint8_t(hi[i / 4] >> (8 * (i % 4)));
+    }
+  }
+  if (tid == 0) *exps = uint8_t(e + 127);
+  __syncthreads();
+  if (side == 1) {                                            // earlier tokens, new ones, zeros
+    const auto below = [](int n) { return n <= 0 ? 0u : n >= 4 ? 0xFFFFFFFFu : (1u << (8 * n)) - 1u; };
+    u32x4 out;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t held = below(fresh0 - 4 * i), upto = below(fresh1 - 4 * i);
+      out[i] = (old[i] & held) | (vt[tid][i] & upto & ~held);
+    }
+    *vc = out;
+  }
+}
+
+template <int D>
+void launch(const Kv8Cache& c, const Kv8Batch& b, const Kv8Append& a, hipStream_t s) {
+  const dim3 grid(unsigned(b.tokens / kKvBlock + 2 * b.sequences), unsigned(c.heads));
+  if (a.interleaved)
+    MOE_LAUNCH("kv8_append", (kv8_append_kernel<D, true>), grid, dim3(2 * D), s, c, b, a);
+  else
+    MOE_LAUNCH("kv8_append", (kv8_append_kernel<D, false>), grid, dim3(2 * D), s, c, b, a);
 }
 
 }  // namespace
 
 hipError_t launch_kv8_append(const Kv8Cache& c, const Kv8Batch& b, const Kv8Append& a, hipStream_t s) {
-  const dim3 grid(unsigned(b.tokens / kKvBlock + 2 * b.sequences), unsigned(c.heads));
   if (c.dim == 64)
-    MOE_LAUNCH("kv8_append", (kv8_append_kernel<64>), grid, dim3(128), s, c, b, a);
+    launch<64>(c, b, a, s);
   else if (c.dim == 128)
-    MOE_LAUNCH("kv8_append", (kv8_append_kernel<128>), grid, dim3(256), s, c, b, a);
+    launch<128>(c, b, a, s);
   else
-    MOE_LAUNCH("kv8_append", (kv8_append_kernel<256>), grid, dim3(512), s, c, b, a);
+    launch<256>(c, b, a, s);
   return hipGetLastError();
 }
 
