@@ -154,8 +154,8 @@ def _ptr(t):
 
 
 def _stream(stream, device):
-    if stream is None:
-        stream = torch.cuda.current_stream(device)
+    if stream is None:   # the handle alone, 0.1 us: a Stream object takes 1.9
+        return torch._C._cuda_getCurrentRawStream(device.index)
     return stream.cuda_stream
 
 
@@ -174,6 +174,15 @@ def _dev(*ts):
                 raise ValueError("all tensors must be on the GPU")
             if not t.is_contiguous():
                 raise ValueError("all tensors must be contiguous")
+
+
+def _like(t, name, dtype, shape, device):
+    """A given buffer, looked over, or a new one."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if t.dtype != dtype or t.shape != shape:
+        raise ValueError(f"{name} must be {dtype} {shape}")
+    return t
 
 
 # --------------------------------------------------------------------------- the four calls
@@ -400,11 +409,22 @@ def moe_grouped_ffn_mxfp8_gather(x, sorted_token_ids, offsets, w_gate, w_up, w_d
 # --------------------------------------------------------------------------- 4-bit weights
 class Int4:
     """A packed 4-bit matrix, or a tensor [E, N, K] of such matrices (include/moe.h): codes and scales u8
-    in the library's tiled layout; zeros: whether there are zero points."""
+    in the library's tiled layout; zeros: whether there are zero points.  The tensors are looked over
+    here, once, and stay."""
 
     def __init__(self, codes, scales, zeros, shape, group):
         self.codes, self.scales, self.zeros = codes, scales, bool(zeros)
         self.shape, self.group = tuple(shape), group
+        *lead, N, K = self.shape
+        mats = 1
+        for n in lead:
+            mats *= n
+        if codes.dtype != torch.uint8 or scales.dtype != torch.uint8:
+            raise TypeError("packed codes and scales are u8")
+        if (codes.numel() < mats * moe_int4_code_bytes(N, K)
+                or scales.numel() < mats * moe_int4_scale_bytes(N, K, group, zeros)):
+            raise ValueError(f"codes or scales are too small for 4-bit weights {self.shape}, groups of {group}")
+        _dev(codes, scales)
 
 
 def moe_int4_code_bytes(rows, K) -> int:
@@ -467,11 +487,8 @@ def moe_matvec_int4(x, w, y=None, stream=None):
     if len(w.shape) != 2 or w.shape[1] != K:
         raise ValueError(f"w {w.shape} does not fit x [T, {K}]")
     N = w.shape[0]
-    if y is None:
-        y = torch.empty((T, N), dtype=torch.bfloat16, device=x.device)
-    elif y.dtype != torch.bfloat16 or tuple(y.shape) != (T, N):
-        raise ValueError(f"y must be bf16 [{T}, {N}]")
-    _dev(x, w.codes, y)
+    y = _like(y, "y", torch.bfloat16, (T, N), x.device)
+    _dev(x, y)
     _check(lib().moe_matvec_int4(_ptr(x), _ptr(w.codes), _ptr(w.scales), w.zeros, T, N, K, w.group, _ptr(y),
                                  _stream(stream, x.device)))
     return y
@@ -482,21 +499,47 @@ def moe_few_tokens_workspace_bytes(T, H, k, F, Fs=0) -> int:
     return lib().moe_few_tokens_workspace_bytes(T, H, k, F, Fs)
 
 
-def _few_weights(x, E, F, Fs, ws):
+_Int4Refs = _Int4Ref * 6
+
+
+def _few_weights(H, E, F, Fs, ws):
     """Checks the layer's three or six weights; whether they are 4-bit."""
-    H = x.shape[1]
-    want = [(E, F, H), (E, F, H), (E, H, F), (1, Fs, H), (1, Fs, H), (1, H, Fs)][:6 if Fs else 3]
-    if len(ws) < len(want) or any(w is None for w in ws[:len(want)]):
-        raise ValueError(f"{len(want)} weights are needed")
-    int4 = isinstance(ws[0], Int4)
-    for w, shape in zip(ws, want):
+    n = 6 if Fs else 3
+    first = ws[0]
+    int4 = isinstance(first, Int4)
+    for i in range(n):
+        w, e, f = ws[i], E if i < 3 else 1, F if i < 3 else Fs
+        if w is None:
+            raise ValueError(f"{n} weights are needed")
+        shape = (e, H, f) if i % 3 == 2 else (e, f, H)
         if isinstance(w, Int4) != int4 or (not int4 and w.dtype != torch.bfloat16):
             raise TypeError("weights are all bf16 or all Int4")
-        if tuple(w.shape) != shape and not (shape[0] == 1 and tuple(w.shape) == shape[1:]):
+        if w.shape != shape and not (e == 1 and w.shape == shape[1:]):
             raise ValueError(f"weights of shape {tuple(w.shape)}, {shape} expected")
-        if int4 and (w.group != ws[0].group or w.zeros != ws[0].zeros):
+        if int4 and (w.group != first.group or w.zeros != first.zeros):
             raise ValueError("4-bit weights of one layer share a group size, and have zero points or not")
     return int4
+
+
+def _few_tokens(x, logits, k, F, Fs, w, renormalize, topk_ids, topk_weights, y, ws, stream):
+    """The layer into buffers whose sizes are known to fit."""
+    T, H = x.shape
+    E = logits.shape[1]
+    if x.dtype != torch.bfloat16 or logits.dtype != torch.float32:
+        raise TypeError("moe_few_tokens takes bf16 x and f32 logits")
+    if logits.shape[0] != T:
+        raise ValueError("logits are [T, E]")
+    _dev(x, logits)
+    if _few_weights(H, E, F, Fs, w):
+        refs = _Int4Refs(*[(None, None) if t is None else (t.codes.data_ptr(), t.scales.data_ptr()) for t in w])
+        _check(lib().moe_few_tokens_int4(_ptr(x), _ptr(logits), T, H, E, k, F, Fs, renormalize, w[0].group, w[0].zeros,
+                                         refs, _ptr(topk_ids), _ptr(topk_weights), _ptr(y), _ptr(ws), ws.numel(),
+                                         _stream(stream, x.device)))
+    else:
+        _dev(*w)
+        _check(lib().moe_few_tokens(_ptr(x), _ptr(logits), T, H, E, k, F, Fs, renormalize, *[_ptr(t) for t in w],
+                                    _ptr(topk_ids), _ptr(topk_weights), _ptr(y), _ptr(ws), ws.numel(),
+                                    _stream(stream, x.device)))
 
 
 def moe_few_tokens(x, logits, k, w_gate, w_up, w_down, ws_gate=None, ws_up=None, ws_down=None, renormalize=1,
@@ -504,36 +547,17 @@ def moe_few_tokens(x, logits, k, w_gate, w_up, w_down, ws_gate=None, ws_up=None,
     """The whole layer for T <= 16 tokens: x bf16 [T, H], logits f32 [T, E], weights as MoELayer's, bf16
     or Int4 -> (y bf16 [T, H], topk_ids, topk_weights)."""
     T, H = x.shape
-    E = logits.shape[1]
     F = w_gate.shape[1]
     Fs = 0 if ws_gate is None else ws_gate.shape[-2]
     dev = x.device
-    if x.dtype != torch.bfloat16 or logits.dtype != torch.float32:
-        raise TypeError("moe_few_tokens takes bf16 x and f32 logits")
-    if logits.shape[0] != T:
-        raise ValueError("logits are [T, E]")
-    w = (w_gate, w_up, w_down, ws_gate, ws_up, ws_down)
-    int4 = _few_weights(x, E, F, Fs, w)
-    if topk_ids is None:
-        topk_ids = torch.empty((T, k), dtype=torch.int32, device=dev)
-    if topk_weights is None:
-        topk_weights = torch.empty((T, k), dtype=torch.float32, device=dev)
-    if y is None:
-        y = torch.empty((T, H), dtype=torch.bfloat16, device=dev)
+    topk_ids = _like(topk_ids, "topk_ids", torch.int32, (T, k), dev)
+    topk_weights = _like(topk_weights, "topk_weights", torch.float32, (T, k), dev)
+    y = _like(y, "y", torch.bfloat16, (T, H), dev)
     if ws is None:
         ws = torch.empty(max(1, moe_few_tokens_workspace_bytes(T, H, k, F, Fs)), dtype=torch.uint8, device=dev)
-    _dev(x, logits, topk_ids, topk_weights, y, ws)
-    if int4:
-        refs = (_Int4Ref * 6)(*[(_ptr(t.codes), _ptr(t.scales)) if t is not None else (None, None) for t in w])
-        _dev(*(t.codes for t in w if t is not None))
-        _check(lib().moe_few_tokens_int4(_ptr(x), _ptr(logits), T, H, E, k, F, Fs, renormalize, w_gate.group, w_gate.zeros, refs,
-                                         _ptr(topk_ids), _ptr(topk_weights), _ptr(y), _ptr(ws), ws.numel(),
-                                         _stream(stream, dev)))
-    else:
-        _dev(*w)
-        _check(lib().moe_few_tokens(_ptr(x), _ptr(logits), T, H, E, k, F, Fs, renormalize, *[_ptr(t) for t in w],
-                                    _ptr(topk_ids), _ptr(topk_weights), _ptr(y), _ptr(ws), ws.numel(),
-                                    _stream(stream, dev)))
+    _dev(topk_ids, topk_weights, y, ws)
+    _few_tokens(x, logits, k, F, Fs, (w_gate, w_up, w_down, ws_gate, ws_up, ws_down), renormalize, topk_ids,
+                topk_weights, y, ws, stream)
     return y, topk_ids, topk_weights
 
 
@@ -570,23 +594,24 @@ def _batch(block_table, seq_lens, cu_tokens):
     B, cols = block_table.shape
     if seq_lens.shape != (B,) or cu_tokens.shape != (B + 1,):
         raise ValueError("seq_lens is [B], cu_tokens [B + 1] for a block_table [B, columns]")
-    for t in (block_table, seq_lens, cu_tokens):
-        if t.dtype != torch.int32:
-            raise TypeError("block_table, seq_lens and cu_tokens are int32")
+    i32 = torch.int32
+    if block_table.dtype != i32 or seq_lens.dtype != i32 or cu_tokens.dtype != i32:
+        raise TypeError("block_table, seq_lens and cu_tokens are int32")
     return B, cols
 
 
-def _rows(t, name, heads, dim):
+def _rows(t, name, T, heads, dim):
     """Row stride of a tensor [T, heads, dim] whose rows are in one piece."""
     if t.dtype != torch.bfloat16:
         raise TypeError(f"{name} must be bf16")
-    if t.dim() != 3 or t.shape[1:] != (heads, dim):
-        raise ValueError(f"{name} must be [T, {heads}, {dim}]")
+    if t.shape != (T, heads, dim):
+        raise ValueError(f"{name} must be [{T}, {heads}, {dim}]")
     if not t.is_cuda:
         raise ValueError("all tensors must be on the GPU")
-    if t.shape[0] and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim)):
+    row, head, one = t.stride()
+    if T and (one != 1 or (heads > 1 and head != dim)):
         raise ValueError(f"{name}: the heads of a row must be in one piece")
-    return t.stride(0) if t.shape[0] > 1 else heads * dim
+    return row if T > 1 else heads * dim
 
 
 def moe_kv8_append(q, k, v, cos_sin, cache, block_table, seq_lens, cu_tokens, interleaved=False, q_out=None,
@@ -594,18 +619,13 @@ def moe_kv8_append(q, k, v, cos_sin, cache, block_table, seq_lens, cu_tokens, in
     """Rotates q [T, q_heads, dim] and k [T, heads, dim] by their positions and writes k and v into the
     cache -> rotated q.  cos_sin f32 [positions, rot]: cos, then sin, of rot / 2 angles.  Rows may be
     strided: slices of one projection's output."""
-    T, q_heads = q.shape[0], q.shape[1]
+    T, q_heads, _ = q.shape
     B, cols = _batch(block_table, seq_lens, cu_tokens)
     dim, heads = cache.dim, cache.heads
-    qs, ks, vs = _rows(q, "q", q_heads, dim), _rows(k, "k", heads, dim), _rows(v, "v", heads, dim)
-    if k.shape[0] != T or v.shape[0] != T:
-        raise ValueError("q, k and v have the same rows")
+    qs, ks, vs = _rows(q, "q", T, q_heads, dim), _rows(k, "k", T, heads, dim), _rows(v, "v", T, heads, dim)
     if cos_sin.dtype != torch.float32:
         raise TypeError("cos_sin must be float32")
-    if q_out is None:
-        q_out = torch.empty((T, q_heads, dim), dtype=torch.bfloat16, device=q.device)
-    elif q_out.dtype != torch.bfloat16 or tuple(q_out.shape) != (T, q_heads, dim):
-        raise ValueError(f"q_out must be bf16 [{T}, {q_heads}, {dim}]")
+    q_out = _like(q_out, "q_out", torch.bfloat16, (T, q_heads, dim), q.device)
     _dev(cos_sin, block_table, seq_lens, cu_tokens, q_out)
     _check(lib().moe_kv8_append(_ptr(q), qs, _ptr(k), ks, _ptr(v), vs, T, q_heads, _ptr(cos_sin), cos_sin.shape[0],
                                 cos_sin.shape[1], 1 if interleaved else 0, ctypes.byref(cache._ref), _ptr(block_table),
@@ -622,14 +642,11 @@ def moe_kv8_attention(q, cache, block_table, seq_lens, cu_tokens, max_new, max_l
                       ws=None, stream=None):
     """Causal attention of the rows q [T, q_heads, dim] over the cache -> out.  max_new: the most new rows of
     a sequence, max_len: the longest sequence; scale: 1 / sqrt(dim) unless given."""
-    T, q_heads = q.shape[0], q.shape[1]
+    T, q_heads, dim = q.shape
     B, cols = _batch(block_table, seq_lens, cu_tokens)
-    if q.dtype != torch.bfloat16 or q.shape[2] != cache.dim:
+    if q.dtype != torch.bfloat16 or dim != cache.dim:
         raise ValueError(f"q must be bf16 [T, q_heads, {cache.dim}]")
-    if out is None:
-        out = torch.empty_like(q)
-    elif out.dtype != torch.bfloat16 or out.shape != q.shape:
-        raise ValueError("out must be like q")
+    out = _like(out, "out", torch.bfloat16, (T, q_heads, dim), q.device)
     if ws is None:
         ws = torch.empty(max(1, moe_kv8_attention_workspace_bytes(T, B, q_heads, cache.heads, cache.dim, max_new, max_len,
                                                                   window)), dtype=torch.uint8, device=q.device)
@@ -840,12 +857,12 @@ class MoELayerFew:
 
     def run(self, x, logits, w_gate, w_up, w_down, ws_gate=None, ws_up=None, ws_down=None, renormalize=1, stream=None):
         n = x.shape[0]
-        if n > self.T or x.shape[1] != self.H or logits.shape[1] != self.E or w_gate.shape[1] != self.F:
+        if n > self.T or x.shape != (n, self.H) or logits.shape != (n, self.E):
             raise ValueError(f"x {tuple(x.shape)}, logits {tuple(logits.shape)}: not this layer's sizes")
-        if (0 if ws_gate is None else ws_gate.shape[-2]) != self.Fs:
+        if (ws_gate is not None) != (self.Fs > 0):
             raise ValueError(f"the shared expert must have Fs={self.Fs}")
         if self.y.shape[0] != n:
             self.topk_ids, self.topk_weights, self.y = self._ids[:n], self._weights[:n], self._y[:n]
-        moe_few_tokens(x, logits, self.k, w_gate, w_up, w_down, ws_gate, ws_up, ws_down, renormalize,
-                       topk_ids=self.topk_ids, topk_weights=self.topk_weights, y=self.y, ws=self.ws, stream=stream)
+        _few_tokens(x, logits, self.k, self.F, self.Fs, (w_gate, w_up, w_down, ws_gate, ws_up, ws_down), renormalize,
+                    self.topk_ids, self.topk_weights, self.y, self.ws, stream)
         return self.y
