@@ -176,13 +176,27 @@ void mv(const uint16_t* x, const Int4Ref& w, int T, int N, int K, uint16_t* y, h
 
 template <int GPT, bool ZEROS>
 hipError_t mv_group(const uint16_t* x, const Int4Ref& w, int T, int N, int K, uint16_t* y, int num_cu, hipStream_t s) {
-  const bool wide = int4_row_tiles(N) >= 4 * int64_t(num_cu);
-  if (T <= 16)
-    wide ? mv<4, 1, 8, GPT, ZEROS, 1>(x, w, T, N, K, y, s) : mv<1, 1, 8, GPT, ZEROS, 4>(x, w, T, N, K, y, s);
-  else if (T <= 32)
-    mv<1, 2, 8, GPT, ZEROS, 2>(x, w, T, N, K, y, s);
+  // Row tiles that share the rows of x, which pass through the caches for every step: as many as leave
+  // the compute units work.  us with 1, 2 and 4 of T x N x K: 1 x 4096 x 4096 6.2, 7.3, 9.3; 4 x 7168 x
+  // 2048 8.6, 6.3, 7.3; 12 x 8192 x 8192 20, 13.8, 19.4; 7 x 12550 x 9088 32, 20, 17; 18 x 4096 x 4096
+  // 9.7, 10.2, 11.6; 40 x 2261 x 4608 18.5, 14.3, 15.2; 32 x 28672 x 4096 60, 39, 25.  Rows past 32 are
+  // another workgroup's: 64 x 4096 x 14336 took 55 us with all rows in one, and takes 35 with two.
+  const int64_t units = int4_row_tiles(N) * ((T + 31) / 32);
+  const int nt = units >= 3 * num_cu ? 4 : units > num_cu ? 2 : 1;
+  if (T <= 16) {
+    if (nt == 4)
+      mv<4, 1, 8, GPT, ZEROS, 1>(x, w, T, N, K, y, s);
+    else if (nt == 2)
+      mv<2, 1, 8, GPT, ZEROS, 2>(x, w, T, N, K, y, s);
+    else
+      mv<1, 1, 8, GPT, ZEROS, 2>(x, w, T, N, K, y, s);
+  }
+  else if (nt == 4)
+    mv<4, 2, 8, GPT, ZEROS, 1>(x, w, T, N, K, y, s);
+  else if (nt == 2)
+    mv<2, 2, 8, GPT, ZEROS, 1>(x, w, T, N, K, y, s);
   else
-    mv<1, 4, 8, GPT, ZEROS, 1>(x, w, T, N, K, y, s);
+    mv<1, 2, 8, GPT, ZEROS, 2>(x, w, T, N, K, y, s);
   return hipGetLastError();
 }
 
