@@ -839,7 +839,7 @@ class MoELayerMXFP8:
 
 
 class MoELayerFew:
-    """The layer for up to T <= 16 tokens (FEW_TOKENS) in two kernels, with bf16 or 4-bit (Int4) weights:
+    """The layer for up to T <= 16 tokens (FEW_TOKENS) in two or three kernels, with bf16 or 4-bit (Int4) weights:
     what a batch's last few sequences run.  Buffers are made once; ``run`` takes any number of tokens
     up to T, allocates nothing and does not synchronize.  After it, ``y``, ``topk_ids`` and
     ``topk_weights`` are the step's (of as many rows as it had tokens)."""

@@ -1,4 +1,4 @@
-// The whole MoE layer for at most 16 tokens in two kernels (gfx950): the step of the few
+// The whole MoE layer for at most 16 tokens in two or three kernels (gfx950): the step of the few
 // sequences that a batch ends on.
 //
 // With so few tokens the layer is the read of the chosen experts' weights, each used for a
@@ -14,6 +14,9 @@
 //   few_down  16 columns of y for all tokens: the sum over all listed experts of Wd h, along one
 //             long k axis (expert after expert, the shared expert last), dealt to the
 //             wavefronts of the workgroup, whose sums are added in LDS in their order.
+//   few_join  where that axis is long and the columns are few, it is cut into parts of a workgroup
+//             each; their sums, in fp32, are added in the parts' order.  (A last workgroup that
+//             adds them behind a fence saves the launch, but the fences cost 42 -> 289 us.)
 //
 // h goes between the kernels as two bf16 numbers, the rounded value and the rounded rest (16
 // significant bits), so that y carries one rounding to bf16, its own.  Up to eight tokens the rest
@@ -413,20 +416,19 @@ __global__ __launch_bounds__(256) void few_join_kernel(const float* __restrict__
 }
 
 // Tiles of 16 rows that share a wavefront's activations (of each of gate and up in few_up), and
-// steps in flight: of weights and of activations.
+// steps in flight: of weights and of activations.  kCut: steps of a wavefront from which the k axis is
+// cut into parts.
 template <typename W>
 struct Shape;
 template <>
 struct Shape<Bf16Weights> {
   static constexpr int kUpTiles = 1, kUp = 2, kUpX = 2;
-  static constexpr int kDownTiles = 1, kDownWaves = 8, kDown = 2, kDownX = 2;
-  static constexpr bool kParts = false;
+  static constexpr int kDownTiles = 1, kDownWaves = 8, kDown = 2, kDownX = 2, kCut = 24;
 };
 template <int GPT, bool ZEROS>
 struct Shape<Int4Weights<GPT, ZEROS>> {
   static constexpr int kUpTiles = 2, kUp = 2, kUpX = 1;
-  static constexpr int kDownTiles = 4, kDownWaves = 8, kDown = 1, kDownX = 1;
-  static constexpr bool kParts = true;
+  static constexpr int kDownTiles = 4, kDownWaves = 8, kDown = 1, kDownX = 1, kCut = 8;
 };
 
 template <typename W, int C, int KS>
@@ -455,11 +457,15 @@ void down_c(const FewShape& s, const W (&w)[6], hipStream_t stream) {
   constexpr int kWaves = S::kDownWaves;
   static_assert(16 * NT <= kFewMaxCols, "workspace");
   const int groups = s.H / (16 * NT);
-  // two workgroups a compute unit, where every wavefront then still has two steps
+  // Where the columns do not give the compute units a workgroup each, the k axis is cut for two a unit
+  // with still two steps for every wavefront, if that saves more than few_join costs, some 4 us (bf16, H
+  // 1536, 8 tokens of 3 x F 11584: 251 us whole, 144 cut; H 2048, 1 token of 8 x F 1024: 17.2 and 14.8;
+  // 4 bits, H 1984, 3 tokens of 5 x F 512: 16.6 and 10.9).
   const int64_t steps = int64_t(std::min(s.T * s.k, s.E)) * ((s.F + W::kCols - 1) / W::kCols) +
                         (s.Fs + W::kCols - 1) / W::kCols;
   const int64_t want = std::min<int64_t>({(kFewParts + groups - 1) / groups, kFewMostParts, steps / (2 * kWaves)});
-  const int parts = S::kParts ? int(std::max<int64_t>(1, want)) : 1;
+  const bool cut = groups < s.num_cu * 3 / 4 && steps >= S::kCut * kWaves;
+  const int parts = cut ? int(std::max<int64_t>(1, want)) : 1;
   MOE_LAUNCH("few_down", (few_down_kernel<W, NT, kWaves, TS, FOLD, S::kDown, S::kDownX>),
              dim3(unsigned(groups * parts)), dim3(64 * kWaves), stream, s.h, s.ids, s.T, s.H, s.E, s.k, s.F, s.Fs,
              parts, w[2], w[5], s.partial, s.y);
