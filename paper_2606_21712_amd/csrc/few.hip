@@ -137,18 +137,20 @@ __device__ __forceinline__ int listed(const Chosen& ch) {
 }
 
 // ------------------------------------------------------------------ gate, up and SwiGLU
-// Unit u: 16 NU features of one listed expert (then of the shared one); KS wavefronts deal its k
-// steps among themselves, P steps of weights and PX of activations in flight.  C operands hold the
-// tokens' activations.  h: routed rows [T, k][2][F], then the shared expert's [T][2][Fs].
-template <typename W, int NU, int C, int KS, int V, int P, int PX>
+// Unit u: 16 NU features of one listed expert, or of the shared one after them.  Workgroups take units in
+// turn; the wavefronts of one deal a unit's k steps among themselves and add their sums in LDS, in their
+// order.  P steps of weights and PX of activations are in flight, across units too: those of the next
+// one load while a unit's sums are joined.  C operands hold the tokens' activations.  h: routed rows
+// [T, k][2][F], then the shared expert's [T][2][Fs].
+template <typename W, int NU, int C, int V, int P, int PX>
 __global__ __launch_bounds__(64 * kUpWaves, 4) void few_up_kernel(const uint16_t* __restrict__ x,
                                                                   const float* __restrict__ logits, int T, int H,
                                                                   int E, int k, int F, int Fs, int renorm, W wg, W wu,
                                                                   W sg, W su, int32_t* __restrict__ ids,
                                                                   float* __restrict__ wts, uint16_t* __restrict__ h) {
-  constexpr int kUnits = kUpWaves / KS, kAcc = W::kAcc, kSums = NU * 2 * C * kAcc;
+  constexpr int kAcc = W::kAcc, kSums = NU * 2 * C * kAcc;
   __shared__ Chosen ch;
-  __shared__ f32x4 part[KS > 1 ? kUpWaves : 1][kSums][64];
+  __shared__ f32x4 part[kUpWaves][kSums][64];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   clear_list(ch, T, E, k);
   __syncthreads();
@@ -162,61 +164,86 @@ __global__ __launch_bounds__(64 * kUpWaves, 4) void few_up_kernel(const uint16_t
   __syncthreads();
 
   const int n = listed(ch);
-  const int ks = wave % KS;
-  const int u = int(blockIdx.x) * kUnits + wave / KS;
   const int per = F / (16 * NU);               // units of an expert
-  const int a = u / per;
-  const bool shared = a >= n;
-  const int rt = shared ? u - n * per : u % per;
-  const bool on = !shared || rt < Fs / (16 * NU);
+  const int units = n * per + Fs / (16 * NU);
+  const int steps = (H + W::kCols - 1) / W::kCols;
+  const int mine = ((steps + kUpWaves - 1) / kUpWaves + P - 1) / P * P;   // a wavefront's steps of a unit
+  const auto bx = buffer_of(x, int64_t(T) * H * 2);
+
+  // A wavefront's place: step i of unit u.  Units start at different columns: their rows lie at equal
+  // distances, and the same column of all rows in flight would ask the same few memory channels.
+  struct Step {
+    int u, i, a, rt, turn;
+  };
+  auto enter = [&](Step& p) {
+    p.a = p.u / per;
+    if (p.a > n) p.a = n;
+    p.rt = p.u - p.a * per;
+    p.turn = p.u * 5 % steps;
+  };
+  auto advance = [&](Step& p) {
+    if (++p.i < mine) return false;
+    p.i = 0;
+    p.u += int(gridDim.x);
+    enter(p);
+    return true;
+  };
+  auto at = [&](const Step& p) {
+    const int s = wave + p.i * kUpWaves + p.turn;
+    return s >= steps ? s - steps : s;
+  };
+  auto on = [&](const Step& p) { return p.u < units && wave + p.i * kUpWaves < steps; };
+
+  typename W::View vg, vu;                     // of the unit that loads weights
+  auto view = [&](const Step& p) {
+    const bool shared = p.a >= n;
+    const int mat = shared ? 0 : __builtin_amdgcn_readfirstlane(ch.expert[p.a]);
+    const int64_t rows = shared ? Fs : F;
+    vg = W::pick(shared, sg, wg).view(mat, rows, H, lane);
+    vu = W::pick(shared, su, wu).view(mat, rows, H, lane);
+  };
+  int xat[C];                                  // of the unit that loads activations
+  auto rows_of = [&](const Step& p) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int t = c * W::kTok + W::token(lane);
+      const bool has = t < T && (p.a >= n || ch.slot[p.a][t] >= 0);
+      xat[c] = has ? t * H * 2 + W::x_at(lane) : kPast;
+    }
+  };
   f32x4 acc[NU][2][C][kAcc];                   // gate and up
   f32x4* flat = &acc[0][0][0][0];
+  typename W::Step wsg[P][NU], wsu[P][NU];
+  u32x4 xb[PX][C][W::kXRegs];
+  Step pw = {int(blockIdx.x), 0, 0, 0, 0}, px;
+  if (pw.u >= units) return;
+  enter(pw);
+  px = pw;
+  view(pw);
+  rows_of(px);
+  auto load_w = [&](int p) {
+    const int s = at(pw);
+    const bool o = on(pw);
 #pragma unroll
-  for (int q = 0; q < kSums; ++q) flat[q] = f32x4{0.f, 0.f, 0.f, 0.f};
-  int slot[C];
-#pragma unroll
-  for (int c = 0; c < C; ++c) {
-    const int t = c * W::kTok + W::token(lane);
-    slot[c] = !on || t >= T ? -1 : shared ? 0 : ch.slot[a][t];
-  }
-  if (on) {
-    const int mat = shared ? 0 : __builtin_amdgcn_readfirstlane(ch.expert[a]);
-    const int64_t rows = shared ? Fs : F;
-    const auto vg = W::pick(shared, sg, wg).view(mat, rows, H, lane);
-    const auto vu = W::pick(shared, su, wu).view(mat, rows, H, lane);
-    const auto bx = buffer_of(x, int64_t(T) * H * 2);
-    int xat[C];
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-      xat[c] = slot[c] >= 0 ? (c * W::kTok + W::token(lane)) * H * 2 + W::x_at(lane) : kPast;
-    const int steps = (H + W::kCols - 1) / W::kCols;
-    const int mine = (steps - ks + KS - 1) / KS;
-    // units start at different columns: their rows lie at equal distances, and the same column of
-    // all rows in flight would ask the same few memory channels
-    const int turn = u * 5 % steps;
-    auto place = [&](int i) {
-      const int s = ks + i * KS + turn;
-      return s >= steps ? s - steps : s;
-    };
-    typename W::Step wsg[P][NU], wsu[P][NU];
-    u32x4 xb[PX][C][W::kXRegs];
-    auto load_w = [&](int p, int i) {
-      const int s = place(i);
-#pragma unroll
-      for (int r = 0; r < NU; ++r) {
-        W::load(wsg[p][r], vg, rt * NU + r, s, i < mine);
-        W::load(wsu[p][r], vu, rt * NU + r, s, i < mine);
-      }
-    };
-    auto load_x = [&](int p, int i) {
-#pragma unroll
-      for (int c = 0; c < C; ++c) W::load_x(xb[p][c], bx, xat[c], place(i), H, i < mine);
-    };
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-      if (p < PX) load_x(p, p);
-      load_w(p, p);
+    for (int r = 0; r < NU; ++r) {
+      W::load(wsg[p][r], vg, pw.rt * NU + r, s, o);
+      W::load(wsu[p][r], vu, pw.rt * NU + r, s, o);
     }
+    if (advance(pw) && pw.u < units) view(pw);
+  };
+  auto load_x = [&](int p) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) W::load_x(xb[p][c], bx, xat[c], at(px), H, on(px));
+    if (advance(px) && px.u < units) rows_of(px);
+  };
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    if (p < PX) load_x(p);
+    load_w(p);
+  }
+  for (int u = int(blockIdx.x); u < units; u += int(gridDim.x)) {
+#pragma unroll
+    for (int q = 0; q < kSums; ++q) flat[q] = f32x4{0.f, 0.f, 0.f, 0.f};
     for (int i = 0; i < mine; i += P) {
 #pragma unroll
       for (int p = 0; p < P; ++p) {
@@ -227,40 +254,44 @@ __global__ __launch_bounds__(64 * kUpWaves, 4) void few_up_kernel(const uint16_t
           W::template add<C>(acc[r][0], wsg[p][r], xb[p % PX], sums);
           W::template add<C>(acc[r][1], wsu[p][r], xb[p % PX], sums);
         }
-        load_x(p % PX, i + p + PX);
-        load_w(p, i + p + P);
+        load_x(p % PX);
+        load_w(p);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
-  }
-  if (KS > 1) {
+    __syncthreads();                           // the last unit's sums have been read
 #pragma unroll
     for (int q = 0; q < kSums; ++q) part[wave][q][lane] = flat[q];
     __syncthreads();
-    if (ks != 0) return;
-#pragma unroll 1
-    for (int i = 1; i < KS; ++i)
+    const int a = min(u / per, n), rt = u - a * per;
+    const bool shared = a >= n;
+    const int width = shared ? Fs : F;
+    for (int o = wave; o < NU * C * kAcc; o += kUpWaves) {
+      const int i = o % kAcc, c = o / kAcc % C, r2 = o / kAcc / C;
+      const int qg = ((r2 * 2) * C + c) * kAcc + i, qu = qg + C * kAcc;
+      f32x4 g = part[0][qg][lane], up = part[0][qu][lane];
 #pragma unroll
-      for (int q = 0; q < kSums; ++q) flat[q] += part[wave + i][q][lane];
-  }
-  const int width = shared ? Fs : F;
+      for (int w = 1; w < kUpWaves; ++w) {
+        g += part[w][qg][lane];
+        up += part[w][qu][lane];
+      }
+      g = W::finish(g);
+      up = W::finish(up);
+      const int t = c * W::kTok + W::token(lane);
+      const int slot = t >= T ? -1 : shared ? 0 : ch.slot[a][t];
+      if (slot < 0 || !W::holds(lane)) continue;
+      const float w = shared ? 1.0f : ch.w[t][slot];
+      float v[4];
 #pragma unroll
-  for (int u2 = 0; u2 < NU * C * kAcc; ++u2) {
-    const int i = u2 % kAcc, c = u2 / kAcc % C, r2 = u2 / kAcc / C;
-    const f32x4 g = W::finish(acc[r2][0][c][i]), up = W::finish(acc[r2][1][c][i]);
-    if (slot[c] < 0 || !W::holds(lane)) continue;
-    const int t = c * W::kTok + W::token(lane);
-    const float w = shared ? 1.0f : ch.w[t][slot[c]];
-    float v[4];
+      for (int r = 0; r < 4; ++r) v[r] = w * silu(g[r]) * up[r];
+      uint16_t* out = h + (shared ? int64_t(T) * k * F * 2 + int64_t(t) * 2 * Fs : (int64_t(t) * k + slot) * 2 * F) +
+                      (rt * NU + r2) * 16 + W::row(i, lane);
+      const u32x2 hi = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+      *reinterpret_cast<u32x2*>(out) = hi;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) v[r] = w * silu(g[r]) * up[r];
-    uint16_t* out = h + (shared ? int64_t(T) * k * F * 2 + int64_t(t) * 2 * Fs : (int64_t(t) * k + slot[c]) * 2 * F) +
-                    (rt * NU + r2) * 16 + W::row(i, lane);
-    const u32x2 hi = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-    *reinterpret_cast<u32x2*>(out) = hi;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) v[r] -= __uint_as_float(r & 1 ? hi[r / 2] & 0xFFFF0000u : hi[r / 2] << 16);
-    *reinterpret_cast<u32x2*>(out + width) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+      for (int r = 0; r < 4; ++r) v[r] -= __uint_as_float(r & 1 ? hi[r / 2] & 0xFFFF0000u : hi[r / 2] << 16);
+      *reinterpret_cast<u32x2*>(out + width) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+    }
   }
 }
 
@@ -415,7 +446,9 @@ __global__ __launch_bounds__(256) void few_join_kernel(const float* __restrict__
   reinterpret_cast<u32x2*>(y)[i] = u32x2{pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3])};
 }
 
-// Tiles of 16 rows that share a wavefront's activations (of each of gate and up in few_up), and
+// Tiles of 16 rows that share a wavefront's activations (of each of gate and up in few_up), workgroups
+// of few_up for a compute unit (as many as stay there: one for each unit, in turn as places come free,
+// took 123 us for a bf16 layer of 64 experts of 2048 x 1024 and 16 tokens, 84 this way), and
 // steps in flight: of weights and of activations.  kCut: steps of a wavefront from which the k axis is
 // cut into parts.
 template <typename W>
@@ -427,28 +460,20 @@ struct Shape<Bf16Weights> {
 };
 template <int GPT, bool ZEROS>
 struct Shape<Int4Weights<GPT, ZEROS>> {
-  static constexpr int kUpTiles = 2, kUp = 2, kUpX = 1;
+  static constexpr int kUpTiles = 2, kUp = 1, kUpX = 1;
   static constexpr int kDownTiles = 4, kDownWaves = 8, kDown = 1, kDownX = 1, kCut = 8;
 };
 
-template <typename W, int C, int KS>
+template <typename W, int C>
 void up_c(const FewShape& s, const W (&w)[6], int64_t units, hipStream_t stream) {
   using S = Shape<W>;
-  const dim3 grid(unsigned((units * KS + kUpWaves - 1) / kUpWaves)), block(64 * kUpWaves);
+  const dim3 grid(unsigned(std::min<int64_t>(units, 2 * int64_t(s.num_cu)))), block(64 * kUpWaves);
   if (s.E <= 64)
-    MOE_LAUNCH("few_up", (few_up_kernel<W, S::kUpTiles, C, KS, 1, S::kUp, S::kUpX>), grid, block, stream, s.x, s.logits,
+    MOE_LAUNCH("few_up", (few_up_kernel<W, S::kUpTiles, C, 1, S::kUp, S::kUpX>), grid, block, stream, s.x, s.logits,
                s.T, s.H, s.E, s.k, s.F, s.Fs, s.renorm, w[0], w[1], w[3], w[4], s.ids, s.wts, s.h);
   else
-    MOE_LAUNCH("few_up", (few_up_kernel<W, S::kUpTiles, C, KS, 4, S::kUp, S::kUpX>), grid, block, stream, s.x, s.logits,
+    MOE_LAUNCH("few_up", (few_up_kernel<W, S::kUpTiles, C, 4, S::kUp, S::kUpX>), grid, block, stream, s.x, s.logits,
                s.T, s.H, s.E, s.k, s.F, s.Fs, s.renorm, w[0], w[1], w[3], w[4], s.ids, s.wts, s.h);
-}
-
-template <typename W, int KS>
-void up_ks(const FewShape& s, const W (&w)[6], int64_t units, hipStream_t stream) {
-  if constexpr (W::kTok < kFewT) {
-    if (s.T > W::kTok) return up_c<W, 2, KS>(s, w, units, stream);
-  }
-  up_c<W, 1, KS>(s, w, units, stream);
 }
 
 template <typename W, int NT, int TS, bool FOLD>
@@ -480,33 +505,28 @@ hipError_t launch(const FewShape& s, const W (&w)[6], hipStream_t stream) {
   // units of few_up at most: the experts that T tokens can choose, and the shared one
   constexpr int kRows = 16 * Shape<W>::kUpTiles;
   const int64_t units = int64_t(std::min(s.T * s.k, s.E)) * (s.F / kRows) + s.Fs / kRows;
-  if constexpr (W::kTok < kFewT) {
-    up_ks<W, 8>(s, w, units, stream);
-  } else {
-    const int64_t want = 12 * int64_t(s.num_cu);
-    if (units >= want)
-      up_ks<W, 1>(s, w, units, stream);
-    else if (2 * units >= want)
-      up_ks<W, 2>(s, w, units, stream);
-    else if (4 * units >= want)
-      up_ks<W, 4>(s, w, units, stream);
-    else
-      up_ks<W, 8>(s, w, units, stream);
-  }
+  if (s.T > W::kTok)
+    up_c<W, (kFewT > W::kTok ? 2 : 1)>(s, w, units, stream);
+  else
+    up_c<W, 1>(s, w, units, stream);
   hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
   constexpr bool kFold = W::kTok == kFewT;
   constexpr int kTiles = Shape<W>::kDownTiles;
+  if (s.T > 8) {
+    down_c<W, kTiles, kFewT / W::kTok, false>(s, w, stream);
+    return hipGetLastError();
+  }
   // bf16: two tiles share the rows of h where that still leaves three quarters of the compute units a
   // workgroup (DeepSeek shape, 8 tokens, H 7168: 216 us with one tile, 193 with two; Mixtral shape,
   // 1 token, H 4096: 38 and 61)
-  const bool wide = W::kTok < kFewT && s.H / 32 >= s.num_cu * 3 / 4;
-  if (s.T > 8)
-    down_c<W, kTiles, kFewT / W::kTok, false>(s, w, stream);
-  else if (wide)
-    down_c<W, 2, 1, kFold>(s, w, stream);
-  else
-    down_c<W, kTiles, 1, kFold>(s, w, stream);
+  if constexpr (W::kTok < kFewT) {
+    if (s.H / 32 >= s.num_cu * 3 / 4) {
+      down_c<W, 2, 1, kFold>(s, w, stream);
+      return hipGetLastError();
+    }
+  }
+  down_c<W, kTiles, 1, kFold>(s, w, stream);
   return hipGetLastError();
 }
 

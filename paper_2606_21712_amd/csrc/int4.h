@@ -66,7 +66,7 @@ struct Int4Weights {
     uint32_t s, z;
   };
   static __device__ __forceinline__ Int4Weights pick(bool first, const Int4Weights& a, const Int4Weights& b) {
-    return {first ? a.codes : b.codes, first ? a.scales : b.scales};
+    return {pick_of(first, a.codes, b.codes), pick_of(first, a.scales, b.scales)};
   }
   __device__ __forceinline__ View view(int mat, int64_t rows, int K, int lane) const {
     const int64_t tiles = int4_row_tiles(rows) * int4_col_tiles(K);

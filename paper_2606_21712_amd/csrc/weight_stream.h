@@ -54,6 +54,14 @@ __device__ __forceinline__ void keep(f32x4& v) {
   asm volatile("" : "+v"(v));
 }
 
+// One of two pointers.  By masks: a choice between kernel arguments becomes one between their addresses in
+// scratch memory, and what is loaded from there no longer counts as the same for all lanes.
+template <typename T>
+__device__ __forceinline__ const T* pick_of(bool first, const T* a, const T* b) {
+  const uint64_t m = first ? ~uint64_t(0) : 0;
+  return reinterpret_cast<const T*>((reinterpret_cast<uint64_t>(a) & m) | (reinterpret_cast<uint64_t>(b) & ~m));
+}
+
 // Row-major bf16 weights [rows, K], K % 64 == 0: a step is 16 rows x 64 columns, loaded as two times 8
 // rows x 128 bytes, whole cache lines.  The products have 16 rows, 32 columns along k and 16 columns
 // of activations; here row m of the first operand is weight row m % 8 in the k half m / 8, and
@@ -78,7 +86,7 @@ struct Bf16Weights {
     u32x4 a[2];
   };
   static __device__ __forceinline__ Bf16Weights pick(bool first, const Bf16Weights& a, const Bf16Weights& b) {
-    return {first ? a.w : b.w};
+    return {pick_of(first, a.w, b.w)};
   }
   static __device__ __forceinline__ int chunk(int lane) { return (lane >> 4) + ((lane & 8) >> 1); }
   __device__ __forceinline__ View view(int mat, int64_t rows, int K, int lane) const {
