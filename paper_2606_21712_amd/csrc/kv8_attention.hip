@@ -735,13 +735,29 @@ hipError_t launch_rows(const Kv8Cache& c, const Kv8Batch& b, const Kv8Attend& a,
 Kv8Plan kv8_plan(int sequences, int q_heads, int heads, int dim, int max_new, int max_len, int window, int num_cu) {
   Kv8Plan p = {};
   const int64_t rows = int64_t(max_new) * (q_heads / heads);
-  p.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 128;
-  p.tiles = int((rows + p.rows - 1) / p.rows);
-  // four workgroups a compute unit; tiles are not cut where there are half as many of them, nor
-  // where they are short
-  const int64_t tiles = int64_t(sequences) * heads * p.tiles;
   const int64_t seen = window > 0 ? std::min<int64_t>(max_len, int64_t(window) + max_new) : max_len;
-  p.target = tiles >= 2 * int64_t(num_cu) || seen <= kMinChunks * kChunk ? 0 : 4 * num_cu;
+  const auto tiles_of = [&](int of) { return int64_t(sequences) * heads * ((rows + of - 1) / of); };
+  const auto work = [&](int of) { return tiles_of(of) * ((seen + kChunk - 1) / kChunk); };
+  // Rows of a tile.  Large ones read a block for more rows, small ones give more workgroups and wait less
+  // for each step: small ones while all steps together are few.  us with 16, 32 and 128: 4 x 218 new tokens
+  // of 5 heads 10.8, 12.2, 18.3; 1 x 699 of 2 x 4 heads 21, 15.6, 20; 6 x 308 of 4 x 4 heads 29, 23, 20;
+  // 4 x 2000 of 8 x 4 heads 488, 308, 190.  Up to 64 rows a tile of 128 is mostly empty (8 x 9 tokens of
+  // 8 x 4 heads, 8000 long: 38 us with 32 rows, 52 with 128).
+  if (work(16) <= 8 * int64_t(num_cu))
+    p.rows = 16;
+  else if (rows > 16 && (rows <= 64 || work(32) <= 12 * int64_t(num_cu)))
+    p.rows = 32;
+  else
+    p.rows = rows <= 16 ? 16 : 128;
+  p.tiles = int((rows + p.rows - 1) / p.rows);
+  // Tiles are cut for so many workgroups a compute unit (32 rows, 4 x 6 tokens of 8 x 4 heads, 16000 long:
+  // 35 us with two, 42 with four; 16 rows, 8 sequences of 40000: 62 and 55), but not where there are
+  // enough of them, nor where they are so short that the join, some 5 us or more, costs what is gained
+  // (4 sequences of 8 x 4 heads of 128, uncut and cut with join: 1024 long 15 and 17 us, 1536 19 and
+  // 17; of 256: 768 long 20.6 and 19.4; tiles of 128 rows of 256, 749 long: 60 and 83).
+  const int64_t tiles = tiles_of(p.rows);
+  const int64_t uncut = (dim <= 128 || p.rows == 128 ? 2 : 1) * kMinChunks * kChunk;
+  p.target = tiles >= 2 * int64_t(num_cu) || seen <= uncut ? 0 : (p.rows == 32 ? 2 : 4) * num_cu;
   return p;
 }
 
