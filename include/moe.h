@@ -386,7 +386,7 @@ moe_status moe_pack_int4(const uint8_t* codes, const uint16_t* scales, const uin
  *   y       bf16 [T, N]   out
  *
  * Codes are multiplied as integers in bf16 (exact) on the matrix cores, sums of a group in
- * fp32, scaled and added up in fp32, rounded once.  The weights are read once for each 64
+ * fp32, scaled and added up in fp32, rounded once.  The weights are read once for each 32
  * rows of x: any T is right, few rows are what it is for.  x finite: an infinite x gives NaN.
  * Errors: INVALID_ARGUMENT for T < 0, N < 1, an unknown group, K not a positive multiple of
  * the group, null or misaligned pointers; UNSUPPORTED for T > 2^20, K > 2^23 or 2 GiB of
@@ -397,8 +397,9 @@ moe_status moe_matvec_int4(const void* x, const uint8_t* codes, const uint8_t* s
 
 /*
  * moe_few_tokens - the whole layer (moe_route, the expert FFNs, the shared expert,
- * moe_combine) for at most MOE_FEW_TOKENS tokens in two kernels: the step of the few
- * sequences that a batch ends on (the paper's long tail: at most 8 active sequences).
+ * moe_combine) for at most MOE_FEW_TOKENS tokens in two kernels, three where the sums of y are
+ * cut into parts: the step of the few sequences that a batch ends on (the paper's long tail: at
+ * most 8 active sequences).
  * Nothing is grouped: the layer's time is one read of the chosen experts' weights.
  *
  *   x               bf16 [T, H]    T <= 16
@@ -411,8 +412,9 @@ moe_status moe_matvec_int4(const void* x, const uint8_t* codes, const uint8_t* s
  *                   and the parts of y's sums; not to be shared by calls that overlap
  *
  * The gate weight multiplies silu(g) u in fp32; h is kept to 16 significant bits (two bf16
- * numbers), all sums are fp32, y is rounded once.  Deterministic; the order of y's sums depends on the experts that the
- * batch chose, so a token's y may differ in its last bit with the tokens beside it.
+ * numbers), all sums are fp32, y is rounded once.  Deterministic; the order of y's sums depends
+ * on the experts that the batch chose, so a token's y may differ in its last bit with the tokens
+ * beside it.
  * Errors: as moe_route and moe_grouped_ffn, plus INVALID_ARGUMENT for Fs < 0 or not a
  * multiple of 64; UNSUPPORTED for T > 16.
  *
@@ -456,7 +458,8 @@ moe_status moe_few_tokens_int4(const void* x, const float* logits, int64_t T, in
  * A sequence may have no rows.  Rows at positions below 0 (a slot of a captured graph whose
  * sequence has ended: seq_lens[b] = 0) are left out: nothing is appended for them, their
  * attention output is 0.  All of these are device arrays and are not checked beyond what
- * keeps the kernels inside their buffers: a page outside [0, pages) is not written.
+ * keeps the kernels inside their buffers: a page outside [0, pages) is not written, and read as
+ * the nearest inside; rows outside [0, T) are left out.
  */
 typedef struct {
     uint8_t* k_codes;
@@ -502,15 +505,20 @@ moe_status moe_kv8_append(const void* q, int64_t q_stride, const void* k, int64_
  *
  *   q           bf16 [T, q_heads, dim]   rotated queries; head h reads kv head h / (q_heads / heads)
  *   max_new     at least every sequence's row count: rows beyond it are not computed
- *   max_len     the longest sequence (for the plan only; any value gives right results)
+ *   max_len     the longest sequence (for the plan only; any value gives right results).  A loop
+ *               whose batches change may pass the largest max_new and max_len each time: the
+ *               workspace for these is then right for every step
  *   window      0, or how many tokens a row sees, itself included
  *   scale       factor of the scores, positive
  *   out         bf16 [T, q_heads, dim]   out
  *   ws, ws_bytes  device scratch of at least moe_kv8_attention_workspace_bytes() for the same sizes
  *
- * A row at position p sees tokens 0..p, with a window p - window + 1..p.  Scores, softmax and
- * sums are fp32, probabilities are rounded to bf16 for the product with the values.  A row that
- * sees nothing is 0.  Cache contents past a sequence's end are not used, whatever they are.
+ * A row at position p sees tokens 0..p, with a window p - window + 1..p.  The products of queries
+ * and keys are exact up to 2^-18 of a query row's largest element; scores, softmax and sums are
+ * fp32, probabilities are rounded to bf16 for the product with the values and for their sum.  A
+ * row that sees nothing is 0.  Cache contents past a sequence's end are not used, whatever they
+ * are, and neither are those outside a row's window.  A NaN that a row sees, in its query, a key or
+ * a value, shows as NaN in its output: of a value in that dimension, else in all.
  * Deterministic for a given plan (sizes, max_new, max_len, compute-unit budget).
  * Errors: as moe_kv8_append, plus INVALID_ARGUMENT for max_new < 1, max_len < 0, window < 0;
  * WORKSPACE_TOO_SMALL.

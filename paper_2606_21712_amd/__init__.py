@@ -521,15 +521,18 @@ def _few_weights(H, E, F, Fs, ws):
     return int4
 
 
-def _few_tokens(x, logits, k, F, Fs, w, renormalize, topk_ids, topk_weights, y, ws, stream):
-    """The layer into buffers whose sizes are known to fit."""
-    T, H = x.shape
-    E = logits.shape[1]
+def _few_inputs(x, logits):
     if x.dtype != torch.bfloat16 or logits.dtype != torch.float32:
         raise TypeError("moe_few_tokens takes bf16 x and f32 logits")
-    if logits.shape[0] != T:
+    if logits.shape[0] != x.shape[0]:
         raise ValueError("logits are [T, E]")
     _dev(x, logits)
+
+
+def _few_tokens(x, logits, k, F, Fs, w, renormalize, topk_ids, topk_weights, y, ws, stream):
+    """The layer of inputs that have been looked over, into buffers that are known to fit."""
+    T, H = x.shape
+    E = logits.shape[1]
     if _few_weights(H, E, F, Fs, w):
         refs = _Int4Refs(*[(None, None) if t is None else (t.codes.data_ptr(), t.scales.data_ptr()) for t in w])
         _check(lib().moe_few_tokens_int4(_ptr(x), _ptr(logits), T, H, E, k, F, Fs, renormalize, w[0].group, w[0].zeros,
@@ -546,6 +549,7 @@ def moe_few_tokens(x, logits, k, w_gate, w_up, w_down, ws_gate=None, ws_up=None,
                    topk_ids=None, topk_weights=None, y=None, ws=None, stream=None):
     """The whole layer for T <= 16 tokens: x bf16 [T, H], logits f32 [T, E], weights as MoELayer's, bf16
     or Int4 -> (y bf16 [T, H], topk_ids, topk_weights)."""
+    _few_inputs(x, logits)
     T, H = x.shape
     F = w_gate.shape[1]
     Fs = 0 if ws_gate is None else ws_gate.shape[-2]
@@ -857,6 +861,7 @@ class MoELayerFew:
 
     def run(self, x, logits, w_gate, w_up, w_down, ws_gate=None, ws_up=None, ws_down=None, renormalize=1, stream=None):
         n = x.shape[0]
+        _few_inputs(x, logits)
         if n > self.T or x.shape != (n, self.H) or logits.shape != (n, self.E):
             raise ValueError(f"x {tuple(x.shape)}, logits {tuple(logits.shape)}: not this layer's sizes")
         if (ws_gate is not None) != (self.Fs > 0):

@@ -169,7 +169,7 @@ __global__ __launch_bounds__(2 * D) void kv8_append_kernel(Kv8Cache c, Kv8Batch 
   const int fresh0 = max(first - p0, 0), fresh1 = min(len - p0, kKvBlock);   // the new tokens' places in the block
   const int place = tid / kPer;
   const int64_t row = int64_t(row0) + p0 - begin + place;
-  const bool is_new = place >= fresh0 && place < fresh1 && row < b.tokens;
+  const bool is_new = place >= fresh0 && place < fresh1 && uint64_t(row) < uint64_t(b.tokens);
   const Runs r = runs_of<INTERLEAVED>(tid % kPer, a.rot);
   uint8_t* kc = c.k_codes + at * (kKvBlock * D) + place * D;
   u32x4* vc = reinterpret_cast<u32x4*>(c.v_codes + at * (kKvBlock * D)) + tid;

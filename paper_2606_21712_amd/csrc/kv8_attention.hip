@@ -207,7 +207,7 @@ __global__ __launch_bounds__(64 * kAttWaves, OCC) void kv8_attention_kernel(Kv8C
     const int local = 16 * r + col;
     const int row = first_row + local;
     const int64_t t = int64_t(row0) + row / G;
-    const bool on = local < rows && t < b.tokens;
+    const bool on = local < rows && uint64_t(t) < uint64_t(b.tokens);
     pos[r] = on ? len - fresh + row / G : -1;
     const uint16_t* p = a.q + (t * a.q_heads + w.head * G + row % G) * D + 16 * g;
     u32x4 v[QW][2];
@@ -503,13 +503,20 @@ __global__ __launch_bounds__(64 * kAttWaves, OCC) void kv8_attention_kernel(Kv8C
     // kStages - 1 steps in flight.  A stage is filled again after the barrier that follows its last reads.
     // All loads but the newest fills being done means that the step's own fill is.
     constexpr int kAhead = kStages - 1, kFill = kPieces / kAttWaves;
+    static_assert(kAhead <= 2, "first fills");
     if (begin < end) {
       Place at[kAhead + 1];                                   // of the steps ch, ch + 1, ..
 #pragma unroll
       for (int i = 0; i <= kAhead; ++i) at[i] = look_up(min(begin + i, last));
       uint32_t ke1 = load_ke(at[0]), ve1 = load_ve(at[0]);
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) fill(at[i], i);
+      // in ring order: the waits below count on it
+      constexpr int st0 = 0, st1 = 1;
+      auto issue = [&](int to, int i) { fill(at[i], to); };
+      __builtin_amdgcn_sched_barrier(0);
+      issue(st0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (kAhead == 2) issue(st1, 1);
+      __builtin_amdgcn_sched_barrier(0);
       for (int ch = begin; ch < end; ++ch) {
         __builtin_amdgcn_s_waitcnt(wait_vm((kAhead - 1) * kFill) & ~0x0F00);   // and the LDS reads
         bare_barrier();
@@ -609,7 +616,7 @@ __global__ __launch_bounds__(64 * kAttWaves, OCC) void kv8_attention_kernel(Kv8C
     if (local >= rows) continue;
     const int row = first_row + local;
     const int64_t t = int64_t(row0) + row / G;
-    if (t >= b.tokens) continue;
+    if (uint64_t(t) >= uint64_t(b.tokens)) continue;
     if (w.parts == 1) {
       if (plan.target > 0 && g == 0)
         reinterpret_cast<RowParts*>(a.ws)[t * a.q_heads + w.head * G + row % G] = RowParts{0, 128};

@@ -411,21 +411,21 @@ moe_status moe_kv8_attention(const void* q, int64_t T, int32_t q_heads, const mo
                              const int32_t* block_table, int32_t table_cols, const int32_t* seq_lens,
                              const int32_t* cu_tokens, int32_t B, int32_t max_new, int32_t max_len, int32_t window,
                              float scale, void* out, void* ws, size_t ws_bytes, moe_stream stream) {
-  moe::Kv8Plan plan = {};
-  size_t need = 0;
-  if (T > 0 && cache != nullptr &&
-      moe::kv8_plan_sizes_ok(B, q_heads, cache->heads, cache->dim, max_new, max_len, window)) {
-    hipError_t err;
-    const int ncu = cu_count(&err);
-    if (err != hipSuccess) return hip_status("moe_kv8_attention", err);
-    plan = moe::kv8_plan(B, q_heads, cache->heads, cache->dim, max_new, max_len, window, ncu);
-    need = moe::kv8_workspace_bytes(plan, T, B, q_heads, cache->heads, cache->dim);
-  }
-  moe::Check c = moe::validate_kv8_attention(q, T, q_heads, cache, block_table, table_cols, seq_lens, cu_tokens, B,
-                                             max_new, max_len, window, scale, out, ws, ws_bytes, need);
+  // the workspace's size depends on the device's compute units: looked at once all else is right
+  const auto check = [&](size_t need) {
+    return moe::validate_kv8_attention(q, T, q_heads, cache, block_table, table_cols, seq_lens, cu_tokens, B, max_new,
+                                       max_len, window, scale, out, ws, ws_bytes, need);
+  };
+  moe::Check c = check(0);
   if (!c.ok() || T == 0) return finish(c);
+  hipError_t err;
+  const int ncu = cu_count(&err);
+  if (err != hipSuccess) return hip_status("moe_kv8_attention", err);
+  const moe::Kv8Plan plan = moe::kv8_plan(B, q_heads, cache->heads, cache->dim, max_new, max_len, window, ncu);
+  c = check(moe::kv8_workspace_bytes(plan, T, B, q_heads, cache->heads, cache->dim));
+  if (!c.ok()) return finish(c);
   const moe::Kv8Batch b = {block_table, seq_lens, cu_tokens, B, table_cols, T};
-  const moe::Kv8Attend a = {static_cast<const uint16_t*>(q), q_heads, max_new, max_len, window, scale,
+  const moe::Kv8Attend a = {static_cast<const uint16_t*>(q), q_heads, window, scale,
                             static_cast<uint16_t*>(out), static_cast<float*>(ws)};
   return hip_status("moe_kv8_attention", moe::launch_kv8_attention(cache_of(*cache), b, a, plan, stream_of(stream)));
 }

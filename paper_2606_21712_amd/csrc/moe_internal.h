@@ -153,7 +153,6 @@ hipError_t launch_kv8_append(const Kv8Cache& c, const Kv8Batch& b, const Kv8Appe
 struct Kv8Attend {
   const uint16_t* q;                      // [tokens, q_heads, dim]
   int q_heads;
-  int max_new, max_len;
   int window;                             // 0: none
   float scale;
   uint16_t* out;

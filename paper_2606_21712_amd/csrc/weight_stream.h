@@ -101,9 +101,8 @@ struct Bf16Weights {
   // A lane's row of activations, and where in it its operand begins (bytes).
   static __device__ __forceinline__ int token(int lane) { return lane & 7; }
   static __device__ __forceinline__ int x_at(int lane) { return 16 * chunk(lane); }
-  static __device__ __forceinline__ void load_x(u32x4 (&x)[kXRegs], const Buffer& b, int lane_at, int s, int K,
+  static __device__ __forceinline__ void load_x(u32x4 (&x)[kXRegs], const Buffer& b, int lane_at, int s, int,
                                                 bool on) {
-    (void)K;
     x[0] = load16<kCached>(b, on, lane_at, s * (kCols * 2));
   }
   template <int C>
