@@ -517,8 +517,8 @@ moe_status moe_kv8_append(const void* q, int64_t q_stride, const void* k, int64_
  * and keys are exact up to 2^-18 of a query row's largest element; scores, softmax and sums are
  * fp32, probabilities are rounded to bf16 for the product with the values and for their sum.  A
  * row that sees nothing is 0.  Cache contents past a sequence's end are not used, whatever they
- * are, and neither are those outside a row's window.  A NaN that a row sees, in its query, a key or
- * a value, shows as NaN in its output: of a value in that dimension, else in all.
+ * are, and neither are those outside a row's window.  A NaN that a row sees shows as NaN in its
+ * output: one in its query or a key in all dimensions, one in a value in that dimension at least.
  * Deterministic for a given plan (sizes, max_new, max_len, compute-unit budget).
  * Errors: as moe_kv8_append, plus INVALID_ARGUMENT for max_new < 1, max_len < 0, window < 0;
  * WORKSPACE_TOO_SMALL.

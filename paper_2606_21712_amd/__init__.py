@@ -169,11 +169,8 @@ def _dt(t: torch.Tensor) -> int:
 
 def _dev(*ts):
     for t in ts:
-        if t is not None:
-            if not t.is_cuda:
-                raise ValueError("all tensors must be on the GPU")
-            if not t.is_contiguous():
-                raise ValueError("all tensors must be contiguous")
+        if t is not None and not (t.is_cuda and t.is_contiguous()):
+            raise ValueError("all tensors must be " + ("contiguous" if t.is_cuda else "on the GPU"))
 
 
 def _like(t, name, dtype, shape, device):
@@ -489,8 +486,8 @@ def moe_matvec_int4(x, w, y=None, stream=None):
     N = w.shape[0]
     y = _like(y, "y", torch.bfloat16, (T, N), x.device)
     _dev(x, y)
-    _check(lib().moe_matvec_int4(_ptr(x), _ptr(w.codes), _ptr(w.scales), w.zeros, T, N, K, w.group, _ptr(y),
-                                 _stream(stream, x.device)))
+    _check(lib().moe_matvec_int4(x.data_ptr(), w.codes.data_ptr(), w.scales.data_ptr(), w.zeros, T, N, K, w.group,
+                                 y.data_ptr(), _stream(stream, x.device)))
     return y
 
 
@@ -583,7 +580,8 @@ class KVCache8:
         _dev(k_codes, v_codes, k_exps, v_exps)
         self.k_codes, self.v_codes, self.k_exps, self.v_exps = k_codes, v_codes, k_exps, v_exps
         self.pages, self.heads, self.page, self.dim = pages, heads, page, dim
-        self._ref = _Kv8Cache(_ptr(k_codes), _ptr(v_codes), _ptr(k_exps), _ptr(v_exps), pages, page, heads, dim)
+        self._ref = ctypes.byref(_Kv8Cache(_ptr(k_codes), _ptr(v_codes), _ptr(k_exps), _ptr(v_exps), pages, page, heads,
+                                           dim))
 
     @classmethod
     def empty(cls, pages, heads, dim, page=64, device="cuda"):
@@ -598,8 +596,7 @@ def _batch(block_table, seq_lens, cu_tokens):
     B, cols = block_table.shape
     if seq_lens.shape != (B,) or cu_tokens.shape != (B + 1,):
         raise ValueError("seq_lens is [B], cu_tokens [B + 1] for a block_table [B, columns]")
-    i32 = torch.int32
-    if block_table.dtype != i32 or seq_lens.dtype != i32 or cu_tokens.dtype != i32:
+    if not block_table.dtype == seq_lens.dtype == cu_tokens.dtype == torch.int32:
         raise TypeError("block_table, seq_lens and cu_tokens are int32")
     return B, cols
 
@@ -630,10 +627,12 @@ def moe_kv8_append(q, k, v, cos_sin, cache, block_table, seq_lens, cu_tokens, in
     if cos_sin.dtype != torch.float32:
         raise TypeError("cos_sin must be float32")
     q_out = _like(q_out, "q_out", torch.bfloat16, (T, q_heads, dim), q.device)
+    positions, rot = cos_sin.shape
     _dev(cos_sin, block_table, seq_lens, cu_tokens, q_out)
-    _check(lib().moe_kv8_append(_ptr(q), qs, _ptr(k), ks, _ptr(v), vs, T, q_heads, _ptr(cos_sin), cos_sin.shape[0],
-                                cos_sin.shape[1], 1 if interleaved else 0, ctypes.byref(cache._ref), _ptr(block_table),
-                                cols, _ptr(seq_lens), _ptr(cu_tokens), B, _ptr(q_out), _stream(stream, q.device)))
+    _check(lib().moe_kv8_append(q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, T, q_heads, cos_sin.data_ptr(),
+                                positions, rot, 1 if interleaved else 0, cache._ref, block_table.data_ptr(), cols,
+                                seq_lens.data_ptr(), cu_tokens.data_ptr(), B, q_out.data_ptr(),
+                                _stream(stream, q.device)))
     return q_out
 
 
@@ -655,9 +654,9 @@ def moe_kv8_attention(q, cache, block_table, seq_lens, cu_tokens, max_new, max_l
         ws = torch.empty(max(1, moe_kv8_attention_workspace_bytes(T, B, q_heads, cache.heads, cache.dim, max_new, max_len,
                                                                   window)), dtype=torch.uint8, device=q.device)
     _dev(q, block_table, seq_lens, cu_tokens, out, ws)
-    _check(lib().moe_kv8_attention(_ptr(q), T, q_heads, ctypes.byref(cache._ref), _ptr(block_table), cols,
-                                   _ptr(seq_lens), _ptr(cu_tokens), B, max_new, max_len, window,
-                                   cache.dim ** -0.5 if scale is None else scale, _ptr(out), _ptr(ws), ws.numel(),
+    _check(lib().moe_kv8_attention(q.data_ptr(), T, q_heads, cache._ref, block_table.data_ptr(), cols,
+                                   seq_lens.data_ptr(), cu_tokens.data_ptr(), B, max_new, max_len, window,
+                                   dim ** -0.5 if scale is None else scale, out.data_ptr(), ws.data_ptr(), ws.numel(),
                                    _stream(stream, q.device)))
     return out
 

@@ -757,14 +757,17 @@ Kv8Plan kv8_plan(int sequences, int q_heads, int heads, int dim, int max_new, in
   else
     p.rows = rows <= 16 ? 16 : 128;
   p.tiles = int((rows + p.rows - 1) / p.rows);
-  // Tiles are cut for so many workgroups a compute unit (32 rows, 4 x 6 tokens of 8 x 4 heads, 16000 long:
-  // 35 us with two, 42 with four; 16 rows, 8 sequences of 40000: 62 and 55), but not where there are
-  // enough of them, nor where they are so short that the join, some 5 us or more, costs what is gained
+  // Few tiles are cut so that all parts together are at most the two workgroups that a compute unit has
+  // place for at a time; more tiles, whose parts would then be of too few sizes, for four a unit (8
+  // heads: 1 sequence of 40000 22.9 us so, 27.5 with four a unit; 8 of up to 40000 52.4 and 55; 20 of 4000 27
+  // and 29; 4 heads, 50 of 4500 42 and 39).  They are not cut where there are enough of
+  // them, nor where they are so short that the join, some 5 us or more, costs what is gained
   // (4 sequences of 8 x 4 heads of 128, uncut and cut with join: 1024 long 15 and 17 us, 1536 19 and
   // 17; of 256: 768 long 20.6 and 19.4; tiles of 128 rows of 256, 749 long: 60 and 83).
   const int64_t tiles = tiles_of(p.rows);
   const int64_t uncut = (dim <= 128 || p.rows == 128 ? 2 : 1) * kMinChunks * kChunk;
-  p.target = tiles >= 2 * int64_t(num_cu) || seen <= uncut ? 0 : (p.rows == 32 ? 2 : 4) * num_cu;
+  if (tiles < 2 * int64_t(num_cu) && seen > uncut)
+    p.target = 3 * tiles <= 2 * int64_t(num_cu) ? 2 * num_cu - int(tiles) : (p.rows == 32 ? 2 : 4) * num_cu;
   return p;
 }
 
