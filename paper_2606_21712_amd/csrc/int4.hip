@@ -94,6 +94,11 @@ __global__ __launch_bounds__(64) void pack_int4_kernel(const uint8_t* __restrict
 // 16 C rows of x on the matrix cores: the weights are the A operand, expanded in registers, x the B
 // operand, read from the caches.  KS wavefronts deal the tiles along k among themselves and add
 // their sums in LDS, in their order; P steps of weights are in flight.
+//
+// Bound by the read of the weights where they are many: 8 x 28672 x 4096, 65 MB in 14.5 us of which
+// some 4 are launch and ramp (loads that stay in the caches: 62 MB took 19.4 us with streaming ones
+// against 19.0, 8 MB 6.8 against 6.2).  1 x 4096 x 4096 takes 5.1 us and 5 x 1003 x 7168 6.6: launch
+// and latency.  From 17 rows on x passes through the L2 more often than the weights do.
 template <int NT, int C, int KS, int GPT, bool ZEROS, int P>
 __global__ __launch_bounds__(64 * KS, 4) void matvec_int4_kernel(const uint16_t* __restrict__ x,
                                                                  Int4Weights<GPT, ZEROS, kCached> w, int T, int N, int K,

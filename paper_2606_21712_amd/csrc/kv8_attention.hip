@@ -29,6 +29,14 @@
 // batch's chunks and takes the quota that gives `target` workgroups; a tile that spans more is
 // cut into parts of equal length.  Parts write their sums, maxima and outputs to scratch, and
 // kv8_join adds them up, in order.
+//
+// One token a sequence is bound by the read of the cache: 8 sequences of up to 40000 tokens, 32 heads on
+// 8 of 128, 271 MB in 53.5 us (5.1 TB/s, the join's 4.6 us and some 6 us of each workgroup's start
+// and end included); 50 of up to 4500, 32 heads on 4 in pages of 16, 138 MB in 40 us.  Prompts are
+// bound by what a compute unit issues: 2048 new tokens of 10240 take 313 us, 980 TFLOP/s, vector
+// instructions 60% of the cycles, matrix cores 45%.  There the four wavefronts share what they read through
+// LDS, and the keys go into the products as they are: 421 us with neither, the load path and the
+// expansion the bounds.
 #include <algorithm>
 
 #include "kv8.h"
