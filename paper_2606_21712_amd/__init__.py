@@ -173,10 +173,19 @@ def _dev(*ts):
             raise ValueError("all tensors must be " + ("contiguous" if t.is_cuda else "on the GPU"))
 
 
-def _like(t, name, dtype, shape, device):
+def _new(shape, dtype, device, stream):
+    """A buffer of the stream that the call runs on: one of the current stream's could still be in use there, or
+    go to its next allocation while the call runs."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _like(t, name, dtype, shape, device, stream):
     """A given buffer, looked over, or a new one."""
     if t is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return _new(shape, dtype, device, stream)
     if t.dtype != dtype or t.shape != shape:
         raise ValueError(f"{name} must be {dtype} {shape}")
     return t
@@ -440,9 +449,9 @@ def moe_quantize_int4(w, group=128, zeros=False, stream=None):
     K = w.shape[-1]
     rows = w.numel() // K if K else 0
     dev = w.device
-    codes = torch.empty((*w.shape[:-1], K // 2), dtype=torch.uint8, device=dev)
-    scales = torch.empty((*w.shape[:-1], max(1, K // group)), dtype=torch.bfloat16, device=dev)
-    z = torch.empty(scales.shape, dtype=torch.uint8, device=dev) if zeros else None
+    codes = _new((*w.shape[:-1], K // 2), torch.uint8, dev, stream)
+    scales = _new((*w.shape[:-1], max(1, K // group)), torch.bfloat16, dev, stream)
+    z = _new(scales.shape, torch.uint8, dev, stream) if zeros else None
     _dev(w, codes, scales, z)
     _check(lib().moe_quantize_int4(_ptr(w), rows, K, group, _ptr(codes), _ptr(scales), _ptr(z), _stream(stream, dev)))
     return codes, scales, z
@@ -462,8 +471,8 @@ def moe_pack_int4(codes, scales, zeros=None, group=128, stream=None):
         mats *= n
     dev = codes.device
     z = zeros is not None
-    out = Int4(torch.empty(max(1, mats * moe_int4_code_bytes(N, K)), dtype=torch.uint8, device=dev),
-               torch.empty(max(1, mats * moe_int4_scale_bytes(N, K, group, z)), dtype=torch.uint8, device=dev), z,
+    out = Int4(_new(max(1, mats * moe_int4_code_bytes(N, K)), torch.uint8, dev, stream),
+               _new(max(1, mats * moe_int4_scale_bytes(N, K, group, z)), torch.uint8, dev, stream), z,
                (*lead, N, K), group)
     _dev(codes, scales, zeros, out.codes)
     _check(lib().moe_pack_int4(_ptr(codes), _ptr(scales), _ptr(zeros), mats, N, K, group, _ptr(out.codes),
@@ -484,7 +493,7 @@ def moe_matvec_int4(x, w, y=None, stream=None):
     if len(w.shape) != 2 or w.shape[1] != K:
         raise ValueError(f"w {w.shape} does not fit x [T, {K}]")
     N = w.shape[0]
-    y = _like(y, "y", torch.bfloat16, (T, N), x.device)
+    y = _like(y, "y", torch.bfloat16, (T, N), x.device, stream)
     _dev(x, y)
     _check(lib().moe_matvec_int4(x.data_ptr(), w.codes.data_ptr(), w.scales.data_ptr(), w.zeros, T, N, K, w.group,
                                  y.data_ptr(), _stream(stream, x.device)))
@@ -551,11 +560,11 @@ def moe_few_tokens(x, logits, k, w_gate, w_up, w_down, ws_gate=None, ws_up=None,
     F = w_gate.shape[1]
     Fs = 0 if ws_gate is None else ws_gate.shape[-2]
     dev = x.device
-    topk_ids = _like(topk_ids, "topk_ids", torch.int32, (T, k), dev)
-    topk_weights = _like(topk_weights, "topk_weights", torch.float32, (T, k), dev)
-    y = _like(y, "y", torch.bfloat16, (T, H), dev)
+    topk_ids = _like(topk_ids, "topk_ids", torch.int32, (T, k), dev, stream)
+    topk_weights = _like(topk_weights, "topk_weights", torch.float32, (T, k), dev, stream)
+    y = _like(y, "y", torch.bfloat16, (T, H), dev, stream)
     if ws is None:
-        ws = torch.empty(max(1, moe_few_tokens_workspace_bytes(T, H, k, F, Fs)), dtype=torch.uint8, device=dev)
+        ws = _new(max(1, moe_few_tokens_workspace_bytes(T, H, k, F, Fs)), torch.uint8, dev, stream)
     _dev(topk_ids, topk_weights, y, ws)
     _few_tokens(x, logits, k, F, Fs, (w_gate, w_up, w_down, ws_gate, ws_up, ws_down), renormalize, topk_ids,
                 topk_weights, y, ws, stream)
@@ -626,7 +635,7 @@ def moe_kv8_append(q, k, v, cos_sin, cache, block_table, seq_lens, cu_tokens, in
     qs, ks, vs = _rows(q, "q", T, q_heads, dim), _rows(k, "k", T, heads, dim), _rows(v, "v", T, heads, dim)
     if cos_sin.dtype != torch.float32:
         raise TypeError("cos_sin must be float32")
-    q_out = _like(q_out, "q_out", torch.bfloat16, (T, q_heads, dim), q.device)
+    q_out = _like(q_out, "q_out", torch.bfloat16, (T, q_heads, dim), q.device, stream)
     positions, rot = cos_sin.shape
     _dev(cos_sin, block_table, seq_lens, cu_tokens, q_out)
     _check(lib().moe_kv8_append(q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, T, q_heads, cos_sin.data_ptr(),
@@ -649,10 +658,10 @@ def moe_kv8_attention(q, cache, block_table, seq_lens, cu_tokens, max_new, max_l
     B, cols = _batch(block_table, seq_lens, cu_tokens)
     if q.dtype != torch.bfloat16 or dim != cache.dim:
         raise ValueError(f"q must be bf16 [T, q_heads, {cache.dim}]")
-    out = _like(out, "out", torch.bfloat16, (T, q_heads, dim), q.device)
+    out = _like(out, "out", torch.bfloat16, (T, q_heads, dim), q.device, stream)
     if ws is None:
-        ws = torch.empty(max(1, moe_kv8_attention_workspace_bytes(T, B, q_heads, cache.heads, cache.dim, max_new, max_len,
-                                                                  window)), dtype=torch.uint8, device=q.device)
+        ws = _new(max(1, moe_kv8_attention_workspace_bytes(T, B, q_heads, cache.heads, dim, max_new, max_len, window)),
+                  torch.uint8, q.device, stream)
     _dev(q, block_table, seq_lens, cu_tokens, out, ws)
     _check(lib().moe_kv8_attention(q.data_ptr(), T, q_heads, cache._ref, block_table.data_ptr(), cols,
                                    seq_lens.data_ptr(), cu_tokens.data_ptr(), B, max_new, max_len, window,

@@ -116,3 +116,43 @@ def test_rows_outside():
     assert codes[1, :2].any(1).all() and not codes[1, 2:].any()
     assert codes[2, 0].any() and not codes[2, 1:].any()
     assert (out != 7.0).any(-1).all()
+
+
+# ---------------------------------------------------------------- another stream than the current one
+@pytest.mark.parametrize("call", ["matvec", "few", "attention"])
+def test_buffers_of_the_call_s_stream(call):
+    """What a call on a given stream allocates is not memory that the current stream still reads."""
+    log(f"[gpu] buffers on another stream: {call}")
+    gen = torch.Generator(device="cuda").manual_seed(3)
+
+    def normal(*shape):
+        return torch.randn(shape, generator=gen, device="cuda").to(torch.bfloat16)
+
+    if call == "matvec":
+        x, w = normal(8, 256), moe.quantize_weights_int4(normal(2048, 256), 64)
+        size, run = 8 * 2048 * 2, lambda st: moe.moe_matvec_int4(x, w, stream=st)
+    elif call == "few":
+        x, logits, w = normal(8, 256), normal(8, 8).float(), (normal(8, 512, 256), normal(8, 512, 256), normal(8, 256, 512))
+        size = moe.moe_few_tokens_workspace_bytes(8, 256, 2, 512)
+        run = lambda st: moe.moe_few_tokens(x, logits, 2, *w, stream=st)[0]  # noqa: E731
+    else:
+        host, table = filled([3000, 2000], 1, 64, 64, np.random.default_rng(1))
+        cache, args = host.device(), (i32(table), i32([3000, 2000]), i32([0, 1, 2]), 1, 3000)
+        q = normal(2, 4, 64)
+        size = moe.moe_kv8_attention_workspace_bytes(2, 2, 4, 1, 64, 1, 3000)
+        run = lambda st: moe.moe_kv8_attention(q, cache, *args, stream=st)  # noqa: E731
+    assert size > 0
+    want = run(None).clone()
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    busy = torch.full((size,), 77, dtype=torch.uint8, device="cuda")
+    copy = torch.empty_like(busy)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(100_000_000)              # some 50 ms
+    copy.copy_(busy)
+    del busy                                    # its memory is the current stream's next block of this size
+    got = run(st)
+    torch.cuda.synchronize()
+    assert torch.equal(want, got)
+    assert (copy == 77).all()
