@@ -718,17 +718,20 @@ __global__ __launch_bounds__(256) void kv8_join_kernel(Kv8Cache c, Kv8Batch b, K
   *reinterpret_cast<uint32_t*>(a.out + unit * D + d) = pack_bf16x2(x0 * inv, x1 * inv);
 }
 
-template <int D, int R, int NW, int OCC, bool SHARED>
-hipError_t launch(const Kv8Cache& c, const Kv8Batch& b, const Kv8Attend& a, const Kv8Plan& p, hipStream_t s) {
+template <int D, int R, int NW, int OCC, bool SHARED, bool UNIFORM>
+hipError_t launch_as(const Kv8Cache& c, const Kv8Batch& b, const Kv8Attend& a, const Kv8Plan& p, hipStream_t s) {
   const dim3 grid(unsigned(p.workgroups)), block(64 * kAttWaves);
-  if (c.page % (16 * NW) == 0)
-    MOE_LAUNCH("kv8_attention", (kv8_attention_kernel<D, R, NW, OCC, SHARED, true>), grid, block, s, c, b, a, p);
-  else
-    MOE_LAUNCH("kv8_attention", (kv8_attention_kernel<D, R, NW, OCC, SHARED, false>), grid, block, s, c, b, a, p);
+  MOE_LAUNCH("kv8_attention", (kv8_attention_kernel<D, R, NW, OCC, SHARED, UNIFORM>), grid, block, s, c, b, a, p);
   hipError_t err = hipGetLastError();
   if (err != hipSuccess || p.target == 0) return err;
   MOE_LAUNCH("kv8_join", (kv8_join_kernel<D>), dim3(unsigned(b.tokens * a.q_heads)), dim3(256), s, c, b, a, p);
   return hipGetLastError();
+}
+
+template <int D, int R, int NW, int OCC, bool SHARED>
+hipError_t launch(const Kv8Cache& c, const Kv8Batch& b, const Kv8Attend& a, const Kv8Plan& p, hipStream_t s) {
+  if (c.page % (16 * NW) == 0) return launch_as<D, R, NW, OCC, SHARED, true>(c, b, a, p, s);
+  return launch_as<D, R, NW, OCC, SHARED, false>(c, b, a, p, s);
 }
 
 template <int D>
@@ -737,7 +740,7 @@ hipError_t launch_rows(const Kv8Cache& c, const Kv8Batch& b, const Kv8Attend& a,
     // pages that hold no whole step of 64 tokens are looked up lane by lane: shorter steps then (50
     // sequences of up to 4500 tokens, pages of 16: 42 us with 64 tokens, 39 with 32)
     if constexpr (D <= 128) {
-      if (c.page % 64 == 0) return launch<D, 1, 4, 2, false>(c, b, a, p, s);
+      if (c.page % 64 == 0) return launch_as<D, 1, 4, 2, false, true>(c, b, a, p, s);
     }
     return launch<D, 1, 2, 2, false>(c, b, a, p, s);
   }
