@@ -763,7 +763,8 @@ class LayerGraph:
 
     The graph holds the device addresses of the tensors given at capture and of the
     layer's own buffers: to run it on new data, copy the data into those tensors in
-    place.  The library's calls neither allocate nor synchronize, and nothing in a
+    place.  ``y``, ``topk_ids`` and ``topk_weights`` are the captured step's outputs, rows of the
+    layer's buffers, which its other runs and graphs write too.  The library's calls neither allocate nor synchronize, and nothing in a
     layer step clears memory with a memset (the tile counters are zeroed by a kernel),
     so the whole step captures.  A first eager run on a side stream (of default
     priority) does the library's one-time set-up outside the capture."""
@@ -782,11 +783,13 @@ class LayerGraph:
         torch.cuda.current_stream().wait_stream(side)
         with torch.cuda.graph(self.graph):
             layer.run(*args, **kwargs)
+        # of this step's rows: a MoELayerFew may run, and be captured, with other numbers of tokens
+        self.y, self.topk_ids, self.topk_weights = layer.y, layer.topk_ids, layer.topk_weights
 
     def replay(self):
-        """Run the captured step on the current stream; returns the layer's y."""
+        """Run the captured step on the current stream; returns its y."""
         self.graph.replay()
-        return self.layer.y
+        return self.y
 
 
 class MoELayerMXFP8:
