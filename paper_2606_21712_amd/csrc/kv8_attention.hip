@@ -40,6 +40,7 @@
 #include <algorithm>
 
 #include "kv8.h"
+#include "kv8_cut.h"
 #include "lds_stage.h"
 #include "mxfp8.h"
 
@@ -47,7 +48,6 @@ namespace moe {
 namespace {
 
 constexpr int kAttWaves = 4;
-constexpr int kChunk = 64;                    // tokens: the unit in which work is dealt
 constexpr int kMinChunks = 2 * kAttWaves;     // of a part: a tile is not cut below this
 constexpr float kSlack = 8.0f;
 constexpr float kLow = -1e30f;                // below every score: the maximum before any token
@@ -198,14 +198,12 @@ __global__ __launch_bounds__(64 * kAttWaves, OCC) void kv8_attention_kernel(Kv8C
   const int in_tile = SHARED ? wave * 16 * R : 0;
   const int first_row = w.tile * (SHARED ? kAttWaves * 16 * R : 16 * R) + in_tile;
   const int rows = min(16 * R, int(min(int64_t(fresh) * G, int64_t(1) << 30)) - first_row);
-  // positions of the first and the last row, and the chunks that the tile's rows see: this part's share
+  // positions of the first and the last row, of the wavefront's and of the tile's
   const int first_pos = len - fresh + first_row / G, last_pos = len - fresh + (first_row + rows - 1) / G;
   const int tile_row = w.tile * plan.rows, tile_rows = min(plan.rows, int(min(int64_t(fresh) * G, int64_t(1) << 30)) - tile_row);
   const int tile_first = len - fresh + tile_row / G, tile_last = len - fresh + (tile_row + tile_rows - 1) / G;
-  const int low = a.window > 0 ? max(tile_first - a.window + 1, 0) : 0;
-  const int c0 = low / kChunk, c1 = tile_last < 0 ? c0 : max(tile_last / kChunk + 1, c0);
-  const int each = (max(c1 - c0, 0) + w.parts - 1) / w.parts;
-  const int begin = min(c0 + w.part * each, c1) * (kChunk / kTok), end = min(c0 + (w.part + 1) * each, c1) * (kChunk / kTok);
+  const Kv8Steps steps = kv8_steps(tile_first, tile_last, a.window, w.part, w.parts, kTok);
+  const int begin = steps.begin, end = steps.end;
 
   // queries: row r is token r / G, head r % G of the group
   int pos[R];                                 // position of the column's token; -1: sees nothing
