@@ -455,11 +455,11 @@ moe_status moe_few_tokens_int4(const void* x, const float* logits, int64_t T, in
  *   cu_tokens    i32 [B + 1] rows of the new tokens: sequence b has rows cu[b] .. cu[b + 1] - 1,
  *                at positions seq_lens[b] - n_b .. seq_lens[b] - 1 (n_b its row count)
  *   T            rows, cu_tokens[B]
- * A sequence may have no rows.  Rows at positions below 0 (a slot of a captured graph whose
- * sequence has ended: seq_lens[b] = 0) are left out: nothing is appended for them, their
- * attention output is 0.  All of these are device arrays and are not checked beyond what
- * keeps the kernels inside their buffers: a page outside [0, pages) is not written, and read as
- * the nearest inside; rows outside [0, T) are left out.
+ * A sequence may have no rows: its pages are neither read nor written.  Rows at positions
+ * below 0 (a slot of a captured graph whose sequence has ended: seq_lens[b] = 0) are left out:
+ * nothing is appended for them, their attention output is 0.  All of these are device arrays
+ * and are not checked beyond what keeps the kernels inside their buffers: a page outside
+ * [0, pages) is not written, and read as the nearest inside; rows outside [0, T) are left out.
  */
 typedef struct {
     uint8_t* k_codes;

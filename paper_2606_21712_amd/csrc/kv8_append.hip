@@ -153,7 +153,7 @@ __global__ __launch_bounds__(2 * D) void kv8_append_kernel(Kv8Cache c, Kv8Batch 
     }
     if (m != ~uint64_t(0)) break;
   }
-  if (seq < 0) return;
+  if (seq < 0 || stop <= row0) return;                        // a sequence without rows is left as it is
   const int begin = len - (stop - row0);                      // position of the first new token
   const int first = max(begin, 0);                            // tokens before position 0 are not written
   const int blk = first / kKvBlock + (slot - (row0 / kKvBlock + 2 * seq));

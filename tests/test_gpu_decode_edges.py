@@ -45,3 +45,36 @@ def test_graphs_of_several_sizes():
         torch.cuda.synchronize()
         assert torch.equal(y, want), i
         assert torch.equal(graphs[g].topk_ids, ids) and torch.equal(graphs[g].topk_weights, wts), i
+
+
+# ---------------------------------------------------------------- sequences that bring no rows
+def test_append_without_rows():
+    """A sequence with no new rows is left as it is, what lies past its end too; one whose page another sequence
+    appends to in the same call does not touch it."""
+    log("[gpu] append without rows")
+    rng = np.random.default_rng(8)
+    Hkv, page, D = 2, 16, 128
+    host = HostCache(5, Hkv, page, D)
+    host.k[:], host.v[:] = (rng.integers(0, 0x7E, t.shape) for t in (host.k, host.v))
+    host.ke[:], host.ve[:] = 120, 121
+    cs = angles(64, D)
+
+    def append(table, lens, new):
+        x = torch.from_numpy(rng.standard_normal((sum(new), 3 * Hkv, D)).astype(np.float32)).to(torch.bfloat16)
+        dev = host.device()
+        cu = np.concatenate([[0], np.cumsum(new)])
+        g = x.cuda()
+        moe.moe_kv8_append(g[:, :Hkv], g[:, Hkv:2 * Hkv], g[:, 2 * Hkv:], torch.from_numpy(cs).cuda(), dev, i32(table),
+                           i32(lens), i32(cu))
+        torch.cuda.synchronize()
+        f = x.float().numpy()
+        for b, n in enumerate(new):
+            if n:
+                rows = slice(cu[b], cu[b + 1])
+                first = lens[b] - n
+                host.append(rotate(f[rows, Hkv:2 * Hkv], np.arange(first, lens[b]), cs, False), f[rows, 2 * Hkv:],
+                            table[b], first, n)
+        assert host.same(dev)
+
+    append([[0, 1], [2, 3]], [21, 13], [0, 3])          # codes lie past the first one's 21 tokens
+    append([[2, 3], [2, 3], [2, 3]], [7, 19, 30], [0, 19, 0])   # the page is now the second one's
