@@ -519,6 +519,9 @@ moe_status moe_kv8_append(const void* q, int64_t q_stride, const void* k, int64_
  * row that sees nothing is 0.  Cache contents past a sequence's end are not used, whatever they
  * are, and neither are those outside a row's window.  A NaN that a row sees shows as NaN in its
  * output: one in its query or a key in all dimensions, one in a value in that dimension at least.
+ * So does a value of 2^128 or more, which bf16 does not hold (what an infinity was appended as):
+ * infinity or NaN.  Values are summed in fp32, weighted by up to 2^8, and then divided by the
+ * weights' sum: those under 2^100 do not overflow there.
  * Deterministic for a given plan (sizes, max_new, max_len, compute-unit budget).
  * Errors: as moe_kv8_append, plus INVALID_ARGUMENT for max_new < 1, max_len < 0, window < 0;
  * WORKSPACE_TOO_SMALL.

@@ -422,24 +422,30 @@ __global__ __launch_bounds__(64 * kAttWaves, OCC) void kv8_attention_kernel(Kv8C
       }
     }
   };
-  // In a step that some row does not see in full: codes of values past the end are anything, NaN too,
-  // and so may be those of a token that a row must not see, and 0 NaN is NaN.  Such codes are taken
-  // out, and the rows that do see their token get a NaN score instead.
-  auto clean = [&](uint32_t x, uint32_t keep, uint32_t& nan) {
+  // In a step that some row does not see in full: values are anything, NaN or infinite too, where no row
+  // sees their token, and where some row must not, and 0 times these is NaN.  What no row of the wavefront sees
+  // is taken out, codes and, for a whole block, its exponent.  Of the rest, codes of NaN and of what
+  // bf16 has no finite number for are taken out, and the rows that do see their token get a NaN score instead.
+  const int seen_from = a.window > 0 ? max(max(first_pos, 0) - a.window + 1, 0) : 0;
+  uint32_t keep[NW];                                          // bytes of the lane's words that some row sees
+  uint32_t over;                                              // 0x80 less the first code taken out, in each byte
+  auto clean = [&](uint32_t x, uint32_t keep, uint32_t& out) {
     x &= keep;
-    nan = ((x & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
-    return x & ~(nan | (nan - (nan >> 7)));
+    out = ((x & 0x7F7F7F7Fu) + over) & 0x80808080u;
+    return x & ~(out | (out - (out >> 7)));
   };
-  uint32_t keep[NW];                                          // bytes of the lane's words that are values
   auto mask = [&](int ch, f32x4 (&s)[NW][R]) {
     const int t0 = ch * kTok + 4 * NW * g;                    // first of the lane's tokens
-    const int n = min(max(len - t0, 0), 4 * NW);
-    ve = n > 0 ? ve : 127u;                                   // a block past the end: its exponent too
+    const int n1 = min(max(last_pos + 1 - t0, 0), 4 * NW), n0 = min(max(seen_from - t0, 0), n1);
+    ve = n0 < n1 ? ve : 127u;
+    // NaN is 0x7F.  At 2^120 codes from 2^8 = 0x78 on are past bf16's numbers, at each power more a power
+    // less; an exponent byte of 255 is NaN
+    over = ve < 247u ? 0x01010101u : ve < 255u ? (ve - 246u) * 0x08080808u : 0x80808080u;
     uint32_t bad[NW];                                         // bit 8 i + 7 of word t: its token 4 t + i
 #pragma unroll
     for (int t = 0; t < NW; ++t) {
-      const int k = min(max(n - 4 * t, 0), 4);
-      keep[t] = k == 4 ? 0xFFFFFFFFu : (1u << (8 * k)) - 1u;
+      const auto below = [](int n) { return n <= 0 ? 0u : n >= 4 ? 0xFFFFFFFFu : (1u << (8 * n)) - 1u; };
+      keep[t] = below(n1 - 4 * t) & ~below(n0 - 4 * t);
       bad[t] = 0;
     }
 #pragma unroll
@@ -447,11 +453,12 @@ __global__ __launch_bounds__(64 * kAttWaves, OCC) void kv8_attention_kernel(Kv8C
       const vwords v = values(d);
 #pragma unroll
       for (int t = 0; t < NW; ++t) {
-        uint32_t nan;
-        clean(v[t], keep[t], nan);
-        bad[t] |= nan;
+        uint32_t out;
+        clean(v[t], keep[t], out);
+        bad[t] |= out;
       }
     }
+    ve = ve < 255u ? ve : 127u;
 #pragma unroll
     for (int t = 0; t < NW; ++t)
 #pragma unroll
@@ -481,8 +488,8 @@ __global__ __launch_bounds__(64 * kAttWaves, OCC) void kv8_attention_kernel(Kv8C
       if (edge) {
 #pragma unroll
         for (int t = 0; t < NW; ++t) {
-          uint32_t nan;
-          v[t] = clean(v[t], keep[t], nan);
+          uint32_t out;
+          v[t] = clean(v[t], keep[t], out);
         }
       }
 #pragma unroll

@@ -78,3 +78,52 @@ def test_append_without_rows():
 
     append([[0, 1], [2, 3]], [21, 13], [0, 3])          # codes lie past the first one's 21 tokens
     append([[2, 3], [2, 3], [2, 3]], [7, 19, 30], [0, 19, 0])   # the page is now the second one's
+
+
+# ---------------------------------------------------------------- values that no row of a tile, or not every one, sees
+def bound(ref, mag):
+    """Probabilities and outputs rounded to bf16, 2^-8 at most each; fp32 scores, 1e-5 of the probabilities."""
+    return 2.0 ** -8 * np.abs(ref) + (2.0 ** -8 + 2e-5) * mag
+
+
+WINDOWS = [  # lens, new, Hq, Hkv, D, page, window: tiles of 16, 32 and 128 rows
+    ([700, 300], [1, 1], 8, 2, 128, 16, 40), ([700, 90], [1, 1], 4, 1, 64, 64, 100), ([500], [1], 4, 4, 256, 16, 17),
+    ([500], [3], 8, 1, 256, 64, 30), ([900, 700], [9, 6], 8, 2, 128, 64, 70), ([800], [12], 4, 1, 64, 16, 50),
+    ([900], [8], 8, 1, 256, 16, 33), ([1100, 600], [90, 70], 4, 2, 128, 64, 130), ([1000], [200], 2, 1, 64, 16, 90),
+    ([700], [150], 4, 2, 256, 64, 100), ([640], [128], 4, 1, 128, 16, 1),
+]
+
+
+@pytest.mark.parametrize("cus", [1, 0])
+@pytest.mark.parametrize("codes,exps", [(0xFF, 254), (0x7E, 254), (0x38, 255), (0x00, 255), (0x7E, 247)])
+@pytest.mark.parametrize("lens,new,Hq,Hkv,D,page,window", WINDOWS)
+def test_before_the_window(budget, cus, codes, exps, lens, new, Hq, Hkv, D, page, window):
+    """Blocks before every row's window hold anything, and pages before it have left the table; so do the places of
+    a block that the first row's window begins in."""
+    log(f"[gpu] before the window cus={cus} {codes:#x} {exps} lens={lens} new={new} D={D} page={page} window={window}")
+    rng = np.random.default_rng(sum(lens) + D)
+    host, table = filled(lens, Hkv, D, page, rng)
+    # one page more, in front: what -1 is read as
+    for name in ("k", "v", "ke", "ve"):
+        t = getattr(host, name)
+        setattr(host, name, np.concatenate([np.full_like(t[:1], codes if len(name) == 1 else exps), t]))
+    table = np.where(table >= 0, table + 1, -1)
+    for b, n in enumerate(lens):
+        low = max(0, n - new[b] - window + 1)                   # the first token that a row sees
+        for blk in range(low // 16 + 1):
+            p, i = int(table[b, blk * 16 // page]), blk * 16 % page // 16
+            m = min(16, low - blk * 16)
+            if m == 16:
+                host.k[p, :, i * 16:i * 16 + 16], host.v[p, :, i] = codes, codes
+                host.ke[p, :, i], host.ve[p, :, i] = exps, exps
+            elif m > 0:
+                host.k[p, :, i * 16:i * 16 + m], host.v[p, :, i, :, :m] = 0x7F, 0xFF
+        table[b, :low // page] = -1
+    q = torch.from_numpy(rng.standard_normal((sum(new), Hq, D)).astype(np.float32)).to(torch.bfloat16)
+    budget(cus)
+    for most in (max(lens), 1):                                 # cut into parts, where few are; whole
+        out = moe.moe_kv8_attention(q.cuda(), host.device(), i32(table), i32(lens), i32(np.cumsum([0] + new)), max(new),
+                                    most, window=window).cpu().double().numpy()
+        with np.errstate(all="ignore"):
+            ref, mag = attention64(q.double().numpy(), host, table, lens, new, window, D ** -0.5)
+        assert (np.abs(out - ref) <= bound(ref, mag)).all()
