@@ -17,7 +17,7 @@ struct Kv8Steps {
 // of the chunks that its rows see.  The last chunk's steps end with the one that holds `last`: the next
 // one's page need not have a place in the block table.
 constexpr Kv8Steps kv8_steps(int first, int last, int window, int part, int parts, int tok) {
-  const int low = window > 0 ? std::max(first - window + 1, 0) : 0;
+  const int low = window > 0 ? std::max(std::max(first, 0) - window + 1, 0) : 0;   // first: maybe below 0
   const int c0 = low / kChunk, c1 = last < 0 ? c0 : std::max(last / kChunk + 1, c0);
   const int each = (std::max(c1 - c0, 0) + parts - 1) / parts;
   const int begin = std::min(c0 + part * each, c1), end = std::min(c0 + (part + 1) * each, c1);

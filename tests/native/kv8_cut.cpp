@@ -16,8 +16,8 @@ void expect(bool ok, const char* what, int len, int fresh, int window, int parts
 // One tile with all rows of the sequence: every token that a row sees is in one step of one part, and every step of
 // a page that holds whole steps begins in a page that the sequence has.
 void check(int len, int fresh, int window, int parts, int tok) {
-  const int first = len - fresh, last = len - 1;
-  const int low = window > 0 && first - window + 1 > 0 ? first - window + 1 : 0;
+  const int first = len - fresh, last = len - 1;            // first: below 0 where rows have no place
+  const int low = window > 0 && int64_t(first) - window + 1 > 0 ? first - window + 1 : 0;
   std::vector<int> seen(size_t(len) / tok + 3, 0);
   for (int p = 0; p < parts; ++p) {
     const moe::Kv8Steps s = moe::kv8_steps(first, last, window, p, parts, tok);
@@ -41,7 +41,7 @@ void check(int len, int fresh, int window, int parts, int tok) {
 int main() {
   for (int len = 0; len <= 700; ++len)
     for (int fresh : {1, 2, 17, 64, 65, 130, 699})
-      for (int window : {0, 1, 33, 100, 500})
+      for (int window : {0, 1, 33, 100, 500, INT32_MAX})
         for (int parts : {1, 2, 3, 7})
           for (int tok : {32, 64}) check(len, fresh, window, parts, tok);
   if (g_fail == 0) std::puts("ok");

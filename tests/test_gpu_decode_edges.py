@@ -127,3 +127,30 @@ def test_before_the_window(budget, cus, codes, exps, lens, new, Hq, Hkv, D, page
         with np.errstate(all="ignore"):
             ref, mag = attention64(q.double().numpy(), host, table, lens, new, window, D ** -0.5)
         assert (np.abs(out - ref) <= bound(ref, mag)).all()
+
+
+@pytest.mark.parametrize("cus", [1, 0])
+@pytest.mark.parametrize("D,Hq,new,window,page", [(128, 2, 6, 0, 16), (64, 4, 40, 20, 64), (128, 2, 100, 0, 64),
+                                                  (256, 1, 100, 30, 16), (256, 4, 6, 9, 64)])
+def test_infinite_value(budget, cus, D, Hq, new, window, page):
+    """A value that no finite bf16 number holds (an infinity that was appended is 448 2^120) makes the rows that see
+    its token infinite or NaN, and no others."""
+    log(f"[gpu] infinite value cus={cus} D={D} new={new} window={window} page={page}")
+    rng = np.random.default_rng(D + new)
+    n, at = 200, 200 - new // 2 - 1                             # length, position of the token
+    host, table = filled([n], 1, D, page, rng)
+    p, i = int(table[0, at // page]), at % page // 16
+    # its block's other values: under 2^114, whose sums times probabilities of up to 2^8 fp32 holds
+    host.ve[p, 0, i] = 247
+    host.v[p, 0, i] = rng.integers(0, 8, host.v[p, 0, i].shape)
+    host.v[p, 0, i, :, at % 16] = 0x7E
+    q = torch.from_numpy(rng.standard_normal((new, Hq, D)).astype(np.float32)).to(torch.bfloat16)
+    budget(cus)
+    out = moe.moe_kv8_attention(q.cuda(), host.device(), i32(table), i32([n]), i32([0, new]), new, n,
+                                window=window).cpu().double().numpy()
+    ref, mag = attention64(q.double().numpy(), host, table, [n], [new], window, D ** -0.5)
+    pos = np.arange(n - new, n)
+    sees = (pos >= at) & ((pos - at < window) if window else True)
+    assert sees.any() and not sees.all()
+    assert (np.abs(out - ref) <= bound(ref, mag))[~sees].all()
+    assert not np.isfinite(out[sees]).any()
