@@ -489,7 +489,8 @@ typedef struct {
  * that grew, their codes are rounded again to the new step; places after the last token are
  * set to 0.  Codes are rounded to nearest even.  An infinity saturates, NaN stays NaN and does
  * not count in s.  Calling again with the same arguments leaves the cache as it is.  Tokens
- * at positions of `positions` or more are rotated as the last one.
+ * at positions of `positions` or more are rotated as the last one.  Queries of tokens whose page
+ * is outside the cache or the table are rotated all the same; those of rows left out are not written.
  * Errors: INVALID_ARGUMENT for negative sizes, heads not dividing q_heads, a page not a positive
  * multiple of 16, a bad stride or rot, null or misaligned pointers; UNSUPPORTED for another dim,
  * T + 2 B of 2^24 or more, heads > 65535.

@@ -161,10 +161,9 @@ __global__ __launch_bounds__(2 * D) void kv8_append_kernel(Kv8Cache c, Kv8Batch 
   if (p0 >= len) return;
   const int per_page = c.page / kKvBlock;
   const int column = blk / per_page;
-  if (column >= b.table_cols) return;
-  const int64_t page = b.table[int64_t(seq) * b.table_cols + column];
-  if (page < 0 || page >= c.pages) return;
-  const int64_t at = kv_block(page, head, blk % per_page, c.heads, per_page);
+  const int64_t page = column < b.table_cols ? b.table[int64_t(seq) * b.table_cols + column] : -1;
+  const bool held = page >= 0 && page < c.pages;              // otherwise only queries are written
+  const int64_t at = kv_block(held ? page : 0, head, blk % per_page, c.heads, per_page);
 
   const int fresh0 = max(first - p0, 0), fresh1 = min(len - p0, kKvBlock);   // the new tokens' places in the block
   const int place = tid / kPer;
@@ -176,7 +175,7 @@ __global__ __launch_bounds__(2 * D) void kv8_append_kernel(Kv8Cache c, Kv8Batch 
   uint8_t* exps = (side == 0 ? c.k_exps : c.v_exps) + at;
   u32x4 old = {0u, 0u, 0u, 0u};                               // this token's codes; one dimension's of all 16 tokens
   int old_e = -127;
-  if (fresh0 > 0) {                                           // the block holds earlier tokens
+  if (held && fresh0 > 0) {                                   // the block holds earlier tokens
     old_e = int(*exps) - 127;
     if (side == 1) {
       old = *vc;
@@ -225,6 +224,7 @@ __global__ __launch_bounds__(2 * D) void kv8_append_kernel(Kv8Cache c, Kv8Batch 
     }
   }
 
+  if (!held) return;                                          // all of the workgroup
   float m = 0.f;                                              // fmaxf passes over NaN
 #pragma unroll
   for (int i = 0; i < 16; ++i) m = fmaxf(m, fabsf(x[i]));

@@ -154,3 +154,25 @@ def test_infinite_value(budget, cus, D, Hq, new, window, page):
     assert sees.any() and not sees.all()
     assert (np.abs(out - ref) <= bound(ref, mag))[~sees].all()
     assert not np.isfinite(out[sees]).any()
+
+
+def test_append_rotates_without_a_page():
+    """New tokens that have no page in the cache are not written; their queries are rotated all the same."""
+    log("[gpu] append: queries of tokens without a page")
+    rng = np.random.default_rng(4)
+    D, Hq, Hkv = 64, 4, 2
+    x = torch.from_numpy(rng.standard_normal((23, Hq + 2 * Hkv, D)).astype(np.float32)).to(torch.bfloat16)
+    cs = angles(64, D)
+    host = HostCache(2, Hkv, 16, D)
+    dev = host.device()
+    table, lens, cu = i32([[-1, -1], [2, 0], [1, 0]]), i32([1, 20, 34]), i32([0, 1, 21, 23])
+    q_out = torch.full((23, Hq, D), 7.0, dtype=torch.bfloat16, device="cuda")
+    g = x.cuda()
+    moe.moe_kv8_append(g[:, :Hq], g[:, Hq:Hq + Hkv], g[:, Hq + Hkv:], torch.from_numpy(cs).cuda(), dev, table, lens, cu,
+                       q_out=q_out)
+    torch.cuda.synchronize()
+    pos = np.concatenate([[0], np.arange(20), [32, 33]])        # the last two are past the table's columns
+    f = x.float().numpy()
+    assert torch.equal(q_out.cpu(), torch.from_numpy(rotate(f[:, :Hq], pos, cs, False)).to(torch.bfloat16))
+    host.append(rotate(f[17:21, Hq:Hq + Hkv], pos[17:21], cs, False), f[17:21, Hq + Hkv:], [1, 0], 16, 4)
+    assert host.same(dev)
