@@ -414,7 +414,8 @@ moe_status moe_matvec_int4(const void* x, const uint8_t* codes, const uint8_t* s
  * The gate weight multiplies silu(g) u in fp32; h is kept to 16 significant bits (two bf16
  * numbers), all sums are fp32, y is rounded once.  Deterministic; the order of y's sums depends
  * on the experts that the batch chose, so a token's y may differ in its last bit with the tokens
- * beside it.
+ * beside it.  Weights and scales that are not finite reach the tokens that chose their expert
+ * alone, as in moe_grouped_ffn.
  * Errors: as moe_route and moe_grouped_ffn, plus INVALID_ARGUMENT for Fs < 0 or not a
  * multiple of 64; UNSUPPORTED for T > 16.
  *

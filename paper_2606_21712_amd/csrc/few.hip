@@ -349,7 +349,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void few_down_kernel(const uint16_t*
   const auto bh = buffer_of(h, int64_t(T) * (int64_t(k) * F + Fs) * 4);
 
   using At = Place<W, C>;
-  auto enter = [&](At& p) {                     // sets what goes with p.a
+  auto enter = [&](At& p, int lane) {           // sets what goes with p.a
     const bool shared = p.a >= n;
     const int mat = shared ? 0 : __builtin_amdgcn_readfirstlane(ch.expert[p.a]);
     p.steps = shared ? ssteps : fsteps;
@@ -371,19 +371,22 @@ __global__ __launch_bounds__(64 * WAVES, 4) void few_down_kernel(const uint16_t*
       p.steps = p.a < n ? fsteps : ssteps;
     }
   };
-  auto advance = [&](At& p) {
+  auto advance = [&](At& p, int lane) {
     p.s += stride;
     if (p.s >= p.steps) {
       carry(p);
-      enter(p);
+      enter(p, lane);
     }
   };
+  auto start = [&](At& p, int lane) {
+    p.a = 0;
+    p.s = begin + rg * 5 % total;               // workgroups start at different columns, as in few_up
+    p.steps = fsteps;                           // T, k >= 1: an expert is listed
+    carry(p);
+    enter(p, lane);
+  };
   At pw, px;
-  pw.a = 0;
-  pw.s = begin + rg * 5 % total;                // workgroups start at different columns, as in few_up
-  pw.steps = fsteps;                            // T, k >= 1: an expert is listed
-  carry(pw);
-  enter(pw);
+  start(pw, lane);
   px = pw;
 
   f32x4 acc[NT][C][kAcc];
@@ -394,12 +397,12 @@ __global__ __launch_bounds__(64 * WAVES, 4) void few_down_kernel(const uint16_t*
   auto load_w = [&](int p, int i) {
 #pragma unroll
     for (int r = 0; r < NT; ++r) W::load(ws[p][r], pw.v, rg * NT + r, pw.s, i < mine);
-    advance(pw);
+    advance(pw, lane);
   };
   auto load_x = [&](int p, int i) {
 #pragma unroll
     for (int c = 0; c < C; ++c) W::load_x(xb[p][c], bh, px.xat[c], px.s, px.cols, i < mine);
-    advance(px);
+    advance(px, lane);
   };
 #pragma unroll
   for (int p = 0; p < P; ++p) {
@@ -418,10 +421,52 @@ __global__ __launch_bounds__(64 * WAVES, 4) void few_down_kernel(const uint16_t*
       __builtin_amdgcn_sched_barrier(0);
     }
   }
+  // A weight that is not finite times the zeros of a token that did not choose its expert is NaN.  Where a sum is
+  // not finite the wavefront walks its steps again, tile by tile, and the tokens that did not choose a
+  // step's expert keep their sums.  (In every step instead, sums and their copies spill.)
+  float odd = 0.f;                              // 0, or NaN
 #pragma unroll
-  for (int q = 0; q < kSums; ++q) {
-    const int i = q % kAcc, t = q / kAcc % TS, r = q / kAcc / TS;
-    part[wave][q][lane] = FOLD ? acc[r][t][i] : acc[r][2 * t][i] + acc[r][(2 * t + 1) % C][i];
+  for (int q = 0; q < 4 * NT * C * kAcc; ++q) odd += 0.f * (&acc[0][0][0])[q / 4][q % 4];
+  auto put = [&](int lane, int r, const f32x4 (&v)[C][kAcc]) {
+#pragma unroll
+    for (int q = 0; q < TS * kAcc; ++q) {
+      const int i = q % kAcc, t = q / kAcc;
+      part[wave][r * TS * kAcc + q][lane] = FOLD ? v[t][i] : v[2 * t][i] + v[(2 * t + 1) % C][i];
+    }
+  };
+  if (__ballot(odd != 0.f) == 0) {
+#pragma unroll
+    for (int r = 0; r < NT; ++r) put(lane, r, acc[r]);
+  } else {
+    // the lane asked for anew: kept through the loop, what hangs on it costs registers there (4 bits, groups of
+    // 32, 13 tokens of 4 x F 4096, H 4096: 91 -> 116 us)
+    const int lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0));
+#pragma unroll 1
+    for (int r = 0; r < NT; ++r) {
+      f32x4 sum[C][kAcc], next[C][kAcc];
+#pragma unroll
+      for (int q = 0; q < C * kAcc; ++q) (&sum[0][0])[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+      start(pw, lane);
+#pragma unroll 1
+      for (int i = 0; i < mine; ++i) {
+        bool chose[C];
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          W::load_x(xb[0][c], bh, pw.xat[c], pw.s, pw.cols, true);
+          chose[c] = pw.xat[c] != kPast;
+        }
+        W::load(ws[0][0], pw.v, rg * NT + r, pw.s, true);
+        typename W::template Sums<C> sums;
+        W::template sums<C>(sums, xb[0], lane);
+#pragma unroll
+        for (int q = 0; q < C * kAcc; ++q) (&next[0][0])[q] = (&sum[0][0])[q];
+        W::template add<C>(next, ws[0][0], xb[0], sums);
+#pragma unroll
+        for (int q = 0; q < C * kAcc; ++q) (&sum[0][0])[q] = chose[q / kAcc] ? (&next[0][0])[q] : (&sum[0][0])[q];
+        advance(pw, lane);
+      }
+      put(lane, r, sum);
+    }
   }
   __syncthreads();
   for (int q = wave; q < kSums; q += WAVES) {

@@ -176,3 +176,41 @@ def test_append_rotates_without_a_page():
     assert torch.equal(q_out.cpu(), torch.from_numpy(rotate(f[:, :Hq], pos, cs, False)).to(torch.bfloat16))
     host.append(rotate(f[17:21, Hq:Hq + Hkv], pos[17:21], cs, False), f[17:21, Hq + Hkv:], [1, 0], 16, 4)
     assert host.same(dev)
+
+
+# ---------------------------------------------------------------- the layer for few tokens
+@pytest.mark.parametrize("int4", [False, True])
+@pytest.mark.parametrize("cus", [8, 0])
+@pytest.mark.parametrize("T,H,F,Fs", [(1, 128, 64, 0), (7, 256, 512, 64), (8, 6144, 64, 0), (13, 256, 1024, 0),
+                                      (16, 448, 128, 128)])
+def test_weights_of_other_experts(budget, cus, T, H, F, Fs, int4):
+    """Weights that are not finite reach the tokens that chose their expert, and no others."""
+    log(f"[gpu] few: non-finite weights int4={int4} cus={cus} T={T} H={H} F={F} Fs={Fs}")
+    E, k, bad = 8, 2, 3
+    x, logits, shapes, r = inputs(T, H, E, k, F, Fs, T + H)
+    w = [(torch.randn(s, generator=r) * s[2] ** -0.5).to(torch.bfloat16) for s in shapes]
+    logits[:, bad] = -9.0
+    logits[0, bad] = 9.0                                        # the first token alone chooses it
+    x, logits = x.cuda(), logits.cuda()
+    budget(cus)
+
+    def run(spoil):
+        ws = [t.clone() for t in w]
+        if not int4:
+            for i, (n, c) in enumerate(spoil):
+                if n is not None:
+                    ws[2][bad, n, c] = (float("inf"), float("nan"))[i % 2]
+            return moe.moe_few_tokens(x, logits, k, *[t.cuda() for t in ws])[0]
+        std = [moe.moe_quantize_int4(t.cuda(), 32, True) for t in ws]
+        for i, (n, c) in enumerate(spoil):
+            if n is not None:
+                std[2][1][bad, n, c // 32] = (float("inf"), float("nan"))[i % 2]
+        return moe.moe_few_tokens(x, logits, k, *[moe.moe_pack_int4(*s, 32) for s in std])[0]
+
+    clean = run([])
+    y = run([(5, 3), (17, F - 1), (H - 1, F // 2)])
+    assert torch.equal(y[1:], clean[1:])
+    hit = torch.zeros(H, dtype=torch.bool, device="cuda")
+    hit[[5, 17, H - 1]] = True
+    assert not y[0, hit].isfinite().any() and torch.equal(y[0, ~hit], clean[0, ~hit])
+    assert clean.isfinite().all()
