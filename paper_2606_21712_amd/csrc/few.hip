@@ -296,8 +296,11 @@ __global__ __launch_bounds__(64 * kUpWaves, 4) void few_up_kernel(const uint16_t
                       (rt * NU + r2) * 16 + W::row(i, lane);
       const u32x2 hi = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
       *reinterpret_cast<u32x2*>(out) = hi;
+      // an h that rounds to infinity has an infinite or NaN rest, which would make the sum of both NaN: any finite
+      // number will do (of NaN, med3 gives one of the bounds)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) v[r] -= __uint_as_float(r & 1 ? hi[r / 2] & 0xFFFF0000u : hi[r / 2] << 16);
+      for (int r = 0; r < 4; ++r)
+        v[r] = __builtin_amdgcn_fmed3f(v[r] - __uint_as_float(r & 1 ? hi[r / 2] & 0xFFFF0000u : hi[r / 2] << 16), -1e38f, 1e38f);
       *reinterpret_cast<u32x2*>(out + width) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
     }
   }

@@ -214,3 +214,23 @@ def test_weights_of_other_experts(budget, cus, T, H, F, Fs, int4):
     hit[[5, 17, H - 1]] = True
     assert not y[0, hit].isfinite().any() and torch.equal(y[0, ~hit], clean[0, ~hit])
     assert clean.isfinite().all()
+
+
+@pytest.mark.parametrize("T", [2, 12])
+def test_h_beyond_bf16(T):
+    """An h above the largest bf16 number is infinite, as in MoELayer: its token's y is infinite where that has a
+    sign, the other tokens' is finite."""
+    log(f"[gpu] few: h beyond bf16 T={T}")
+    H = F = 64
+    x = torch.zeros(T, H, dtype=torch.bfloat16)
+    x[:, 0] = 1.0
+    x[0, 0] = 1e20
+    wg, wu, wd = (torch.zeros(1, 64, 64, dtype=torch.bfloat16) for _ in range(3))
+    wg[0, 0, 0] = wu[0, 0, 0] = 1.0
+    wg[0, 1, 0] = wu[0, 1, 0] = 1.8e-1                          # 3.24e38: finite, and rounds to a finite number
+    wd[0, :, 0] = torch.where(torch.arange(H) % 2 == 0, 1.0, -1.0)
+    logits = torch.zeros(T, 1)
+    args = [t.cuda() for t in (x, logits, wg, wu, wd)]
+    y = moe.moe_few_tokens(args[0], args[1], 1, *args[2:])[0]
+    ref = moe.MoELayer(T, H, 1, 1, F, gather=True).run(*args)
+    assert torch.equal(y, ref) and y[0].isinf().all() and y[1:].isfinite().all()
