@@ -557,7 +557,7 @@ def moe_few_tokens(x, logits, k, w_gate, w_up, w_down, ws_gate=None, ws_up=None,
     or Int4 -> (y bf16 [T, H], topk_ids, topk_weights)."""
     _few_inputs(x, logits)
     T, H = x.shape
-    F = w_gate.shape[1]
+    F = w_gate.shape[-2]
     Fs = 0 if ws_gate is None else ws_gate.shape[-2]
     dev = x.device
     topk_ids = _like(topk_ids, "topk_ids", torch.int32, (T, k), dev, stream)

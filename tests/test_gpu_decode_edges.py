@@ -234,3 +234,21 @@ def test_h_beyond_bf16(T):
     y = moe.moe_few_tokens(args[0], args[1], 1, *args[2:])[0]
     ref = moe.MoELayer(T, H, 1, 1, F, gather=True).run(*args)
     assert torch.equal(y, ref) and y[0].isinf().all() and y[1:].isfinite().all()
+
+
+@pytest.mark.parametrize("int4", [False, True])
+def test_one_expert_without_its_axis(int4):
+    """Weights of a single expert as matrices, F other than H."""
+    log(f"[gpu] few: 2-D weights int4={int4}")
+    T, H, F, Fs = 5, 128, 320, 64
+    x, logits, shapes, r = inputs(T, H, 1, 1, F, Fs, 2)
+    w = [(torch.randn(s, generator=r) * s[2] ** -0.5).to(torch.bfloat16).cuda() for s in shapes]
+    if int4:
+        w = [moe.quantize_weights_int4(t, 32) for t in w]
+        flat = [moe.Int4(t.codes, t.scales, t.zeros, t.shape[1:], t.group) for t in w]
+    else:
+        flat = [t[0] for t in w]
+    x, logits = x.cuda(), logits.cuda()
+    want = moe.moe_few_tokens(x, logits, 1, *w)
+    got = moe.moe_few_tokens(x, logits, 1, *flat)
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
