@@ -27,7 +27,8 @@ __global__ __launch_bounds__(256) void quantize_int4_kernel(const uint16_t* __re
     }
   }
   // the step, rounded to bf16 before it is used: codes are of the scale that is stored
-  const float step = zeros ? (hi - lo) / 15.0f : fmaxf(hi, 0.f - lo) / 7.0f;
+  // (hi - lo in halves, the same bits: whole it may be past fp32)
+  const float step = zeros ? (0.5f * hi - 0.5f * lo) / 7.5f : fmaxf(hi, 0.f - lo) / 7.0f;
   const uint16_t sb = uint16_t(pack_bf16x2(step, 0.f) & 0xFFFFu);
   const float s = bf16_to_f32(sb);
   const float z = !zeros ? 8.0f : s > 0.f ? fminf(rintf(-lo / s), 15.0f) : 0.0f;

@@ -252,3 +252,20 @@ def test_one_expert_without_its_axis(int4):
     want = moe.moe_few_tokens(x, logits, 1, *w)
     got = moe.moe_few_tokens(x, logits, 1, *flat)
     assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+# ---------------------------------------------------------------- 4-bit weights
+def test_quantize_largest():
+    """A group that spans more than the largest fp32 number has a finite scale."""
+    log("[gpu] quantize int4: largest values")
+    w = torch.zeros(2, 64, dtype=torch.bfloat16)
+    top = torch.finfo(torch.bfloat16).max
+    w[0, 0], w[0, 1], w[0, 2] = top, -top, 0.5 * top
+    w[1, 3] = -top
+    codes, s, z = moe.moe_quantize_int4(w.cuda(), 64, True)
+    lo, hi = w.double().amin(1).clamp_max(0), w.double().amax(1).clamp_min(0)
+    assert torch.equal(s.cpu()[:, 0], ((hi - lo) / 15).to(torch.bfloat16))
+    f = s.cpu().double()
+    zero = torch.round(-lo[:, None] / f).clamp_max(15)
+    q = (torch.round(w.double() / f) + zero).clamp(0, 15).to(torch.uint8)
+    assert torch.equal(z.cpu().double(), zero) and torch.equal(codes.cpu(), q[:, 0::2] | (q[:, 1::2] << 4))
