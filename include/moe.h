@@ -412,10 +412,10 @@ moe_status moe_matvec_int4(const void* x, const uint8_t* codes, const uint8_t* s
  *                   and the parts of y's sums; not to be shared by calls that overlap
  *
  * The gate weight multiplies silu(g) u in fp32; h is kept to 16 significant bits (two bf16
- * numbers), all sums are fp32, y is rounded once.  Deterministic; the order of y's sums depends
- * on the experts that the batch chose, so a token's y may differ in its last bit with the tokens
- * beside it.  Weights and scales that are not finite reach the tokens that chose their expert
- * alone, as in moe_grouped_ffn.
+ * numbers), all sums are fp32, y is rounded once.  Deterministic for a given device and
+ * compute-unit budget; the order of y's sums depends on the experts that the batch chose, so a
+ * token's y may differ in its last bit with the tokens beside it.  Weights and scales that are
+ * not finite reach the tokens that chose their expert alone, as in moe_grouped_ffn.
  * Errors: as moe_route and moe_grouped_ffn, plus INVALID_ARGUMENT for Fs < 0 or not a
  * multiple of 64; UNSUPPORTED for T > 16.
  *
@@ -568,10 +568,14 @@ moe_status moe_profiler_record(int i, const char** name, float* ms);
  * device's count (values above the device's count are used as given), so a
  * caller can leave compute units to concurrent streams; the grouped GEMMs then run
  * these kernels for small groups too, where a kernel with one workgroup per tile is
- * otherwise faster.  The fp32 GEMMs and the fused router choose their tiles by it.
+ * otherwise faster.  The fp32 GEMMs, the fused router and moe_matvec_int4 choose their tiles
+ * by it.  The first kernel of moe_few_tokens is persistent too; its down projection, and
+ * moe_kv8_attention over long sequences, are cut into parts for n compute units (with more
+ * tiles than that, a workgroup for each tile).
  * n = 0 restores the device's count.  Results do not depend on it beyond fp32
  * rounding: the order of the GEMMs' sums depends on the kernel, and how the down
- * projection's last round of tiles is split along k on the grid.
+ * projection's last round of tiles is split along k on the grid.  (moe_kv8_attention's depend
+ * on it by the rounding of its probabilities too, which are relative to a maximum of each part.)
  * Process-wide; set it between calls, not while other host threads launch.
  * Errors: INVALID_ARGUMENT for n < 0.
  */

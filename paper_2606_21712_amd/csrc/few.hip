@@ -544,7 +544,8 @@ void down_c(const FewShape& s, const W (&w)[6], hipStream_t stream) {
   // 4 bits, H 1984, 3 tokens of 5 x F 512: 16.6 and 10.9).
   const int64_t steps = int64_t(std::min(s.T * s.k, s.E)) * ((s.F + W::kCols - 1) / W::kCols) +
                         (s.Fs + W::kCols - 1) / W::kCols;
-  const int64_t want = std::min<int64_t>({(kFewParts + groups - 1) / groups, kFewMostParts, steps / (2 * kWaves)});
+  const int64_t all = std::min<int64_t>(2 * int64_t(s.num_cu), kFewParts);
+  const int64_t want = std::min<int64_t>({(all + groups - 1) / groups, kFewMostParts, steps / (2 * kWaves)});
   const bool cut = groups < s.num_cu * 3 / 4 && steps >= S::kCut * kWaves;
   const int parts = cut ? int(std::max<int64_t>(1, want)) : 1;
   MOE_LAUNCH("few_down", (few_down_kernel<W, NT, kWaves, TS, FOLD, S::kDown, S::kDownX>),

@@ -30,9 +30,9 @@ constexpr int kMinPieceSteps = 8;
 // caller workspace: calls whose moe_permute_workspace_bytes() exceeds it are refused.
 constexpr unsigned long kPermuteStaticScratchBytes = 4ul << 20;
 
-// The layer for few tokens: its down projection is cut along k into parts, so that about
-// kFewParts workgroups run (two on each of 256 compute units), at most kFewMostParts for each
-// of its groups of up to kFewMaxCols columns; each part keeps fp32 sums [T, H].
+// The layer for few tokens: its down projection is cut along k into parts, so that about two
+// workgroups run on each compute unit, kFewParts at most (256 compute units), and at most kFewMostParts
+// for each of its groups of up to kFewMaxCols columns; each part keeps fp32 sums [T, H].
 constexpr int kFewParts = 512;
 constexpr int kFewMostParts = 16;
 constexpr int kFewMaxCols = 64;

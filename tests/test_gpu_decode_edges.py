@@ -269,3 +269,24 @@ def test_quantize_largest():
     zero = torch.round(-lo[:, None] / f).clamp_max(15)
     q = (torch.round(w.double() / f) + zero).clamp(0, 15).to(torch.uint8)
     assert torch.equal(z.cpu().double(), zero) and torch.equal(codes.cpu(), q[:, 0::2] | (q[:, 1::2] << 4))
+
+
+# ---------------------------------------------------------------- the compute-unit budget
+@pytest.mark.parametrize("cus,H,T,F", [(8, 64, 3, 4096), (24, 128, 8, 2048), (40, 192, 16, 2048), (0, 256, 2, 8192)])
+def test_down_parts_keep_to_the_budget(budget, cus, H, T, F):
+    """The down projection's parts, of which each writes its sums to the workspace, are two workgroups a compute unit
+    at most, one group of 16 columns more aside."""
+    log(f"[gpu] few: parts cus={cus} H={H} T={T} F={F}")
+    E, k = 8, 2
+    x, logits, shapes, r = inputs(T, H, E, k, F, 0, H)
+    w = [(torch.randn(s, generator=r) * s[2] ** -0.5).to(torch.bfloat16).cuda() for s in shapes]
+    ws = torch.full((moe.moe_few_tokens_workspace_bytes(T, H, k, F),), 0xAB, dtype=torch.uint8, device="cuda")
+    budget(cus)
+    moe.moe_few_tokens(x.cuda(), logits.cuda(), k, *w, ws=ws)
+    torch.cuda.synchronize()
+    sums = ws[-(-T * k * F * 4 // 256) * 256:].view(torch.int32)
+    sums = sums[:sums.numel() // (T * H) * (T * H)].view(-1, T * H)
+    parts = int((sums != 0xABABABAB - 2 ** 32).any(1).sum())
+    groups = H // 16
+    units = cus or torch.cuda.get_device_properties(0).multi_processor_count
+    assert 1 < parts and (parts - 1) * groups < 2 * units
