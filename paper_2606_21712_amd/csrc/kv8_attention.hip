@@ -113,7 +113,7 @@ __device__ __forceinline__ Cut cut_of(const Kv8Batch& b, const Kv8Attend& a, con
   c.len = min(b.lens[seq], p.capacity);
   if (c.fresh <= 0) return c;
   c.tiles = int(min((int64_t(c.fresh) * G + p.rows - 1) / p.rows, int64_t(p.tiles)));
-  c.chunks = (max(c.len, 0) + kChunk - 1) / kChunk;
+  c.chunks = kv8_chunks(c.len);
   if (a.window > 0) c.chunks = min(c.chunks, int((int64_t(a.window) + p.rows) / kChunk + 2));
   return c;
 }
@@ -808,8 +808,9 @@ hipError_t launch_kv8_attention(const Kv8Cache& c, const Kv8Batch& b, const Kv8A
   const uint32_t per_page = uint32_t(c.page / kKvBlock);
   p.inverse = per_page == 1 ? 0xFFFFFFFFu : uint32_t((uint64_t(1) << 32) / per_page);
   p.row_words = row_words(b.tokens, a.q_heads);
-  p.workgroups = kv8_workgroups(p, b.sequences, c.heads);
   p.capacity = int(std::min<int64_t>(int64_t(b.table_cols) * c.page, INT32_MAX));
+  if (!kv8_counts_fit(int64_t(b.sequences) * p.tiles, p.capacity)) p.target = 0;
+  p.workgroups = kv8_workgroups(p, b.sequences, c.heads);
   if (c.dim == 64) return launch_rows<64>(c, b, a, p, s);
   if (c.dim == 128) return launch_rows<128>(c, b, a, p, s);
   return launch_rows<256>(c, b, a, p, s);

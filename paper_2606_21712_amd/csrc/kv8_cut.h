@@ -8,6 +8,13 @@ namespace moe {
 
 constexpr int kChunk = 64;                    // tokens: the unit in which work is dealt
 
+// Chunks of `len` tokens.
+constexpr int kv8_chunks(int len) { return len > 0 ? (len - 1) / kChunk + 1 : 0; }
+
+// Whether the chunks of `tiles` tiles of up to `capacity` tokens are counted in 32 bits, as the kernel adds
+// them up where it cuts tiles: 511 tiles of 268 million tokens are not.
+constexpr bool kv8_counts_fit(int64_t tiles, int capacity) { return tiles * kv8_chunks(capacity) <= INT32_MAX; }
+
 // Steps [begin, end) of `tok` tokens (kChunk or a divisor of it); end <= begin: none.
 struct Kv8Steps {
   int begin, end;

@@ -44,6 +44,14 @@ int main() {
       for (int window : {0, 1, 33, 100, 500, INT32_MAX})
         for (int parts : {1, 2, 3, 7})
           for (int tok : {32, 64}) check(len, fresh, window, parts, tok);
+  // the largest lengths that a block table has place for, and tiles up to two a compute unit of 256
+  for (int64_t len : {int64_t(0), int64_t(1), int64_t(64), int64_t(65), int64_t(1) << 28, int64_t(INT32_MAX) - 15,
+                      int64_t(INT32_MAX)}) {
+    const int64_t chunks = (len + moe::kChunk - 1) / moe::kChunk;
+    expect(moe::kv8_chunks(int(len)) == chunks, "chunks", int(len), 0, 0, 0, 0);
+    for (int tiles = 1; tiles < 512; ++tiles)
+      expect(moe::kv8_counts_fit(tiles, int(len)) == (tiles * chunks <= INT32_MAX), "counts", int(len), tiles, 0, 0, 0);
+  }
   if (g_fail == 0) std::puts("ok");
   return g_fail != 0;
 }

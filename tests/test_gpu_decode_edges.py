@@ -290,3 +290,26 @@ def test_down_parts_keep_to_the_budget(budget, cus, H, T, F):
     groups = H // 16
     units = cus or torch.cuda.get_device_properties(0).multi_processor_count
     assert 1 < parts and (parts - 1) * groups < 2 * units
+
+
+def test_table_of_many_columns():
+    """A block table with place for more tokens than can be counted in 32 bits for all tiles: the long sequence is not
+    cut, its output is the same to the rounding of the probabilities."""
+    log("[gpu] attention: a table of 400 million tokens")
+    rng = np.random.default_rng(6)
+    D, page, cols, B = 64, 1 << 18, 1536, 400
+    lens = [3000] + [int(n) for n in rng.integers(1, 40, B - 1)]
+    cache = moe.KVCache8.empty(1, 1, D, page)
+    for t in (cache.k_codes, cache.v_codes):
+        t.copy_(torch.from_numpy(rng.integers(0, 0x58, t.shape, dtype=np.uint8)))
+    cache.k_exps.fill_(127 - 6)
+    cache.v_exps.fill_(127 - 6)
+    q = torch.from_numpy(rng.standard_normal((B, 1, D)).astype(np.float32)).to(torch.bfloat16).cuda()
+    wide = torch.full((B, cols), -1, dtype=torch.int32, device="cuda")
+    wide[:, 0] = 0
+    args = i32(lens), i32(range(B + 1)), 1, max(lens)
+    a = moe.moe_kv8_attention(q, cache, wide, *args)
+    b = moe.moe_kv8_attention(q, cache, wide[:, :1].contiguous(), *args)
+    torch.cuda.synchronize()
+    assert torch.equal(a[1:], b[1:])
+    assert (a[0] - b[0]).float().norm() <= 2.0 ** -7 * b[0].float().norm() and b[0].float().norm() > 0
