@@ -516,7 +516,7 @@ moe_status moe_kv8_append(const void* q, int64_t q_stride, const void* k, int64_
  *   ws, ws_bytes  device scratch of at least moe_kv8_attention_workspace_bytes() for the same sizes
  *
  * A row at position p sees tokens 0..p, with a window p - window + 1..p.  The products of queries
- * and keys are exact up to 2^-18 of a query row's largest element; scores, softmax and sums are
+ * and keys are exact up to 2^-17 of a query row's largest element; scores, softmax and sums are
  * fp32, probabilities are rounded to bf16 for the product with the values and for their sum.  A
  * row that sees nothing is 0.  Cache contents past a sequence's end are not used, whatever they
  * are, and neither are those outside a row's window.  A NaN that a row sees shows as NaN in its

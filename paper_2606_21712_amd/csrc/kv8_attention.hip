@@ -16,13 +16,14 @@
 //                  holds for block g.  No score moves between lanes.
 //
 // The first product takes 8-bit numbers on both sides: a query row is scaled by a power of two and
-// written as the sum of two E4M3 numbers, which together hold the eight significant bits of bf16 (numbers
-// 2^-10 below the row's largest and less are off by up to 2^-18 of it).  Two 8-bit products cost what one
+// written as the sum of two E4M3 numbers, which together hold the eight significant bits of bf16.  (Numbers
+// 2^-9 below the row's largest and less are off by up to 2^-17 of it: that is half the second
+// number's smallest step, 2^-9, where the largest is 2^7.)  Two 8-bit products cost what one
 // in bf16 does, and the keys' codes need no expansion: an expansion costs the vector unit
 // four times an ordinary instruction, and was what bound prompts.  The values' codes, times their
 // block's power of two, are expanded to bf16 exactly (E4M3 has four significant bits).  Scores, maxima
-// and outputs are fp32; probabilities are rounded to bf16 (2^-9 relative) for the second product.  Their
-// sum is one more row of that product, of ones: fp32 sums of the rounded probabilities, which is
+// and outputs are fp32; probabilities are rounded to bf16 (2^-8 relative at most) for the second product.
+// Their sum is one more row of that product, of ones: fp32 sums of the rounded probabilities, which is
 // what the values are weighted with.
 //
 // Work is dealt by what the sequences hold, which only the device knows: every workgroup adds up the

@@ -9,7 +9,7 @@ import torch
 import paper_2606_21712_amd as moe
 from gpu_util import log
 from test_gpu_few import inputs, layer64, route64
-from test_gpu_kv8 import attention64, filled, i32
+from test_gpu_kv8 import HostCache, attention64, filled, i32
 
 pytestmark = pytest.mark.gpu
 
@@ -86,6 +86,31 @@ def test_many_sequences(B, longest):
     assert (np.abs(out - ref) <= 2.0 ** -8 * np.abs(ref) + (2.0 ** -8 + 2e-5) * mag).all()
     none = np.repeat([n == 0 for n in lens], new)
     assert none.any() and not out[none].any()
+
+
+@pytest.mark.parametrize("D,page", [(64, 16), (128, 64), (256, 16)])
+def test_small_elements_of_a_query(D, page):
+    """Elements far below a query row's largest: off by 2^-17 of that at most.  They are chosen so that each is off by
+    that much, one half up and one down, against keys of opposite signs; two tokens' probabilities show it."""
+    log(f"[gpu] attention: small elements of a query D={D}")
+    half = (D - 2) // 2
+    q = torch.zeros(1, 1, D, dtype=torch.float64)
+    q[0, 0, 0] = 1.0                                        # the largest, 2^7 of the row's units
+    q[0, 0, 2:2 + half] = (2.0 ** -4 + 2.0 ** -10) / 128
+    q[0, 0, 2 + half:] = (2.0 ** -4 + 3 * 2.0 ** -10) / 128
+    assert torch.equal(q.to(torch.bfloat16).double(), q)
+    host = HostCache(1, 1, page, D)
+    one = int(torch.ones(1).to(torch.float8_e4m3fn).view(torch.uint8))
+    host.ke[0, 0, 0] = host.ve[0, 0, 0] = 127
+    host.k[0, 0, 0, 2:2 + half], host.k[0, 0, 0, 2 + half:] = one, one | 0x80
+    host.v[0, 0, 0, :, 0] = one                             # out: the first token's probability
+    scale = 2.0 ** 16 / D
+    out = moe.moe_kv8_attention(q.to(torch.bfloat16).cuda(), host.device(), i32([[0]]), i32([2]), i32([0, 1]), 1, 2,
+                                scale=scale).cpu().double()
+    score = float(q[0, 0, 2:2 + half].sum() - q[0, 0, 2 + half:].sum()) * scale
+    got = torch.log(out / (1 - out))
+    # the probability is rounded to bf16 twice, 2^-8 each
+    assert ((got - score).abs() <= 2.0 ** -17 * (D - 2) * scale + 4 * 2.0 ** -8 / (1 - out)).all()
 
 
 @pytest.mark.parametrize("T,H,E,k,F,Fs", [(3, 512, 8, 2, 1024, 0), (8, 1024, 16, 4, 512, 256), (16, 768, 32, 4, 640, 0)])
