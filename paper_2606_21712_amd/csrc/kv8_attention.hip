@@ -34,7 +34,7 @@
 // One token a sequence is bound by the read of the cache: 8 sequences of up to 40000 tokens, 32 heads on
 // 8 of 128, 271 MB in 53.5 us (5.1 TB/s, the join's 4.6 us and some 6 us of each workgroup's start
 // and end included); 50 of up to 4500, 32 heads on 4 in pages of 16, 138 MB in 40 us.  Prompts are
-// bound by what a compute unit issues: 2048 new tokens of 10240 take 313 us, 980 TFLOP/s, vector
+// bound by what a compute unit issues: 2048 new tokens of 10240 take 319 us, 970 TFLOP/s, vector
 // instructions 60% of the cycles, matrix cores 45%.  There the four wavefronts share what they read through
 // LDS, and the keys go into the products as they are: 421 us with neither, the load path and the
 // expansion the bounds.
@@ -766,7 +766,7 @@ Kv8Plan kv8_plan(int sequences, int q_heads, int heads, int dim, int max_new, in
   // for each step: small ones while all steps together are few.  us with 16, 32 and 128: 4 x 218 new tokens
   // of 5 heads 10.8, 12.2, 18.3; 1 x 699 of 2 x 4 heads 21, 15.6, 20; 6 x 308 of 4 x 4 heads 29, 23, 20;
   // 4 x 2000 of 8 x 4 heads 488, 308, 190.  Up to 64 rows a tile of 128 is mostly empty (8 x 9 tokens of
-  // 8 x 4 heads, 8000 long: 38 us with 32 rows, 52 with 128).
+  // 8 x 4 heads, with 32 and 128 rows: all 8000 long 46 and 49 us, of up to 8000 25 and 36).
   if (work(16) <= 8 * int64_t(num_cu))
     p.rows = 16;
   else if (rows > 16 && (rows <= 64 || work(32) <= 12 * int64_t(num_cu)))
