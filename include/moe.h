@@ -536,6 +536,105 @@ moe_status moe_kv8_attention(const void* q, int64_t T, int32_t q_heads, const mo
                              float scale, void* out, void* ws, size_t ws_bytes, moe_stream stream);
 
 /*
+ * The dense half of a layer in 8-bit integers: what runs before, after and beside the experts when
+ * every FLOP of a dense batch counts (Section 7's batch sizes; the shared experts and dense
+ * feed-forward blocks of the models of Section 6).  moe_norm_join gives the codes that moe_matmul_int8 and
+ * moe_gated_int8 read, moe_quantize_int8 those of any rows.
+ *
+ *   value[r][k] = scale[r] * code[r][k]      codes int8, a scale (f32) for each row
+ *
+ * A row is a token of the activations or an output channel of the weights.  Two representations:
+ *
+ *   row-major  i8 [rows, K]: activations, and weights as they are quantised
+ *   packed     weights as the products read them, rows padded to 16 and columns to 128 with zeros:
+ *              i8 [rows / 16][K / 64][1024]: byte 16 l + j of a piece is row l % 16, column
+ *              16 (l / 16) + j.  moe_int8_code_bytes gives the size
+ *
+ * Codes of a row of values v with m = max |v|:  scale = m / 127, code = round(v * (127 / m)), ties to
+ * even, each operation rounded to fp32 (rows with m < 2^-100 are multiplied by 2^100 first, so that
+ * 127 / m is finite); a row of zeros has scale 0.  A row that holds an infinity or a NaN gets the scale NaN
+ * and codes 0, so that its products show it.
+ */
+
+/*
+ * moe_norm_join - the joint between two blocks, in one pass over the residual stream: a block's output is
+ * normalised, gated, scaled and added to the stream, and the stream is normalised for the next block.
+ *
+ *   x'  = x + alpha * g * j       j = norm(y) * (offset + w_post) with post = 1, y with post = 0
+ *   z   = norm(x') * (offset + w_pre)                   norm(v) = v / sqrt(mean(v^2) + eps)
+ *
+ *   x           dt [T, H]      the stream, bf16 or f32
+ *   y           bf16 [T, H]    a block's output; NULL: x' = x, and post, w_post, gate and x_out are 0 or NULL
+ *   w_post, w_pre  bf16 [H]    NULL: factors of 1 (without offset).  offset: 0, or 1 for weights stored less 1
+ *   gate        bf16, by gate_kind: MOE_GATE_CHANNEL [H], MOE_GATE_TOKEN [T] (gate_stride elements
+ *               apart), MOE_GATE_FULL [T, H]; with sigmoid = 1 the gate is 1 / (1 + exp(-gate))
+ *   x_out       dt [T, H]      out: x'; may be x itself (then x_out_stride = x_stride)
+ *   z           out: bf16 [T, H], or with z_codes = 1 int8 [T, H] and z_scales f32 [T].  NULL: not computed
+ *   *_stride    elements from a row to the next, rows in whole 16-byte pieces
+ *
+ * Arithmetic is fp32, x' and z are rounded once; z is taken of x' before its rounding.  The codes of z
+ * are those of x' (offset + w_pre), the norm's factor is in the scale alone.  Squares are summed in fp32:
+ * rows of more than 2^60 in size overflow.  A NaN or infinity stays in its row.
+ * Errors: INVALID_ARGUMENT for H not a positive multiple of 8, T < 0, eps < 0, numbers that are not
+ * finite, flags that are not 0 or 1, an unknown gate_kind, bad strides, arguments without the one they belong to,
+ * null or misaligned pointers; UNSUPPORTED for H > 32768 or an unknown dtype.
+ */
+typedef enum { MOE_GATE_NONE = 0, MOE_GATE_CHANNEL = 1, MOE_GATE_TOKEN = 2, MOE_GATE_FULL = 3 } moe_gate;
+moe_status moe_norm_join(const void* x, int64_t x_stride, moe_dtype dt, const void* y, int64_t y_stride, int32_t post,
+                         const void* w_post, const void* gate, int64_t gate_stride, int32_t gate_kind, int32_t sigmoid,
+                         float alpha, const void* w_pre, float offset, float eps, int64_t T, int32_t H, void* x_out,
+                         int64_t x_out_stride, int32_t z_codes, void* z, float* z_scales, moe_stream stream);
+
+/*
+ * moe_quantize_int8 - bf16 rows to row-major codes and their scales.
+ *
+ *   src     bf16 [rows, K], src_stride elements from a row to the next (a multiple of 8)
+ *   codes   i8 [rows, K]  out;   scales  f32 [rows]  out
+ *
+ * Errors: INVALID_ARGUMENT for rows < 0, K not a positive multiple of 16, a bad stride, null or
+ * misaligned pointers; UNSUPPORTED for K > 131056.
+ */
+moe_status moe_quantize_int8(const void* src, int64_t src_stride, int64_t rows, int32_t K, int8_t* codes, float* scales,
+                             moe_stream stream);
+
+/*
+ * moe_pack_int8 - row-major to packed codes.  Run once when weights are loaded.
+ * Errors: as moe_quantize_int8; UNSUPPORTED for rows > 2^24 or 2^26 pieces of 1 KB.
+ */
+size_t moe_int8_code_bytes(int64_t rows, int32_t K);
+moe_status moe_pack_int8(const int8_t* codes, int64_t rows, int32_t K, int8_t* out, moe_stream stream);
+
+/*
+ * moe_matmul_int8 - y = x W^T (+ bias) of 8-bit codes, for one row as for large batches.
+ *
+ *   x, x_scales   row-major codes [T, K], f32 [T]
+ *   w, w_scales   packed codes [N, K], f32 [N]
+ *   bias          bf16 [N], or NULL
+ *   y             bf16 [T, N]  out:  x_scales[t] * w_scales[n] * sum_k x[t][k] w[n][k] + bias[n]
+ *   ws, ws_bytes  device scratch of at least moe_matmul_int8_workspace_bytes(); not to be shared by
+ *                 calls that overlap
+ *
+ * The integer sums are exact, so results depend neither on how a call is cut up nor on the other rows;
+ * scales and bias are applied in fp32 in this order, y is rounded once.  A token's NaN scale is
+ * in its row alone.
+ * Errors: INVALID_ARGUMENT for T < 0, N < 1, K not a positive multiple of 16, null or misaligned
+ * pointers; UNSUPPORTED for K > 131056, T > 2^20 or N > 2^24; WORKSPACE_TOO_SMALL.
+ *
+ * moe_gated_int8 - both projections of a gated block, its activation and product:
+ *   h[t][f] = silu(g) * u,   g = x Wg^T, u = x Wu^T as above, in fp32; h bf16 [T, F], rounded once.
+ *   wg, wu        packed codes [F, K]
+ * Errors as moe_matmul_int8.
+ */
+size_t moe_matmul_int8_workspace_bytes(int64_t T, int32_t N, int32_t K);
+moe_status moe_matmul_int8(const int8_t* x, const float* x_scales, const int8_t* w, const float* w_scales,
+                           const void* bias, int64_t T, int32_t N, int32_t K, void* y, void* ws, size_t ws_bytes,
+                           moe_stream stream);
+size_t moe_gated_int8_workspace_bytes(int64_t T, int32_t F, int32_t K);
+moe_status moe_gated_int8(const int8_t* x, const float* x_scales, const int8_t* wg, const float* wg_scales,
+                          const int8_t* wu, const float* wu_scales, int64_t T, int32_t F, int32_t K, void* h, void* ws,
+                          size_t ws_bytes, moe_stream stream);
+
+/*
  * Per-kernel timing (a benchmarking aid, not part of the layer).
  *
  * moe_profiler_start(capacity) creates `capacity` pairs of HIP events on the

@@ -25,6 +25,8 @@ __all__ = [
     "Int4", "moe_int4_code_bytes", "moe_int4_scale_bytes", "moe_quantize_int4", "moe_pack_int4", "quantize_weights_int4",
     "moe_matvec_int4", "moe_few_tokens", "moe_few_tokens_workspace_bytes", "MoELayerFew", "FEW_TOKENS",
     "KVCache8", "KV8_BLOCK", "moe_kv8_append", "moe_kv8_attention", "moe_kv8_attention_workspace_bytes",
+    "Int8", "moe_int8_code_bytes", "moe_quantize_int8", "moe_pack_int8", "quantize_weights_int8", "moe_norm_join",
+    "moe_matmul_int8", "moe_matmul_int8_workspace_bytes", "moe_gated_int8", "moe_gated_int8_workspace_bytes",
     "profiler_start", "profiler_select", "profiler_stop", "profiler_records", "set_cu_budget",
     "DTYPE_F32", "DTYPE_BF16",
 ]
@@ -104,6 +106,15 @@ _SIGNATURES = {
     "moe_kv8_attention_workspace_bytes": (_SZ, [_I64, _I32, _I32, _I32, _I32, _I32, _I32, _I32]),
     "moe_kv8_attention": (ctypes.c_int, [_P, _I64, _I32, ctypes.POINTER(_Kv8Cache), _P, _I32, _P, _P, _I32, _I32, _I32,
                                          _I32, ctypes.c_float, _P, _P, _SZ, _P]),
+    "moe_norm_join": (ctypes.c_int, [_P, _I64, ctypes.c_int, _P, _I64, _I32, _P, _P, _I64, _I32, _I32, ctypes.c_float, _P,
+                                     ctypes.c_float, ctypes.c_float, _I64, _I32, _P, _I64, _I32, _P, _P, _P]),
+    "moe_quantize_int8": (ctypes.c_int, [_P, _I64, _I64, _I32, _P, _P, _P]),
+    "moe_int8_code_bytes": (_SZ, [_I64, _I32]),
+    "moe_pack_int8": (ctypes.c_int, [_P, _I64, _I32, _P, _P]),
+    "moe_matmul_int8_workspace_bytes": (_SZ, [_I64, _I32, _I32]),
+    "moe_matmul_int8": (ctypes.c_int, [_P, _P, _P, _P, _P, _I64, _I32, _I32, _P, _P, _SZ, _P]),
+    "moe_gated_int8_workspace_bytes": (_SZ, [_I64, _I32, _I32]),
+    "moe_gated_int8": (ctypes.c_int, [_P, _P, _P, _P, _P, _P, _I64, _I32, _I32, _P, _P, _SZ, _P]),
     "moe_profiler_start": (ctypes.c_int, [ctypes.c_int]),
     "moe_profiler_select": (ctypes.c_int, [ctypes.c_char_p]),
     "moe_set_cu_budget": (ctypes.c_int, [_I32]),
@@ -668,6 +679,199 @@ def moe_kv8_attention(q, cache, block_table, seq_lens, cu_tokens, max_new, max_l
                                    dim ** -0.5 if scale is None else scale, out.data_ptr(), ws.data_ptr(), ws.numel(),
                                    _stream(stream, q.device)))
     return out
+
+
+# --------------------------------------------------------------------------- the dense half in 8-bit integers
+class Int8:
+    """A packed matrix [N, K] of 8-bit weights (include/moe.h): codes int8 in the library's tiled layout, scales
+    f32 [N].  The tensors are looked over here, once, and stay."""
+
+    def __init__(self, codes, scales, shape):
+        self.codes, self.scales = codes, scales
+        self.shape = N, K = tuple(shape)
+        if codes.dtype != torch.int8 or scales.dtype != torch.float32:
+            raise TypeError("packed codes are int8, scales float32")
+        if codes.numel() < moe_int8_code_bytes(N, K) or scales.shape != (N,):
+            raise ValueError(f"codes or scales do not fit 8-bit weights {self.shape}")
+        _on(codes.get_device(), codes, scales)
+
+
+def moe_int8_code_bytes(rows, K) -> int:
+    return lib().moe_int8_code_bytes(rows, K)
+
+
+def _on(index, *ts):
+    """All tensors are on the GPU of that index, and contiguous."""
+    for t in ts:
+        if t is not None and not (t.get_device() == index >= 0 and t.is_contiguous()):
+            raise ValueError("all tensors must be " + ("contiguous" if t.get_device() == index >= 0 else "on one GPU"))
+
+
+def _run(fn, index, stream, *args):
+    """A call on the GPU of that index, whichever is the current one."""
+    if index == torch._C._cuda_getDevice():
+        _check(fn(*args, torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream))
+        return
+    with torch.cuda.device(index):
+        _run(fn, index, stream, *args)
+
+
+def _matrix(t, name, T, H, dtypes, index):
+    """Row stride of a tensor [T, H] whose rows are in one piece."""
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} must be " + " or ".join(map(str, dtypes)))
+    if t.shape != (T, H):
+        raise ValueError(f"{name} must be [{T}, {H}]")
+    if t.get_device() != index or index < 0:
+        raise ValueError("all tensors must be on one GPU")
+    row, one = t.stride()
+    if one != 1 and H > 1:
+        raise ValueError(f"{name}: rows must be in one piece")
+    return row if T > 1 else H
+
+
+_BF16, _STREAMS = (torch.bfloat16,), (torch.bfloat16, torch.float32)
+
+
+def _weight(w, name, H, index):
+    """Address of a norm's weight: a tensor bf16 [H], or True for none."""
+    if w is True:
+        return None
+    if w.dtype != torch.bfloat16 or w.shape != (H,):
+        raise ValueError(f"{name} must be bf16 [{H}], or True")
+    _on(index, w)
+    return w.data_ptr()
+
+
+def moe_norm_join(x, y=None, post=None, gate=None, sigmoid=False, alpha=1.0, pre=None, offset=0.0, eps=1e-6, int8=False,
+                  x_out=None, z=None, scales=None, stream=None):
+    """The joint between two blocks: x' = x + alpha * gate * norm(y) * (offset + post), z = norm(x') * (offset + pre)
+    -> (x', z, scales).
+
+    x bf16 or f32 [T, H]; y bf16 [T, H], or None: x' is x.  post, pre: norm weights bf16 [H], True for a norm
+    without weights, None for no norm (no post: y as it is; no pre: no z).  gate: bf16 [H] or [1, H] (of the
+    channels), [T, 1] (of the tokens) or [T, H]; with T = 1 [1, H] counts for either.  sigmoid: of the gate.  int8:
+    z as codes with a scale for each row, else bf16 (scales None).  x_out may be x.  x, y, a gate [T, H] and
+    x_out may be slices with rows in one piece."""
+    T, H = x.shape
+    dev, index = x.device, x.get_device()
+    xs = _matrix(x, "x", T, H, _STREAMS, index)
+    yp = gp = post_w = op = None
+    ys = gs = os_ = kind = 0
+    if y is not None:
+        ys, yp = _matrix(y, "y", T, H, _BF16, index), y.data_ptr()
+        if gate is not None:
+            if gate.dtype != torch.bfloat16:
+                raise TypeError("gate must be bf16")
+            if gate.get_device() != index:
+                raise ValueError("all tensors must be on one GPU")
+            if gate.shape in ((H,), (1, H)):
+                kind, contiguous = 1, gate.stride(-1) == 1 or H == 1
+                if not contiguous:
+                    raise ValueError("gate: rows must be in one piece")
+            elif gate.shape == (T, 1):
+                kind, gs = 2, gate.stride(0) if T > 1 else 1
+            else:
+                kind, gs = 3, _matrix(gate, "gate", T, H, _BF16, index)
+            gp = gate.data_ptr()
+        if post is not None:
+            post_w = _weight(post, "post", H, index)
+        x_out = _like(x_out, "x_out", x.dtype, (T, H), dev, stream)
+        os_, op = _matrix(x_out, "x_out", T, H, _STREAMS, index), x_out.data_ptr()
+    elif post is not None or gate is not None or x_out is not None:
+        raise ValueError("post, gate and x_out need y")
+    pre_w = None
+    if pre is not None:
+        pre_w = _weight(pre, "pre", H, index)
+        z = _like(z, "z", torch.int8 if int8 else torch.bfloat16, (T, H), dev, stream)
+        if int8:
+            scales = _like(scales, "scales", torch.float32, (T,), dev, stream)
+        elif scales is not None:
+            raise ValueError("scales need int8")
+        _on(index, z, scales)
+    elif z is not None or scales is not None or int8:
+        raise ValueError("z, scales and int8 need pre")
+    _run(lib().moe_norm_join, index, stream, x.data_ptr(), xs, DTYPE_F32 if x.dtype == torch.float32 else DTYPE_BF16, yp,
+         ys, 0 if post is None else 1, post_w, gp, gs, kind, 1 if sigmoid else 0, alpha, pre_w, offset, eps, T, H, op,
+         os_, 1 if int8 else 0, None if z is None else z.data_ptr(), None if scales is None else scales.data_ptr())
+    return x if y is None else x_out, z, scales
+
+
+def moe_quantize_int8(src, codes=None, scales=None, stream=None):
+    """bf16 [T, K], rows in one piece -> (codes int8 [T, K], scales f32 [T])."""
+    T, K = src.shape
+    index = src.get_device()
+    row = _matrix(src, "src", T, K, _BF16, index)
+    codes = _like(codes, "codes", torch.int8, (T, K), src.device, stream)
+    scales = _like(scales, "scales", torch.float32, (T,), src.device, stream)
+    _on(index, codes, scales)
+    _run(lib().moe_quantize_int8, index, stream, src.data_ptr(), row, T, K, codes.data_ptr(), scales.data_ptr())
+    return codes, scales
+
+
+def moe_pack_int8(codes, scales, stream=None):
+    """Weights as row-major codes int8 [N, K] and scales f32 [N] -> Int8.  The scales are kept as they are."""
+    if codes.dtype != torch.int8:
+        raise TypeError("moe_pack_int8 takes int8 codes")
+    N, K = codes.shape
+    index = codes.get_device()
+    _on(index, codes)
+    out = Int8(_new(max(1, moe_int8_code_bytes(N, K)), torch.int8, codes.device, stream), scales, (N, K))
+    _run(lib().moe_pack_int8, index, stream, codes.data_ptr(), N, K, out.codes.data_ptr())
+    return out
+
+
+def quantize_weights_int8(w, stream=None):
+    """Weights bf16 [N, K] -> Int8: moe_quantize_int8, then moe_pack_int8."""
+    return moe_pack_int8(*moe_quantize_int8(w, stream=stream), stream=stream)
+
+
+def moe_matmul_int8_workspace_bytes(T, N, K) -> int:
+    return lib().moe_matmul_int8_workspace_bytes(T, N, K)
+
+
+def moe_gated_int8_workspace_bytes(T, F, K) -> int:
+    return lib().moe_gated_int8_workspace_bytes(T, F, K)
+
+
+def _int8_inputs(x, scales, w):
+    T, K = x.shape
+    if x.dtype != torch.int8 or scales.dtype != torch.float32:
+        raise TypeError("x is int8 codes, its scales float32")
+    if scales.shape != (T,) or w.shape[1] != K:
+        raise ValueError(f"scales {tuple(scales.shape)} or weights {w.shape} do not fit x [{T}, {K}]")
+    return T, w.shape[0], K
+
+
+def moe_matmul_int8(x, scales, w, bias=None, y=None, ws=None, stream=None):
+    """x codes int8 [T, K] and scales f32 [T], w Int8 [N, K], bias bf16 [N] or None -> y bf16 [T, N]."""
+    T, N, K = _int8_inputs(x, scales, w)
+    if bias is not None and (bias.dtype != torch.bfloat16 or bias.shape != (N,)):
+        raise ValueError(f"bias must be bf16 [{N}]")
+    y = _like(y, "y", torch.bfloat16, (T, N), x.device, stream)
+    if ws is None:
+        ws = _new(max(1, moe_matmul_int8_workspace_bytes(T, N, K)), torch.uint8, x.device, stream)
+    index = x.get_device()
+    _on(index, x, scales, w.codes, bias, y, ws)
+    _run(lib().moe_matmul_int8, index, stream, x.data_ptr(), scales.data_ptr(), w.codes.data_ptr(), w.scales.data_ptr(),
+         None if bias is None else bias.data_ptr(), T, N, K, y.data_ptr(), ws.data_ptr(), ws.numel())
+    return y
+
+
+def moe_gated_int8(x, scales, w_gate, w_up, h=None, ws=None, stream=None):
+    """x codes int8 [T, K] and scales f32 [T], w_gate and w_up Int8 [F, K] -> h = silu(x Wg^T) * (x Wu^T), bf16 [T, F]."""
+    T, F, K = _int8_inputs(x, scales, w_gate)
+    if w_up.shape != w_gate.shape:
+        raise ValueError(f"w_gate {w_gate.shape} and w_up {w_up.shape} differ")
+    h = _like(h, "h", torch.bfloat16, (T, F), x.device, stream)
+    if ws is None:
+        ws = _new(max(1, moe_gated_int8_workspace_bytes(T, F, K)), torch.uint8, x.device, stream)
+    index = x.get_device()
+    _on(index, x, scales, w_gate.codes, w_up.codes, h, ws)
+    _run(lib().moe_gated_int8, index, stream, x.data_ptr(), scales.data_ptr(), w_gate.codes.data_ptr(),
+         w_gate.scales.data_ptr(), w_up.codes.data_ptr(), w_up.scales.data_ptr(), T, F, K, h.data_ptr(), ws.data_ptr(),
+         ws.numel())
+    return h
 
 
 # --------------------------------------------------------------------------- scheduling

@@ -166,4 +166,25 @@ inline bool stream_nt(int64_t R, int E, int K, int N, bool swiglu, bool fp8, int
   return weight_bytes >= (int64_t(128) << 20) && GroupLoad(R, E).rows <= mr;
 }
 
+// ---- rows that a workgroup keeps in registers (norm.hip)
+
+// Threads of a workgroup, and vectors of 8 elements that each keeps of a row of n elements (n % 8 == 0).
+struct RowShape {
+  int threads, vectors;
+};
+inline RowShape row_shape(int n, int64_t rows, int num_cu) {
+  const int nvec = (n + 7) / 8;
+  if (rows <= 2 * int64_t(num_cu)) {     // few rows: a row's latency counts
+    for (int t : {64, 256, 512, 1024})
+      if (nvec <= t) return {t, 1};
+    if (nvec <= 2048) return {1024, 2};
+  }
+  for (int v : {1, 2, 4})
+    if (nvec <= 64 * v) return {64, v};
+  if (nvec <= 512) return {256, 2};
+  if (nvec <= 1024) return {256, 4};
+  if (nvec <= 2048) return {512, 4};
+  return {1024, nvec <= 4096 ? 4 : 16};
+}
+
 }  // namespace moe

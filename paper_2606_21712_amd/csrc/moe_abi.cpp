@@ -430,4 +430,71 @@ moe_status moe_kv8_attention(const void* q, int64_t T, int32_t q_heads, const mo
   return hip_status("moe_kv8_attention", moe::launch_kv8_attention(cache_of(*cache), b, a, plan, stream_of(stream)));
 }
 
+// ------------------------------------------------------------------ the dense half in 8-bit integers
+moe_status moe_norm_join(const void* x, int64_t x_stride, moe_dtype dt, const void* y, int64_t y_stride, int32_t post,
+                         const void* w_post, const void* gate, int64_t gate_stride, int32_t gate_kind, int32_t sigmoid,
+                         float alpha, const void* w_pre, float offset, float eps, int64_t T, int32_t H, void* x_out,
+                         int64_t x_out_stride, int32_t z_codes, void* z, float* z_scales, moe_stream stream) {
+  moe::Check c = moe::validate_norm_join(x, x_stride, dt, y, y_stride, post, w_post, gate, gate_stride, gate_kind,
+                                         sigmoid, alpha, w_pre, offset, eps, T, H, x_out, x_out_stride, z_codes, z,
+                                         z_scales);
+  if (!c.ok() || T == 0) return finish(c);
+  hipError_t err;
+  const int ncu = cu_count(&err);
+  if (err != hipSuccess) return hip_status("moe_norm_join", err);
+  const moe::NormJoin a = {x, x_stride, dt == MOE_DTYPE_F32, static_cast<const uint16_t*>(y), y_stride, post != 0,
+                           static_cast<const uint16_t*>(w_post), static_cast<const uint16_t*>(gate), gate_stride,
+                           gate_kind, sigmoid != 0, alpha, static_cast<const uint16_t*>(w_pre), offset, eps, T, H,
+                           x_out, x_out_stride, z_codes != 0, z, z_scales};
+  return hip_status("moe_norm_join", moe::launch_norm_join(a, ncu, stream_of(stream)));
+}
+
+moe_status moe_quantize_int8(const void* src, int64_t src_stride, int64_t rows, int32_t K, int8_t* codes, float* scales,
+                             moe_stream stream) {
+  moe::Check c = moe::validate_quantize_int8(src, src_stride, rows, K, codes, scales);
+  if (!c.ok() || rows == 0) return finish(c);
+  hipError_t err;
+  const int ncu = cu_count(&err);
+  if (err != hipSuccess) return hip_status("moe_quantize_int8", err);
+  return hip_status("moe_quantize_int8", moe::launch_quantize_int8(static_cast<const uint16_t*>(src), src_stride, rows, K,
+                                                                   codes, scales, ncu, stream_of(stream)));
+}
+
+size_t moe_int8_code_bytes(int64_t rows, int32_t K) { return moe::int8_code_bytes(rows, K); }
+
+moe_status moe_pack_int8(const int8_t* codes, int64_t rows, int32_t K, int8_t* out, moe_stream stream) {
+  moe::Check c = moe::validate_pack_int8(codes, rows, K, out);
+  if (!c.ok() || rows == 0) return finish(c);
+  return hip_status("moe_pack_int8", moe::launch_pack_int8(codes, rows, K, out, stream_of(stream)));
+}
+
+size_t moe_matmul_int8_workspace_bytes(int64_t, int32_t, int32_t) { return 0; }
+size_t moe_gated_int8_workspace_bytes(int64_t, int32_t, int32_t) { return 0; }
+
+moe_status moe_matmul_int8(const int8_t* x, const float* x_scales, const int8_t* w, const float* w_scales,
+                           const void* bias, int64_t T, int32_t N, int32_t K, void* y, void* ws, size_t ws_bytes,
+                           moe_stream stream) {
+  moe::Check c = moe::validate_matmul_int8(x, x_scales, w, w_scales, bias, T, N, K, y, ws, ws_bytes, 0);
+  if (!c.ok() || T == 0) return finish(c);
+  hipError_t err;
+  const int ncu = cu_count(&err);
+  if (err != hipSuccess) return hip_status("moe_matmul_int8", err);
+  const moe::Int8Product p = {x, x_scales, w, nullptr, w_scales, nullptr, static_cast<const uint16_t*>(bias),
+                              static_cast<uint16_t*>(y), int(T), N, K, (K + 127) / 128 * 2};
+  return hip_status("moe_matmul_int8", moe::launch_int8_product(p, ncu, stream_of(stream)));
+}
+
+moe_status moe_gated_int8(const int8_t* x, const float* x_scales, const int8_t* wg, const float* wg_scales,
+                          const int8_t* wu, const float* wu_scales, int64_t T, int32_t F, int32_t K, void* h, void* ws,
+                          size_t ws_bytes, moe_stream stream) {
+  moe::Check c = moe::validate_gated_int8(x, x_scales, wg, wg_scales, wu, wu_scales, T, F, K, h, ws, ws_bytes, 0);
+  if (!c.ok() || T == 0) return finish(c);
+  hipError_t err;
+  const int ncu = cu_count(&err);
+  if (err != hipSuccess) return hip_status("moe_gated_int8", err);
+  const moe::Int8Product p = {x, x_scales, wg, wu, wg_scales, wu_scales, nullptr, static_cast<uint16_t*>(h), int(T), F, K,
+                              (K + 127) / 128 * 2};
+  return hip_status("moe_gated_int8", moe::launch_int8_product(p, ncu, stream_of(stream)));
+}
+
 }  // extern "C"

@@ -173,4 +173,45 @@ size_t kv8_workspace_bytes(const Kv8Plan& p, int64_t tokens, int sequences, int 
 hipError_t launch_kv8_attention(const Kv8Cache& c, const Kv8Batch& b, const Kv8Attend& a, const Kv8Plan& p,
                                 hipStream_t s);
 
+// ---- the dense half of a layer in 8-bit integers (layouts in int8.h)
+enum { kGateNone = 0, kGateChannel = 1, kGateToken = 2, kGateFull = 3 };   // moe_gate
+struct NormJoin {
+  const void* x;                          // [T, H] bf16, or f32
+  int64_t x_stride;                       // elements from one row to the next
+  bool f32;
+  const uint16_t* y;                      // bf16 [T, H], or null
+  int64_t y_stride;
+  bool post;
+  const uint16_t* w_post;                 // bf16 [H], or null: ones
+  const uint16_t* gate;
+  int64_t gate_stride;
+  int gate_kind;
+  bool sigmoid;
+  float alpha;
+  const uint16_t* w_pre;                  // as w_post
+  float offset, eps;
+  int64_t T;
+  int H;
+  void* x_out;
+  int64_t x_out_stride;
+  bool codes;
+  void* z;                                // bf16 or int8 [T, H], or null
+  float* z_scales;
+};
+hipError_t launch_norm_join(const NormJoin& a, int num_cu, hipStream_t s);
+hipError_t launch_quantize_int8(const uint16_t* src, int64_t stride, int64_t rows, int K, int8_t* codes, float* scales,
+                                int num_cu, hipStream_t s);
+hipError_t launch_pack_int8(const int8_t* codes, int64_t rows, int K, int8_t* out, hipStream_t s);
+struct Int8Product {
+  const int8_t* x;                        // [T, K]
+  const float* x_scales;
+  const int8_t *w0, *w1;                  // packed [N, K]; w1: the gated form's up projection
+  const float *s0, *s1;
+  const uint16_t* bias;                   // bf16 [N], or null
+  uint16_t* y;                            // [T, N]
+  int T, N, K;
+  int steps;                              // of 64 columns, an even number
+};
+hipError_t launch_int8_product(const Int8Product& p, int num_cu, hipStream_t s);
+
 }  // namespace moe

@@ -654,4 +654,160 @@ Check validate_kv8_attention(const void* q, int64_t T, int32_t q_heads, const mo
   return Check{};
 }
 
+// ------------------------------------------------------------------ the dense half in 8-bit integers
+namespace {
+
+Check flag(const char* fn, const char* name, int32_t v) {
+  if (v == 0 || v == 1) return Check{};
+  return fail(MOE_ERR_INVALID_ARGUMENT, fn, (std::string(name) + "=%lld must be 0 or 1").c_str(), v);
+}
+
+// Elements from a row of H to the next: whole 16-byte pieces.
+Check stride_of(const char* fn, const char* name, int64_t stride, int32_t H, int per16) {
+  if (stride >= H && stride % per16 == 0 && stride < (int64_t(1) << 40)) return Check{};
+  return fail(MOE_ERR_INVALID_ARGUMENT, fn,
+              (std::string(name) + "=%lld must be at least the row's %lld elements, in pieces of 16 bytes").c_str(),
+              stride, H);
+}
+
+Check int8_cols(const char* fn, int32_t K) {
+  if (K < 1 || K % 16 != 0) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "K=%lld must be a positive multiple of 16", K);
+  if (K > kInt8MaxK) return fail(MOE_ERR_UNSUPPORTED, fn, "K=%lld exceeds %lld", K, kInt8MaxK);
+  return Check{};
+}
+
+constexpr int64_t kInt8MaxRows = int64_t(1) << 24;
+
+Check int8_sizes(const char* fn, int64_t T, int32_t N, int32_t K) {
+  MOE_TRY(int8_cols(fn, K));
+  if (T < 0) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "T=%lld is negative", T);
+  if (N < 1) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "N=%lld must be >= 1", N);
+  if (T > (1 << 20)) return fail(MOE_ERR_UNSUPPORTED, fn, "T=%lld exceeds %lld", T, 1 << 20);
+  if (N > kInt8MaxRows) return fail(MOE_ERR_UNSUPPORTED, fn, "N=%lld exceeds %lld", N, kInt8MaxRows);
+  return Check{};
+}
+
+Check int8_workspace(const char* fn, const void* ws, size_t ws_bytes, size_t need) {
+  if (ws_bytes < need)
+    return fail(MOE_ERR_WORKSPACE_TOO_SMALL, fn, "workspace %lld bytes < %lld needed", (long long)ws_bytes,
+                (long long)need);
+  if (need > 0) MOE_TRY(ptr(fn, "ws", ws));
+  return Check{};
+}
+
+}  // namespace
+
+Check validate_norm_join(const void* x, int64_t x_stride, int x_dt, const void* y, int64_t y_stride, int32_t post,
+                         const void* w_post, const void* gate, int64_t gate_stride, int32_t gate_kind, int32_t sigmoid,
+                         float alpha, const void* w_pre, float offset, float eps, int64_t T, int32_t H,
+                         const void* x_out, int64_t x_out_stride, int32_t z_codes, const void* z, const void* z_scales) {
+  const char* fn = "moe_norm_join";
+  MOE_TRY(dtype(fn, x_dt));
+  if (H < 1 || H % 8 != 0) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "H=%lld must be a positive multiple of 8", H);
+  if (H > kNormMaxH) return fail(MOE_ERR_UNSUPPORTED, fn, "H=%lld exceeds %lld", H, kNormMaxH);
+  if (T < 0) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "T=%lld is negative", T);
+  if (T > (int64_t(1) << 31)) return fail(MOE_ERR_UNSUPPORTED, fn, "T=%lld exceeds 2^31", T);
+  MOE_TRY(flag(fn, "post", post));
+  MOE_TRY(flag(fn, "sigmoid", sigmoid));
+  MOE_TRY(flag(fn, "z_codes", z_codes));
+  if (gate_kind < 0 || gate_kind > 3) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "unknown gate_kind=%lld", gate_kind);
+  if (!(eps >= 0.f) || eps > 1e30f) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "eps must be finite, and not negative");
+  if (!(alpha >= -1e30f && alpha <= 1e30f)) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "alpha must be finite");
+  if (!(offset >= -1e30f && offset <= 1e30f)) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "offset must be finite");
+  if (T == 0) return Check{};
+  const int per16 = x_dt == MOE_DTYPE_F32 ? 4 : 8;
+  MOE_TRY(ptr(fn, "x", x));
+  MOE_TRY(stride_of(fn, "x_stride", x_stride, H, per16));
+  if (y != nullptr) {
+    MOE_TRY(ptr(fn, "y", y));
+    MOE_TRY(stride_of(fn, "y_stride", y_stride, H, 8));
+    MOE_TRY(ptr(fn, "x_out", x_out));
+    MOE_TRY(stride_of(fn, "x_out_stride", x_out_stride, H, per16));
+    if (w_post != nullptr && !post) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "w_post without post");
+    if (w_post != nullptr) MOE_TRY(ptr(fn, "w_post", w_post));
+    if ((gate != nullptr) != (gate_kind != 0))
+      return fail(MOE_ERR_INVALID_ARGUMENT, fn, "gate and gate_kind=%lld do not fit", gate_kind);
+    if (gate != nullptr) MOE_TRY(ptr(fn, "gate", gate));
+    if (gate_kind == MOE_GATE_FULL) MOE_TRY(stride_of(fn, "gate_stride", gate_stride, H, 8));
+    if (gate_kind == MOE_GATE_TOKEN && (gate_stride < 1 || gate_stride >= (int64_t(1) << 40)))
+      return fail(MOE_ERR_INVALID_ARGUMENT, fn, "gate_stride=%lld must be >= 1", gate_stride);
+  } else if (post || w_post != nullptr || gate != nullptr || gate_kind != 0 || x_out != nullptr) {
+    return fail(MOE_ERR_INVALID_ARGUMENT, fn, "post, gate and x_out need y");
+  }
+  if (z == nullptr) {
+    if (y == nullptr) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "neither y nor z: nothing to do");
+    if (w_pre != nullptr || z_codes || z_scales != nullptr)
+      return fail(MOE_ERR_INVALID_ARGUMENT, fn, "w_pre, z_codes and z_scales need z");
+    return Check{};
+  }
+  MOE_TRY(ptr(fn, "z", z));
+  if (w_pre != nullptr) MOE_TRY(ptr(fn, "w_pre", w_pre));
+  if (z_codes) return ptr(fn, "z_scales", z_scales);
+  if (z_scales != nullptr) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "z_scales without z_codes");
+  return Check{};
+}
+
+size_t int8_code_bytes(int64_t rows, int32_t K) {
+  if (rows <= 0 || K <= 0 || rows > INT64_MAX / (int64_t(1) << 32)) return 0;
+  return up16(rows) * up128(K);
+}
+
+Check validate_quantize_int8(const void* src, int64_t src_stride, int64_t rows, int32_t K, const void* codes,
+                             const void* scales) {
+  const char* fn = "moe_quantize_int8";
+  MOE_TRY(int8_cols(fn, K));
+  if (rows < 0) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "rows=%lld is negative", rows);
+  if (rows > (int64_t(1) << 31)) return fail(MOE_ERR_UNSUPPORTED, fn, "rows=%lld exceeds 2^31", rows);
+  if (rows == 0) return Check{};
+  MOE_TRY(ptr(fn, "src", src));
+  MOE_TRY(stride_of(fn, "src_stride", src_stride, K, 8));
+  MOE_TRY(ptr(fn, "codes", codes));
+  return ptr(fn, "scales", scales);
+}
+
+Check validate_pack_int8(const void* codes, int64_t rows, int32_t K, const void* out) {
+  const char* fn = "moe_pack_int8";
+  MOE_TRY(int8_cols(fn, K));
+  if (rows < 0) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "rows=%lld is negative", rows);
+  // one workgroup of 64 threads a step of 16 rows x 64 columns, fewer than 2^32 threads
+  if (rows > kInt8MaxRows || int64_t(up16(rows)) / 16 > (int64_t(1) << 26) / (int64_t(up128(K)) / 64) - 1)
+    return fail(MOE_ERR_UNSUPPORTED, fn, "rows=%lld of K=%lld are too many", rows, K);
+  if (rows == 0) return Check{};
+  MOE_TRY(ptr(fn, "codes", codes));
+  return ptr(fn, "out", out);
+}
+
+bool int8_sizes_ok(int64_t T, int32_t N, int32_t K) { return T > 0 && int8_sizes("", T, N, K).ok(); }
+
+Check validate_matmul_int8(const void* x, const void* x_scales, const void* w, const void* w_scales, const void* bias,
+                           int64_t T, int32_t N, int32_t K, const void* y, const void* ws, size_t ws_bytes,
+                           size_t need) {
+  const char* fn = "moe_matmul_int8";
+  MOE_TRY(int8_sizes(fn, T, N, K));
+  if (T == 0) return Check{};
+  MOE_TRY(ptr(fn, "x", x));
+  MOE_TRY(ptr(fn, "x_scales", x_scales));
+  MOE_TRY(ptr(fn, "w", w));
+  MOE_TRY(ptr(fn, "w_scales", w_scales));
+  if (bias != nullptr) MOE_TRY(ptr(fn, "bias", bias));
+  MOE_TRY(ptr(fn, "y", y));
+  return int8_workspace(fn, ws, ws_bytes, need);
+}
+
+Check validate_gated_int8(const void* x, const void* x_scales, const void* wg, const void* wg_scales, const void* wu,
+                          const void* wu_scales, int64_t T, int32_t F, int32_t K, const void* h, const void* ws,
+                          size_t ws_bytes, size_t need) {
+  const char* fn = "moe_gated_int8";
+  MOE_TRY(int8_sizes(fn, T, F, K));
+  if (T == 0) return Check{};
+  MOE_TRY(ptr(fn, "x", x));
+  MOE_TRY(ptr(fn, "x_scales", x_scales));
+  MOE_TRY(ptr(fn, "wg", wg));
+  MOE_TRY(ptr(fn, "wg_scales", wg_scales));
+  MOE_TRY(ptr(fn, "wu", wu));
+  MOE_TRY(ptr(fn, "wu_scales", wu_scales));
+  MOE_TRY(ptr(fn, "h", h));
+  return int8_workspace(fn, ws, ws_bytes, need);
+}
+
 }  // namespace moe

@@ -97,4 +97,20 @@ Check validate_kv8_attention(const void* q, int64_t T, int32_t q_heads, const mo
 bool kv8_plan_sizes_ok(int32_t B, int32_t q_heads, int32_t heads, int32_t dim, int32_t max_new, int32_t max_len,
                        int32_t window);
 
+// The dense half of a layer in 8-bit integers
+Check validate_norm_join(const void* x, int64_t x_stride, int x_dt, const void* y, int64_t y_stride, int32_t post,
+                         const void* w_post, const void* gate, int64_t gate_stride, int32_t gate_kind, int32_t sigmoid,
+                         float alpha, const void* w_pre, float offset, float eps, int64_t T, int32_t H,
+                         const void* x_out, int64_t x_out_stride, int32_t z_codes, const void* z, const void* z_scales);
+size_t int8_code_bytes(int64_t rows, int32_t K);
+Check validate_quantize_int8(const void* src, int64_t src_stride, int64_t rows, int32_t K, const void* codes,
+                             const void* scales);
+Check validate_pack_int8(const void* codes, int64_t rows, int32_t K, const void* out);
+Check validate_matmul_int8(const void* x, const void* x_scales, const void* w, const void* w_scales, const void* bias,
+                           int64_t T, int32_t N, int32_t K, const void* y, const void* ws, size_t ws_bytes, size_t need);
+Check validate_gated_int8(const void* x, const void* x_scales, const void* wg, const void* wg_scales, const void* wu,
+                          const void* wu_scales, int64_t T, int32_t F, int32_t K, const void* h, const void* ws,
+                          size_t ws_bytes, size_t need);
+bool int8_sizes_ok(int64_t T, int32_t N, int32_t K);
+
 }  // namespace moe

@@ -37,4 +37,9 @@ constexpr int kFewParts = 512;
 constexpr int kFewMostParts = 16;
 constexpr int kFewMaxCols = 64;
 
+// Products of 8-bit codes: K up to which sums of 128 * 128 stay inside 32 bits, and the longest row that
+// a norm keeps in registers.
+constexpr int kInt8MaxK = 131056;
+constexpr int kNormMaxH = 32768;
+
 }  // namespace moe

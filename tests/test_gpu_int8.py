@@ -1,0 +1,451 @@
+"""The dense half of a layer in 8-bit integers on the GPU: codes, packing and integer products bit for bit against
+plain implementations, the gated products and the norms against 64 bits, each alone and all in a row."""
+from __future__ import annotations
+
+import itertools
+
+import pytest
+import torch
+
+import paper_2606_21712_amd as moe
+from gpu_util import log
+
+pytestmark = pytest.mark.gpu
+BF, F32, F64 = torch.bfloat16, torch.float32, torch.float64
+BF_ROUND = 2.0 ** -8            # a rounding to bf16, relative to the value
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def bits(t):
+    return t.contiguous().view({2: torch.int16, 4: torch.int32, 1: torch.int8}[t.element_size()])
+
+
+# --------------------------------------------------------------------------- rows to codes
+def codes_plain(v):
+    """The definition on the host in fp32, whose division is correctly rounded."""
+    m = v.abs().amax(1)
+    fine = m.isfinite()                                       # NaN is the largest of its row
+    up = torch.where(m < 2.0 ** -100, 2.0 ** 100, 1.0)
+    inverse = torch.where(m > 0, torch.tensor(127.0) / (m * up), torch.tensor(0.0))
+    q = torch.round(v * up[:, None] * inverse[:, None])
+    q = torch.where(fine[:, None], q, 0.0).to(torch.int8)
+    return q, torch.where(fine, m / 127, float("nan"))
+
+
+def rows_of_all_kinds(T, K, seed):
+    v = torch.randn(T, K, generator=gen(seed)) * torch.logspace(-6, 6, T)[:, None]
+    special = [torch.zeros(K), torch.full((K,), -3.0), torch.arange(K) % 3 - 1.0, torch.randn(K, generator=gen(seed)) * 2.0 ** -130,
+               torch.full((K,), 2.0 ** -133), torch.full((K,), 3.0e38)]
+    special[2][K // 2] = 2.0                                    # halves of 127: ties
+    for i, s in enumerate(special[:max(0, T - 1)]):
+        v[i] = s
+    return v.to(BF)
+
+
+@pytest.mark.parametrize("T,K", [(1, 16), (7, 48), (9, 512), (700, 528), (700, 1024), (600, 2048), (9, 4096), (550, 4112),
+                                 (530, 8192), (9, 8208), (520, 16384), (11, 16400), (515, 32768), (3, 131056)])
+def test_quantize(T, K):
+    """Bit for bit, with rows of zeros, one value, ties, subnormal and huge values among them."""
+    log(f"[gpu] quantize int8 {T}x{K}")
+    v = rows_of_all_kinds(T, K, K)
+    codes, scales = moe.moe_quantize_int8(v.cuda())
+    q, s = codes_plain(v.float())
+    assert torch.equal(codes.cpu(), q)
+    assert torch.equal(bits(scales.cpu()), bits(s))
+
+
+def test_quantize_rows_that_are_not_finite():
+    log("[gpu] quantize int8: infinities and NaN")
+    v = torch.randn(6, 4096, generator=gen(1)).to(BF)
+    v[1, 5], v[2, 4095], v[3, 0], v[4, 77], v[4, 78] = float("inf"), float("-inf"), float("nan"), float("nan"), float("inf")
+    codes, scales = (t.cpu() for t in moe.moe_quantize_int8(v.cuda()))
+    assert scales[1:5].isnan().all() and not codes[1:5].any()
+    q, s = codes_plain(v[[0, 5]].float())
+    assert torch.equal(codes[[0, 5]], q) and torch.equal(scales[[0, 5]], s)
+
+
+def test_quantize_slices_buffers_and_streams():
+    log("[gpu] quantize int8: slices, buffers, streams")
+    wide = torch.randn(33, 1000, generator=gen(2)).to(BF).cuda()
+    part = wide[:, 200:200 + 528]
+    q, s = codes_plain(part.cpu().float())
+    codes = torch.full((35, 528), 99, dtype=torch.int8, device="cuda")
+    scales = torch.full((35,), 99.0, device="cuda")
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    c2, s2 = moe.moe_quantize_int8(part, codes=codes[1:34], scales=torch.empty(33, device="cuda"), stream=st)
+    torch.cuda.synchronize()
+    assert torch.equal(c2.cpu(), q) and torch.equal(s2.cpu(), s)
+    assert (codes[[0, 34]] == 99).all() and (scales == 99).all()       # what lies beside is left alone
+    assert moe.moe_quantize_int8(part[:0])[0].shape == (0, 528)
+
+
+# --------------------------------------------------------------------------- packed weights
+def random_int8(N, K, seed):
+    return (torch.randint(-128, 128, (N, K), generator=gen(seed), dtype=torch.int8),
+            (torch.rand(N, generator=gen(seed + 1)) + 0.5) * K ** -0.5 / 64)
+
+
+def packed_plain(q):
+    N, K = q.shape
+    full = torch.zeros((-(-N // 16) * 16, -(-K // 128) * 128), dtype=torch.int8)
+    full[:N, :K] = q
+    t = full.reshape(full.shape[0] // 16, 16, full.shape[1] // 64, 4, 16)      # tile, row, step, chunk, byte
+    return t.permute(0, 2, 3, 1, 4).reshape(-1)
+
+
+@pytest.mark.parametrize("N,K", [(1, 16), (16, 64), (17, 128), (100, 144), (33, 1008), (5, 16384)])
+def test_pack(N, K):
+    log(f"[gpu] pack int8 {N}x{K}")
+    q, s = random_int8(N, K, N)
+    w = moe.moe_pack_int8(q.cuda(), s.cuda())
+    assert w.codes.numel() == moe.moe_int8_code_bytes(N, K) and w.shape == (N, K)
+    assert torch.equal(w.codes.cpu(), packed_plain(q))
+    # from bf16: the same codes as quantising and packing by hand
+    b = torch.randn(N, K, generator=gen(K)).to(BF)
+    v = moe.quantize_weights_int8(b.cuda())
+    assert torch.equal(v.codes.cpu(), packed_plain(codes_plain(b.float())[0]))
+    assert torch.equal(v.scales.cpu(), codes_plain(b.float())[1])
+
+
+# --------------------------------------------------------------------------- products
+def sums(x, w):
+    """Exact: fp64 holds integers to 2^53."""
+    return (x.cuda().double() @ w.cuda().double().T).cpu()
+
+
+def matmul_plain(x, sx, w, sw, bias=None):
+    """fp32 operation by operation, as the contract says: bit for bit."""
+    y = sums(x, w).float() * sx[:, None] * sw
+    return (y if bias is None else y + bias.float()).to(BF)
+
+
+SHAPES = [(1, 16), (16, 64), (31, 128), (100, 144), (257, 1008), (129, 4096), (1003, 2064), (2052, 640), (64, 16384)]
+ROWS = [1, 2, 5, 16, 17, 31, 33, 48, 63, 64, 65, 100, 127, 128, 129, 200, 256, 257, 300, 511, 700]
+
+
+@pytest.mark.parametrize("T", ROWS)
+@pytest.mark.parametrize("N,K", SHAPES)
+def test_matmul(T, N, K):
+    """Bit for bit: the sums are exact, the scales' and the bias's fp32 roundings are the contract's."""
+    log(f"[gpu] matmul int8 T={T} {N}x{K}")
+    x, sx = random_int8(T, K, T + 1)
+    w, sw = random_int8(N, K, N + K)
+    bias = torch.randn(N, generator=gen(N)).to(BF) if (T + N) % 2 else None
+    y = moe.moe_matmul_int8(x.cuda(), sx.cuda(), moe.moe_pack_int8(w.cuda(), sw.cuda()), None if bias is None else bias.cuda())
+    assert torch.equal(bits(y.cpu()), bits(matmul_plain(x, sx, w, sw, bias)))
+
+
+def gated_tolerance(g, u, h):
+    """One rounding to bf16; g, u and their product a few fp32 roundings; exp(-g) is exp2 of a product
+    whose rounding it magnifies by |g|, plus the reciprocal.  Beyond |g| = 88 exp overflows and h is 0, off by under
+    88 e^-88 |u|."""
+    return BF_ROUND * h.abs() * 1.001 + (g.abs() + 16) * 2.0 ** -23 * h.abs() + 1e-36 * (1 + u.abs())
+
+
+@pytest.mark.parametrize("T", ROWS)
+@pytest.mark.parametrize("F,K", SHAPES)
+def test_gated(T, F, K):
+    log(f"[gpu] gated int8 T={T} {F}x{K}")
+    x, sx = random_int8(T, K, T + 1)
+    (wg, sg), (wu, su) = random_int8(F, K, F), random_int8(F, K, F + 7)
+    sg[::3] *= 40                                               # gates far out on both sides
+    h = moe.moe_gated_int8(x.cuda(), sx.cuda(), moe.moe_pack_int8(wg.cuda(), sg.cuda()), moe.moe_pack_int8(wu.cuda(), su.cuda()))
+    g, u = (sums(x, w) * sx.double()[:, None] * s.double() for w, s in ((wg, sg), (wu, su)))
+    ref = g * torch.sigmoid(g) * u
+    err = (h.cpu().double() - ref).abs()
+    assert (err <= gated_tolerance(g, u, ref)).all(), float((err / gated_tolerance(g, u, ref)).max())
+
+
+@pytest.mark.parametrize("T", [1, 40, 300])
+def test_products_at_their_largest_sums(T):
+    """All codes -128 and K as long as it may be: 2^31 - 2^18 in a sum."""
+    log(f"[gpu] int8 products: largest sums, T={T}")
+    K, N = 131056, 48
+    x = torch.full((T, K), -128, dtype=torch.int8, device="cuda")
+    w = torch.full((N, K), -128, dtype=torch.int8, device="cuda")
+    one = torch.ones(max(T, N), device="cuda")
+    y = moe.moe_matmul_int8(x, one[:T], moe.moe_pack_int8(w, one[:N]))
+    assert (y.float() == torch.tensor(float(K * 128 * 128)).to(BF).float().item()).all()
+
+
+@pytest.mark.parametrize("T", [3, 20, 90, 400])
+def test_products_keep_rows_apart(T):
+    """NaN and infinite scales stay in their row and their channel; a zero sum times infinity is NaN."""
+    log(f"[gpu] int8 products: scales that are not finite, T={T}")
+    x, sx = random_int8(T, 256, 5)
+    w, sw = random_int8(70, 256, 6)
+    sx[1], sw[3] = float("nan"), float("inf")
+    y = moe.moe_matmul_int8(x.cuda(), sx.cuda(), moe.moe_pack_int8(w.cuda(), sw.cuda())).cpu()
+    assert y[1].isnan().all() and not y[[i for i in range(T) if i != 1]][:, [i for i in range(70) if i != 3]].isnan().any()
+    ref = matmul_plain(x, sx, w, sw)
+    assert torch.equal(y.isnan(), ref.isnan()) and torch.equal(y.nan_to_num(7.0, 8.0, 9.0), ref.nan_to_num(7.0, 8.0, 9.0))
+
+
+def test_products_streams_buffers_and_neighbours():
+    """Another stream, given buffers, and what lies around the output."""
+    log("[gpu] int8 products: streams, buffers")
+    for T in (5, 40, 150, 300):
+        x, sx = (t.cuda() for t in random_int8(T, 512, T))
+        w = moe.moe_pack_int8(*(t.cuda() for t in random_int8(203, 512, 3)))
+        y0, h0 = moe.moe_matmul_int8(x, sx, w), moe.moe_gated_int8(x, sx, w, w)
+        around = [torch.full((T + 16, 203), 5.0, dtype=BF, device="cuda") for _ in range(2)]
+        y1, h1 = (a[8:8 + T] for a in around)                           # 16-byte aligned, as 8 rows are whole pieces
+        st = torch.cuda.Stream()
+        st.wait_stream(torch.cuda.current_stream())
+        moe.moe_matmul_int8(x, sx, w, y=y1, stream=st)
+        moe.moe_gated_int8(x, sx, w, w, h=h1, stream=st)
+        torch.cuda.synchronize()
+        assert torch.equal(bits(y0), bits(y1)) and torch.equal(bits(h0), bits(h1))
+        assert all((a[:8] == 5).all() and (a[8 + T:] == 5).all() for a in around)
+    assert moe.moe_matmul_int8(x[:0], sx[:0], w).shape == (0, 203)
+    assert moe.moe_gated_int8(x[:0], sx[:0], w, w).shape == (0, 203)
+
+
+def test_product_rows_do_not_depend_on_the_batch():
+    """A token's outputs are the same bits alone and in any batch: the sums are exact."""
+    log("[gpu] int8 products: batches")
+    x, sx = (t.cuda() for t in random_int8(700, 1040, 9))
+    w, v = (moe.moe_pack_int8(*(t.cuda() for t in random_int8(600, 1040, i))) for i in (10, 11))
+    y, h = moe.moe_matmul_int8(x, sx, w), moe.moe_gated_int8(x, sx, w, v)
+    for T in (1, 16, 30, 64, 100, 250, 400):
+        assert torch.equal(bits(moe.moe_matmul_int8(x[:T], sx[:T], w)), bits(y[:T])), T
+        assert torch.equal(bits(moe.moe_gated_int8(x[:T], sx[:T], w, v)), bits(h[:T])), T
+
+
+@pytest.mark.parametrize("T,N,K", [(140000, 40, 16384), (150000, 16384, 64)])
+def test_products_past_32_bits(T, N, K):
+    """Offsets into x, and into y, that pass 2^31 elements: the last rows, and some between."""
+    log(f"[gpu] matmul int8 T={T} {N}x{K}")
+    x = torch.randint(-128, 128, (T, K), dtype=torch.int8, device="cuda")
+    sx = torch.rand(T, device="cuda") + 0.5
+    w, sw = random_int8(N, K, 1)
+    y = moe.moe_matmul_int8(x, sx, moe.moe_pack_int8(w.cuda(), sw.cuda()))
+    at = torch.tensor([0, 1, T // 2, T - 300, T - 2, T - 1])
+    assert torch.equal(bits(y[at.cuda()].cpu()), bits(matmul_plain(x[at.cuda()].cpu(), sx[at.cuda()].cpu(), w, sw)))
+
+
+# --------------------------------------------------------------------------- the norms
+def norm64(v, w, offset, eps):
+    n = v / (v.square().mean(1, keepdim=True) + eps).sqrt()
+    return n if w is True else n * (offset + w.double())
+
+
+def join64(x, y, post, gate, sigmoid, alpha, pre, offset, eps):
+    """x', z, and the sizes that errors are relative to: |x| + |alpha g j|."""
+    x = x.double()
+    size = x.abs()
+    if y is not None:
+        j = y.double() if post is None else norm64(y.double(), post, offset, eps)
+        if gate is not None:
+            j = j * (torch.sigmoid(gate.double()) if sigmoid else gate.double())
+        size = size + (alpha * j).abs()
+        x = x + alpha * j
+    return x, None if pre is None else norm64(x, pre, offset, eps), size
+
+
+# fp32 through a row of 32768 at most: a thread's 32 squares and a tree of 10, 42 roundings of 2^-24 halved by the square
+# root, twice; exp, products and reciprocals some 20 more
+FP32 = 2.0 ** -18
+
+
+def check_join(got, x, y, post, gate, sigmoid, alpha, pre, offset, eps, int8):
+    xo, z, scales = got
+    x64, z64, size = join64(x, y, post, gate, sigmoid, alpha, pre, offset, eps)
+    if y is not None:
+        err = (xo.cpu().double() - x64).abs()
+        tol = FP32 * size + (BF_ROUND if x.dtype == BF else 2.0 ** -24) * x64.abs()
+        assert (err <= tol).all(), float((err / tol).max())
+    if pre is None:
+        assert z is None and scales is None
+        return
+    unit = 1 / (x64.square().mean(1, keepdim=True) + eps).sqrt()
+    fine = 2 * FP32 * size * unit * (1 if pre is True else (offset + pre.double()).abs())   # of z before it is rounded
+    if int8:
+        s = scales.cpu().double()[:, None]
+        top = z64.abs().amax(1, keepdim=True)
+        assert ((s - top / 127).abs() <= fine.amax(1, keepdim=True) / 100).all()
+        assert z.cpu().int().abs().max() <= 127
+        err, tol = (z.cpu().double() * s - z64).abs(), 0.5001 * s + 2 * fine + 1e-40
+    else:
+        err, tol = (z.cpu().double() - z64).abs(), fine + BF_ROUND * z64.abs()
+    assert (err <= tol).all(), float((err / tol).max())
+
+
+def join_inputs(T, H, dt, seed, gate=None):
+    g = gen(seed)
+    x = (torch.randn(T, H, generator=g) * torch.where(torch.rand(H, generator=g) < 0.02, 30.0, 1.5)).to(dt)
+    y = (torch.randn(T, H, generator=g) * torch.logspace(-2, 2, T)[:, None]).to(BF)
+    w1, w2 = ((1 + 0.3 * torch.randn(H, generator=g)).to(BF) for _ in range(2))
+    shape = dict(none=None, vector=(H,), channel=(1, H), token=(T, 1), full=(T, H))[gate or "none"]
+    return x, y, w1, w2, None if shape is None else torch.randn(shape, generator=g).to(BF)
+
+
+def cuda(*ts):
+    return [t.cuda() if isinstance(t, torch.Tensor) else t for t in ts]
+
+
+def join(x, y, post, gate, sigmoid, alpha, pre, offset, eps, int8, **kw):
+    x, y, post, gate, pre = cuda(x, y, post, gate, pre)
+    return moe.moe_norm_join(x, y, post=post, gate=gate, sigmoid=sigmoid, alpha=alpha, pre=pre, offset=offset, eps=eps,
+                             int8=int8, **kw)
+
+
+@pytest.mark.parametrize("T,H", [(1, 8), (5, 512), (3, 520), (700, 256), (600, 1000), (600, 2048), (2, 4096), (530, 4096),
+                                 (550, 7168), (9, 8192), (7, 11000), (520, 11008), (4, 16392), (513, 32768)])
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("int8", [False, True])
+def test_norm_join(T, H, dt, int8):
+    """Every size of workgroup, one row and many, both streams, both outputs."""
+    log(f"[gpu] norm_join {T}x{H} {dt} int8={int8}")
+    x, y, w1, w2, _ = join_inputs(T, H, dt, T + H)
+    args = (x, y, w1, None, False, 1.0, w2, 0.0, 1e-6, int8)
+    check_join(join(*args), *args)
+
+
+@pytest.mark.parametrize("gate", ["none", "vector", "channel", "token", "full"])
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("post,pre", [("w", "w"), (None, "w"), (True, True), ("w", None), (None, None)])
+def test_norm_join_forms(gate, sigmoid, post, pre):
+    """Each gate, with and without its sigmoid, and norms with weights, without, and none."""
+    for T, H, dt, offset, alpha, int8 in [(37, 776, BF, 0.0, 0.5, False), (600, 512, F32, 1.0, -1.25, pre is not None),
+                                          (1, 4096, BF, 1.0, 1.0, False)]:
+        log(f"[gpu] norm_join gate={gate} sigmoid={sigmoid} post={post} pre={pre} {T}x{H}")
+        x, y, w1, w2, g = join_inputs(T, H, dt, 3, gate)
+        args = (x, y, w1 if post == "w" else post, g, sigmoid, alpha, w2 if pre == "w" else pre, offset, 1e-5, int8)
+        check_join(join(*args), *args)
+
+
+@pytest.mark.parametrize("int8", [False, True])
+def test_norm_alone(int8):
+    """Without a block's output: the first norm of a model; the stream stays what it is."""
+    log(f"[gpu] norm alone int8={int8}")
+    x, _, _, w, _ = join_inputs(19, 1536, BF, 8)
+    args = (x, None, None, None, False, 1.0, w, 0.0, 1e-6, int8)
+    got = join(*args)
+    check_join(got, *args)
+    assert torch.equal(bits(got[0].cpu()), bits(x))
+
+
+def test_norm_join_slices_in_place_and_streams():
+    """Rows of wider tensors, the stream written over itself, given buffers, another stream: the same bits."""
+    log("[gpu] norm_join: slices, in place")
+    T, H = 45, 1024
+    for dt in (BF, F32):
+        x, y, w1, w2, g = cuda(*join_inputs(T, H, dt, 4, "full"))
+        want = moe.moe_norm_join(x, y, post=w1, gate=g, pre=w2)
+        wide_x = torch.zeros(T, 3 * H, dtype=dt, device="cuda")
+        wide_y, wide_g = torch.zeros(T, H + 64, dtype=BF, device="cuda"), torch.zeros(T, 2 * H, dtype=BF, device="cuda")
+        sx, sy, sg = wide_x[:, H:2 * H], wide_y[:, 64:], wide_g[:, :H]
+        for dst, src in ((sx, x), (sy, y), (sg, g)):
+            dst.copy_(src)
+        out = torch.full((T, 2 * H), 7.0, dtype=dt, device="cuda")
+        z = torch.empty(T, H, dtype=BF, device="cuda")
+        st = torch.cuda.Stream()
+        st.wait_stream(torch.cuda.current_stream())
+        moe.moe_norm_join(sx, sy, post=w1, gate=sg, pre=w2, x_out=out[:, H:], z=z, stream=st)
+        torch.cuda.synchronize()
+        assert torch.equal(bits(out[:, H:]), bits(want[0])) and torch.equal(bits(z), bits(want[1]))
+        assert (out[:, :H] == 7).all() and not wide_x[:, :H].any() and not wide_x[:, 2 * H:].any()
+        got = moe.moe_norm_join(sx, sy, post=w1, gate=sg, pre=w2, x_out=sx)
+        assert got[0] is sx and torch.equal(bits(sx), bits(want[0])) and torch.equal(bits(got[1]), bits(want[1]))
+        tok = torch.randn(T, 24, device="cuda").to(BF)
+        a = moe.moe_norm_join(x, y, gate=tok[:, 8:9], pre=w2)[1]
+        b = moe.moe_norm_join(x, y, gate=tok[:, 8:9].contiguous(), pre=w2)[1]
+        assert torch.equal(bits(a), bits(b))
+    assert moe.moe_norm_join(x[:0], y[:0], pre=w2)[1].shape == (0, H)
+
+
+@pytest.mark.parametrize("T,H", [(6, 512), (6, 4096), (600, 2048)])
+def test_norm_join_values_that_are_not_finite(T, H):
+    """A NaN or an infinity shows in its row (as the scale NaN for codes) and nowhere else; rows of zeros are zeros."""
+    log(f"[gpu] norm_join: NaN and infinities {T}x{H}")
+    x, y, w1, w2, _ = join_inputs(T, H, BF, 12)
+    x[1, 3], y[2, H - 1], x[4, 0] = float("nan"), float("inf"), float("inf")
+    x[3], y[3] = 0, 0
+    good = [i for i in range(T) if i not in (1, 2, 4)]
+    for int8 in (False, True):
+        args = (x, y, w1, None, False, 1.0, w2, 0.0, 1e-6, int8)
+        xo, z, scales = join(*args)
+        if int8:
+            s = scales.cpu()
+            assert s[[1, 2, 4]].isnan().all() and not z[[1, 2, 4]].any() and s[3] == 0 and not z[3].any()
+        else:
+            assert z[1].isnan().all() and z[2].isnan().any() and z[4].isnan().any() and not z[3].any()
+        check_join((xo[good], z[good], scales[good] if int8 else None), x[good], y[good], w1, None, False, 1.0, w2, 0.0, 1e-6,
+                   int8)
+
+
+def test_norm_join_past_32_bits():
+    """Rows that begin past 2^31 elements."""
+    T, H = 300000, 8192
+    log(f"[gpu] norm_join {T}x{H}")
+    x = torch.randn(T, H, dtype=BF, device="cuda")
+    y = torch.randn(T, H, dtype=BF, device="cuda")
+    w = torch.ones(H, dtype=BF)
+    xo, z, s = moe.moe_norm_join(x, y, post=w.cuda(), pre=w.cuda(), int8=True)
+    at = torch.tensor([0, T // 2, T - 1]).cuda()
+    check_join((xo[at], z[at], s[at]), x[at].cpu(), y[at].cpu(), w, None, False, 1.0, w, 0.0, 1e-6, True)
+
+
+# --------------------------------------------------------------------------- together
+def block(x, y, w, out=None):
+    """A dense feed-forward block as it is used: from the last block's output y and the stream x to its own."""
+    x, z, s = moe.moe_norm_join(x, y, post=w["post"], pre=w["pre"], int8=True)
+    h = moe.moe_gated_int8(z, s, w["gate"], w["up"])
+    return x, moe.moe_matmul_int8(*moe.moe_quantize_int8(h), w["down"], y=out), h
+
+
+def block_weights(H, F, seed):
+    def w(n, k, i):
+        return (torch.randn(n, k, generator=gen(seed + i)) * k ** -0.5).to(BF).cuda()
+    v = dict(gate=w(F, H, 0), up=w(F, H, 1), down=w(H, F, 2))
+    return (v, dict({k: moe.quantize_weights_int8(t) for k, t in v.items()}, pre=torch.ones(H, dtype=BF, device="cuda"),
+                    post=torch.ones(H, dtype=BF, device="cuda")))
+
+
+@pytest.mark.parametrize("T", [1, 13, 64, 200, 600])
+def test_block(T):
+    """All operators in a row against the same block in 64 bits without any codes.  Codes are off by half a step, a 254th
+    of the row's largest, 4 deviations or so out: 0.5 / sqrt(3) * 4 / 127 = 0.9% of the rows' size for each of the four
+    quantised operands of a product chain, in quadrature 2.5% with the silu's slope; 4% allowed."""
+    H, F = 1024, 2816
+    log(f"[gpu] dense block T={T}")
+    raw, w = block_weights(H, F, 50)
+    x, y = (torch.randn(T, H, generator=gen(T + i)).to(BF).cuda() for i in (0, 1))
+    xo, out, _ = block(x, y, w)
+    x64, z64, _ = join64(x, y, w["post"], None, False, 1.0, w["pre"], 0.0, 1e-6)
+    g, u = (z64 @ raw[k].double().T for k in ("gate", "up"))
+    ref = (g * torch.sigmoid(g) * u) @ raw["down"].double().T
+    assert (xo.double() - x64).norm() <= BF_ROUND * x64.norm()
+    assert (out.double() - ref).norm() <= 0.04 * ref.norm(), float((out.double() - ref).norm() / ref.norm())
+
+
+def test_block_in_a_graph():
+    """The block captured and replayed, its inputs changed between replays, eager steps on other buffers between: the
+    eager step's bits every time.  Two graphs of blocks of two sizes take turns."""
+    log("[gpu] dense block in a graph")
+    _, w = block_weights(512, 1408, 60)
+    graphs = []
+    for T in (9, 300):
+        x, y = (torch.randn(T, 512, device="cuda").to(BF) for _ in range(2))
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            block(x, y, w)
+        torch.cuda.current_stream().wait_stream(side)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = block(x, y, w)
+        graphs.append((graph, x, y, out))
+    for i, (graph, x, y, out) in itertools.product(range(3), graphs):
+        x.copy_(torch.randn(x.shape, generator=gen(i)).to(BF))
+        y.copy_(torch.randn(y.shape, generator=gen(i + 10)).to(BF))
+        graph.replay()
+        want = block(x, y, w)
+        torch.cuda.synchronize()
+        for a, b in zip(out, want):
+            assert torch.equal(bits(a), bits(b)), (i, x.shape)
