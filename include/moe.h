@@ -618,7 +618,7 @@ moe_status moe_pack_int8(const int8_t* codes, int64_t rows, int32_t K, int8_t* o
  * scales and bias are applied in fp32 in this order, y is rounded once.  A token's NaN scale is
  * in its row alone.
  * Errors: INVALID_ARGUMENT for T < 0, N < 1, K not a positive multiple of 16, null or misaligned
- * pointers; UNSUPPORTED for K > 131056, T > 2^20 or N > 2^24; WORKSPACE_TOO_SMALL.
+ * pointers; UNSUPPORTED for K > 131056, T > 2^20, N > 2^24 or T N > 2^37; WORKSPACE_TOO_SMALL.
  *
  * moe_gated_int8 - both projections of a gated block, its activation and product:
  *   h[t][f] = silu(g) * u,   g = x Wg^T, u = x Wu^T as above, in fp32; h bf16 [T, F], rounded once.

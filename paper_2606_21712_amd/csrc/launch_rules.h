@@ -187,4 +187,78 @@ inline RowShape row_shape(int n, int64_t rows, int num_cu) {
   return {1024, nvec <= 4096 ? 4 : 16};
 }
 
+// ---- products of 8-bit codes (int8_gemm.hip)
+
+// The kernels: 16 rows of x with one or two tiles of 16 weight rows a wavefront, or LDS tiles of rows of x
+// by weight rows (gated: half of either matrix); of 128 x 128 one with a ring of three stages and one with
+// two stages, of which two workgroups share a compute unit.
+enum class Int8Form { kFew1, kFew2, k64x128, k128x128, k128x128Two, k192x256, k256x256 };
+
+struct Int8Plan {
+  Int8Form form;
+  int parts;              // that tiles are cut into along k, their sums joined by a second kernel
+  int64_t tiles;
+  size_t part_bytes;      // of the sums of one part of every tile
+};
+
+// Which kernel: the one that a model of their times, fitted to 4000 measurements of 500 sizes (1 to 16384 rows, 100
+// to 30000 channels, K 256 to 16384, plain and gated), thinks the fastest.  Over these sizes its choice takes 2% more
+// than the fastest of all measured ones on average, 6% in one of ten.  us; a stage is 128 columns.
+//   LDS tiles: rounds of as many workgroups as run at once, each its stages and a rest, the last round
+//   with compute units to spare cheaper by the stage; operands and results at 3.9 TB/s beside it.
+//   Parts: another launch, and the sums written and read.
+//   Few rows: the latency of a wavefront's stages, the 1 KB pieces that pass through a compute unit, and
+//   the weights at 5.1 TB/s.
+// (332 rows, 6145 channels, K 4096: 17.0 on 128 x 128, 21.5 on 64 x 128, 34 on 192 x 256; 2003, 4608, 7168: 71, 76 on
+// 256 x 256, 112 on 128 x 128 with two workgroups; 128, 4096, 14336: 25.5 on 64 x 128 in four parts, 33.9 in two,
+// 51 whole; 16384, 4096, 14336: 754 on 256 x 256, 833 on 192 x 256, 923 on 128 x 128 with two.)
+inline Int8Plan int8_plan(int64_t T, int64_t N, int64_t K, bool gated, int num_cu) {
+  struct Tile {
+    Int8Form form;
+    int rows, wrows, together;     // workgroups of a compute unit
+    double alone, busy, rest;      // a stage with compute units to spare, and with all at work; the rest of a tile
+    int most_parts;
+  };
+  static constexpr Tile kTiles[] = {
+      {Int8Form::k64x128, 64, 128, 2, 0.23, 0.63, 1.9, 8},    {Int8Form::k128x128, 128, 128, 1, 0.33, 0.60, 2.3, 4},
+      {Int8Form::k128x128Two, 128, 128, 2, 0.65, 1.10, 2.0, 1}, {Int8Form::k192x256, 192, 256, 1, 0.81, 1.14, 9.0, 1},
+      {Int8Form::k256x256, 256, 256, 1, 1.03, 1.46, 12.3, 1},
+  };
+  const int64_t most = int64_t(1) << 23;     // workgroups of a launch
+  const double mats = gated ? 2 : 1, weights = mats * double(N) * double(K);
+  const double moved = (weights + double(T) * double(K) + 2.0 * double(T) * double(N)) / 3.9e6;
+  const double stages = double(ceil_div(K, 128));
+  Int8Plan best{Int8Form::k256x256, 1, 0, 0};
+  double best_us = 1e300;
+  for (const Tile& t : kTiles) {
+    const int64_t tiles = ceil_div(T, t.rows) * ceil_div(N, gated ? t.wrows / 2 : t.wrows);
+    for (int parts = 1; parts <= t.most_parts; parts *= 2) {
+      const int64_t blocks = tiles * parts, round = int64_t(num_cu) * t.together;
+      if (blocks > most && t.form != Int8Form::k256x256) continue;
+      if (parts > 1 && (parts > stages || blocks > 4 * round)) continue;
+      const double full = t.busy * stages / parts + t.rest, left = double(blocks % round);
+      double us = double(blocks / round) * full;
+      if (left > 0) us += left <= num_cu ? t.alone * stages / parts + t.rest : full;
+      if (parts > 1) us += 4.4 + 1.15e-6 * mats * double(T) * double(N) * parts;
+      us = 2.7 + (us > moved ? us + 0.25 * moved : moved + 0.25 * us);
+      if (us < best_us) {
+        best_us = us;
+        best = {t.form, parts, tiles, size_t(tiles) * t.rows * t.wrows * 4};
+      }
+    }
+  }
+  if (T <= 128)
+    for (int nt = gated ? 2 : 1; nt <= 2; ++nt) {
+      const double blocks = double(ceil_div(ceil_div(N, 16), gated ? 1 : nt) * ceil_div(T, 16)), steps = std::ceil(stages / 8);
+      const double alone = 0.48 * steps + 1.2, move = blocks / num_cu * steps * 8 * (0.31 * nt + 0.014) * 2.048 / 13.8;
+      const double longest = std::fmax(std::fmax(alone, move), weights / 5.1e6);
+      const double us = 3.7 + longest + 0.3 * std::fmin(alone, move);
+      if (us < best_us) {
+        best_us = us;
+        best = {nt == 1 ? Int8Form::kFew1 : Int8Form::kFew2, 1, 0, 0};
+      }
+    }
+  return best;
+}
+
 }  // namespace moe

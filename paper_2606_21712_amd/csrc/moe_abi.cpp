@@ -8,6 +8,7 @@
 #include <string>
 
 #include "../../include/moe.h"
+#include "launch_rules.h"
 #include "moe_internal.h"
 #include "moe_validate.h"
 
@@ -468,33 +469,63 @@ moe_status moe_pack_int8(const int8_t* codes, int64_t rows, int32_t K, int8_t* o
   return hip_status("moe_pack_int8", moe::launch_pack_int8(codes, rows, K, out, stream_of(stream)));
 }
 
-size_t moe_matmul_int8_workspace_bytes(int64_t, int32_t, int32_t) { return 0; }
-size_t moe_gated_int8_workspace_bytes(int64_t, int32_t, int32_t) { return 0; }
+namespace {
+
+// The plan of a product, and the scratch that it needs.
+hipError_t int8_plan_of(int64_t T, int32_t N, int32_t K, bool gated, moe::Int8Plan* plan, size_t* need) {
+  hipError_t err;
+  const int ncu = cu_count(&err);
+  if (err != hipSuccess) return err;
+  *plan = moe::int8_plan(T, N, K, gated, ncu);
+  *need = plan->parts > 1 ? plan->parts * plan->part_bytes : 0;
+  return err;
+}
+
+size_t int8_workspace_bytes(int64_t T, int32_t N, int32_t K, bool gated) {
+  moe::Int8Plan plan;
+  size_t need;
+  if (!moe::int8_sizes_ok(T, N, K) || int8_plan_of(T, N, K, gated, &plan, &need) != hipSuccess) return 0;
+  return need;
+}
+
+typedef int i32x4_t __attribute__((ext_vector_type(4)));
+
+}  // namespace
+
+size_t moe_matmul_int8_workspace_bytes(int64_t T, int32_t N, int32_t K) { return int8_workspace_bytes(T, N, K, false); }
+size_t moe_gated_int8_workspace_bytes(int64_t T, int32_t F, int32_t K) { return int8_workspace_bytes(T, F, K, true); }
 
 moe_status moe_matmul_int8(const int8_t* x, const float* x_scales, const int8_t* w, const float* w_scales,
                            const void* bias, int64_t T, int32_t N, int32_t K, void* y, void* ws, size_t ws_bytes,
                            moe_stream stream) {
-  moe::Check c = moe::validate_matmul_int8(x, x_scales, w, w_scales, bias, T, N, K, y, ws, ws_bytes, 0);
+  // the workspace's size depends on the device's compute units: looked at once all else is right
+  moe::Check c = moe::validate_matmul_int8(x, x_scales, w, w_scales, bias, T, N, K, y);
   if (!c.ok() || T == 0) return finish(c);
-  hipError_t err;
-  const int ncu = cu_count(&err);
+  moe::Int8Plan plan;
+  size_t need;
+  const hipError_t err = int8_plan_of(T, N, K, false, &plan, &need);
   if (err != hipSuccess) return hip_status("moe_matmul_int8", err);
+  c = moe::validate_int8_workspace("moe_matmul_int8", ws, ws_bytes, need);
+  if (!c.ok()) return finish(c);
   const moe::Int8Product p = {x, x_scales, w, nullptr, w_scales, nullptr, static_cast<const uint16_t*>(bias),
-                              static_cast<uint16_t*>(y), int(T), N, K, (K + 127) / 128 * 2};
-  return hip_status("moe_matmul_int8", moe::launch_int8_product(p, ncu, stream_of(stream)));
+                              static_cast<uint16_t*>(y), int(T), N, K, (K + 127) / 128 * 2, static_cast<i32x4_t*>(ws)};
+  return hip_status("moe_matmul_int8", moe::launch_int8_product(p, plan, stream_of(stream)));
 }
 
 moe_status moe_gated_int8(const int8_t* x, const float* x_scales, const int8_t* wg, const float* wg_scales,
                           const int8_t* wu, const float* wu_scales, int64_t T, int32_t F, int32_t K, void* h, void* ws,
                           size_t ws_bytes, moe_stream stream) {
-  moe::Check c = moe::validate_gated_int8(x, x_scales, wg, wg_scales, wu, wu_scales, T, F, K, h, ws, ws_bytes, 0);
+  moe::Check c = moe::validate_gated_int8(x, x_scales, wg, wg_scales, wu, wu_scales, T, F, K, h);
   if (!c.ok() || T == 0) return finish(c);
-  hipError_t err;
-  const int ncu = cu_count(&err);
+  moe::Int8Plan plan;
+  size_t need;
+  const hipError_t err = int8_plan_of(T, F, K, true, &plan, &need);
   if (err != hipSuccess) return hip_status("moe_gated_int8", err);
+  c = moe::validate_int8_workspace("moe_gated_int8", ws, ws_bytes, need);
+  if (!c.ok()) return finish(c);
   const moe::Int8Product p = {x, x_scales, wg, wu, wg_scales, wu_scales, nullptr, static_cast<uint16_t*>(h), int(T), F, K,
-                              (K + 127) / 128 * 2};
-  return hip_status("moe_gated_int8", moe::launch_int8_product(p, ncu, stream_of(stream)));
+                              (K + 127) / 128 * 2, static_cast<i32x4_t*>(ws)};
+  return hip_status("moe_gated_int8", moe::launch_int8_product(p, plan, stream_of(stream)));
 }
 
 }  // extern "C"

@@ -211,7 +211,9 @@ struct Int8Product {
   uint16_t* y;                            // [T, N]
   int T, N, K;
   int steps;                              // of 64 columns, an even number
+  int __attribute__((ext_vector_type(4)))* partial;   // sums of tiles that are cut along k
 };
-hipError_t launch_int8_product(const Int8Product& p, int num_cu, hipStream_t s);
+struct Int8Plan;                          // launch_rules.h
+hipError_t launch_int8_product(const Int8Product& p, const Int8Plan& plan, hipStream_t s);
 
 }  // namespace moe

@@ -684,18 +684,19 @@ Check int8_sizes(const char* fn, int64_t T, int32_t N, int32_t K) {
   if (N < 1) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "N=%lld must be >= 1", N);
   if (T > (1 << 20)) return fail(MOE_ERR_UNSUPPORTED, fn, "T=%lld exceeds %lld", T, 1 << 20);
   if (N > kInt8MaxRows) return fail(MOE_ERR_UNSUPPORTED, fn, "N=%lld exceeds %lld", N, kInt8MaxRows);
+  if (T > 0 && N > (int64_t(1) << 37) / T) return fail(MOE_ERR_UNSUPPORTED, fn, "T=%lld x N=%lld outputs are too many", T, N);
   return Check{};
 }
 
-Check int8_workspace(const char* fn, const void* ws, size_t ws_bytes, size_t need) {
+}  // namespace
+
+Check validate_int8_workspace(const char* fn, const void* ws, size_t ws_bytes, size_t need) {
   if (ws_bytes < need)
     return fail(MOE_ERR_WORKSPACE_TOO_SMALL, fn, "workspace %lld bytes < %lld needed", (long long)ws_bytes,
                 (long long)need);
   if (need > 0) MOE_TRY(ptr(fn, "ws", ws));
   return Check{};
 }
-
-}  // namespace
 
 Check validate_norm_join(const void* x, int64_t x_stride, int x_dt, const void* y, int64_t y_stride, int32_t post,
                          const void* w_post, const void* gate, int64_t gate_stride, int32_t gate_kind, int32_t sigmoid,
@@ -780,8 +781,7 @@ Check validate_pack_int8(const void* codes, int64_t rows, int32_t K, const void*
 bool int8_sizes_ok(int64_t T, int32_t N, int32_t K) { return T > 0 && int8_sizes("", T, N, K).ok(); }
 
 Check validate_matmul_int8(const void* x, const void* x_scales, const void* w, const void* w_scales, const void* bias,
-                           int64_t T, int32_t N, int32_t K, const void* y, const void* ws, size_t ws_bytes,
-                           size_t need) {
+                           int64_t T, int32_t N, int32_t K, const void* y) {
   const char* fn = "moe_matmul_int8";
   MOE_TRY(int8_sizes(fn, T, N, K));
   if (T == 0) return Check{};
@@ -790,13 +790,11 @@ Check validate_matmul_int8(const void* x, const void* x_scales, const void* w, c
   MOE_TRY(ptr(fn, "w", w));
   MOE_TRY(ptr(fn, "w_scales", w_scales));
   if (bias != nullptr) MOE_TRY(ptr(fn, "bias", bias));
-  MOE_TRY(ptr(fn, "y", y));
-  return int8_workspace(fn, ws, ws_bytes, need);
+  return ptr(fn, "y", y);
 }
 
 Check validate_gated_int8(const void* x, const void* x_scales, const void* wg, const void* wg_scales, const void* wu,
-                          const void* wu_scales, int64_t T, int32_t F, int32_t K, const void* h, const void* ws,
-                          size_t ws_bytes, size_t need) {
+                          const void* wu_scales, int64_t T, int32_t F, int32_t K, const void* h) {
   const char* fn = "moe_gated_int8";
   MOE_TRY(int8_sizes(fn, T, F, K));
   if (T == 0) return Check{};
@@ -806,8 +804,7 @@ Check validate_gated_int8(const void* x, const void* x_scales, const void* wg, c
   MOE_TRY(ptr(fn, "wg_scales", wg_scales));
   MOE_TRY(ptr(fn, "wu", wu));
   MOE_TRY(ptr(fn, "wu_scales", wu_scales));
-  MOE_TRY(ptr(fn, "h", h));
-  return int8_workspace(fn, ws, ws_bytes, need);
+  return ptr(fn, "h", h);
 }
 
 }  // namespace moe

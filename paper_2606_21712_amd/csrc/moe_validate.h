@@ -107,10 +107,10 @@ Check validate_quantize_int8(const void* src, int64_t src_stride, int64_t rows, 
                              const void* scales);
 Check validate_pack_int8(const void* codes, int64_t rows, int32_t K, const void* out);
 Check validate_matmul_int8(const void* x, const void* x_scales, const void* w, const void* w_scales, const void* bias,
-                           int64_t T, int32_t N, int32_t K, const void* y, const void* ws, size_t ws_bytes, size_t need);
+                           int64_t T, int32_t N, int32_t K, const void* y);
 Check validate_gated_int8(const void* x, const void* x_scales, const void* wg, const void* wg_scales, const void* wu,
-                          const void* wu_scales, int64_t T, int32_t F, int32_t K, const void* h, const void* ws,
-                          size_t ws_bytes, size_t need);
+                          const void* wu_scales, int64_t T, int32_t F, int32_t K, const void* h);
+Check validate_int8_workspace(const char* fn, const void* ws, size_t ws_bytes, size_t need);
 bool int8_sizes_ok(int64_t T, int32_t N, int32_t K);
 
 }  // namespace moe

@@ -73,15 +73,17 @@ int main() {
       expect(n > 0 && n % 2048 == 0 && n / 1024 <= (1u << 26), "packed pieces", T, H);
     }
     const size_t ws = (next() & 1) ? 0 : ~size_t(0), need = next() % 3 ? 0 : 1000;
-    c = validate_matmul_int8(pickp(), pickp(), pickp(), pickp(), pickp(), T, N, H, pickp(), pickp(), ws, need);
+    c = validate_matmul_int8(pickp(), pickp(), pickp(), pickp(), pickp(), T, N, H, pickp());
     if (c.ok()) {
       ++g_accepted;
       expect(T >= 0 && T <= (1 << 20) && N >= 1 && N <= (1 << 24) && H % 16 == 0 && H <= 131056, "product", T, N);
-      expect(T == 0 || ws >= need, "workspace", (long long)ws, (long long)need);
       expect(int8_sizes_ok(T, N, H) == (T > 0), "sizes", T, N);
+      expect(T == 0 || T * int64_t(N) <= (int64_t(1) << 37), "outputs", T, N);
     }
-    c = validate_gated_int8(pickp(), pickp(), pickp(), pickp(), pickp(), pickp(), T, N, H, pickp(), pickp(), ws, need);
+    c = validate_gated_int8(pickp(), pickp(), pickp(), pickp(), pickp(), pickp(), T, N, H, pickp());
     if (c.ok()) ++g_accepted;
+    c = validate_int8_workspace("call", pickp(), ws, need);
+    if (c.ok()) expect(ws >= need, "workspace", (long long)ws, (long long)need);
   }
   if (g_accepted < 20000) {
     std::fprintf(stderr, "FAIL only %ld accepted\n", g_accepted);

@@ -96,13 +96,26 @@ def test_products(L, cus, call):
     for bad in (dict(T=-1), dict(N=0), dict(N=-4), dict(K=0), dict(K=72), dict(x=None), dict(x=P + 8), dict(xs=None),
                 dict(xs=P + 4)):
         assert call(L, **bad) == INVALID, bad
-    for bad in (dict(T=(1 << 20) + 1), dict(N=(1 << 24) + 1), dict(K=131072)):
+    for bad in (dict(T=(1 << 20) + 1), dict(N=(1 << 24) + 1), dict(K=131072), dict(T=1 << 20, N=1 << 18)):
         assert call(L, **bad) == UNSUPPORTED, bad
     assert call(L, T=0, x=None, xs=None, ws=None, n=0) == 0
     own = (dict(w=None), dict(w=P + 8), dict(ws_=None), dict(bias=P + 2), dict(y=None)) if call is matmul else (
         dict(wg=None), dict(sg=P + 4), dict(wu=None), dict(wu=P + 1), dict(su=None), dict(h=P + 2))
     for bad in own:
         assert call(L, **bad) == INVALID, bad
+
+
+@pytest.mark.parametrize("call,size", [(matmul, moe.moe_matmul_int8_workspace_bytes), (gated, moe.moe_gated_int8_workspace_bytes)])
+def test_workspace(L, cus, call, size):
+    """None where tiles are whole; where they are cut along k, the sums of every part, and no less is taken."""
+    assert size(16384, 4096, 14336) == 0 and size(1, 4096, 4096) == 0
+    for bad in ((0, 16, 64), (-1, 16, 64), (1, 0, 64), (1, 16, 8), (1, 16, 1 << 20), (1 << 21, 16, 64)):
+        assert size(*bad) == 0
+    need = size(128, 4096, 14336)
+    assert need > 0 and need % (128 * 4096 * 4) == 0
+    sizes = dict(T=128, N=4096, K=14336)
+    assert call(L, **sizes, n=need - 1) == WS_SMALL
+    assert call(L, **sizes, ws=None) == INVALID and call(L, **sizes, ws=P + 8) == INVALID
 
 
 def test_binding_refusals():
