@@ -693,7 +693,8 @@ class Int8:
             raise TypeError("packed codes are int8, scales float32")
         if codes.numel() < moe_int8_code_bytes(N, K) or scales.shape != (N,):
             raise ValueError(f"codes or scales do not fit 8-bit weights {self.shape}")
-        _on(codes.get_device(), codes, scales)
+        self.index = codes.get_device()
+        _on(self.index, codes, scales)
 
 
 def moe_int8_code_bytes(rows, K) -> int:
@@ -710,27 +711,28 @@ def _on(index, *ts):
 def _run(fn, index, stream, *args):
     """A call on the GPU of that index, whichever is the current one."""
     if index == torch._C._cuda_getDevice():
-        _check(fn(*args, torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream))
+        status = fn(*args, torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream)
+        if status:
+            _check(status)
         return
     with torch.cuda.device(index):
         _run(fn, index, stream, *args)
 
 
-def _matrix(t, name, T, H, dtypes, index):
+def _matrix(t, name, shape, index, dtype=torch.bfloat16):
     """Row stride of a tensor [T, H] whose rows are in one piece."""
-    if t.dtype not in dtypes:
-        raise TypeError(f"{name} must be " + " or ".join(map(str, dtypes)))
-    if t.shape != (T, H):
-        raise ValueError(f"{name} must be [{T}, {H}]")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {tuple(shape)}")
     if t.get_device() != index or index < 0:
         raise ValueError("all tensors must be on one GPU")
+    if t.is_contiguous():
+        return shape[1]
     row, one = t.stride()
-    if one != 1 and H > 1:
+    if one != 1:
         raise ValueError(f"{name}: rows must be in one piece")
-    return row if T > 1 else H
-
-
-_BF16, _STREAMS = (torch.bfloat16,), (torch.bfloat16, torch.float32)
+    return row
 
 
 def _weight(w, name, H, index):
@@ -743,6 +745,21 @@ def _weight(w, name, H, index):
     return w.data_ptr()
 
 
+def _gate(gate, T, H, index):
+    """Address, row stride and kind (moe_gate) of a gate."""
+    if gate.dtype != torch.bfloat16:
+        raise TypeError("gate must be bf16")
+    if gate.get_device() != index:
+        raise ValueError("all tensors must be on one GPU")
+    if gate.shape == (H,) or gate.shape == (1, H):
+        if gate.stride(-1) != 1:
+            raise ValueError("gate: rows must be in one piece")
+        return gate.data_ptr(), 0, 1
+    if gate.shape == (T, 1):
+        return gate.data_ptr(), gate.stride(0) if T > 1 else 1, 2
+    return gate.data_ptr(), _matrix(gate, "gate", (T, H), index), 3
+
+
 def moe_norm_join(x, y=None, post=None, gate=None, sigmoid=False, alpha=1.0, pre=None, offset=0.0, eps=1e-6, int8=False,
                   x_out=None, z=None, scales=None, stream=None):
     """The joint between two blocks: x' = x + alpha * gate * norm(y) * (offset + post), z = norm(x') * (offset + pre)
@@ -753,56 +770,47 @@ def moe_norm_join(x, y=None, post=None, gate=None, sigmoid=False, alpha=1.0, pre
     channels), [T, 1] (of the tokens) or [T, H]; with T = 1 [1, H] counts for either.  sigmoid: of the gate.  int8:
     z as codes with a scale for each row, else bf16 (scales None).  x_out may be x.  x, y, a gate [T, H] and
     x_out may be slices with rows in one piece."""
-    T, H = x.shape
-    dev, index = x.device, x.get_device()
-    xs = _matrix(x, "x", T, H, _STREAMS, index)
-    yp = gp = post_w = op = None
+    shape, dt, index = x.shape, x.dtype, x.get_device()
+    T, H = shape
+    if dt != torch.bfloat16 and dt != torch.float32:
+        raise TypeError("x must be bf16 or f32")
+    xs = _matrix(x, "x", shape, index, dt)
+    yp = gp = post_w = op = pre_w = zp = sp = None
     ys = gs = os_ = kind = 0
     if y is not None:
-        ys, yp = _matrix(y, "y", T, H, _BF16, index), y.data_ptr()
+        ys, yp = _matrix(y, "y", shape, index), y.data_ptr()
         if gate is not None:
-            if gate.dtype != torch.bfloat16:
-                raise TypeError("gate must be bf16")
-            if gate.get_device() != index:
-                raise ValueError("all tensors must be on one GPU")
-            if gate.shape in ((H,), (1, H)):
-                kind, contiguous = 1, gate.stride(-1) == 1 or H == 1
-                if not contiguous:
-                    raise ValueError("gate: rows must be in one piece")
-            elif gate.shape == (T, 1):
-                kind, gs = 2, gate.stride(0) if T > 1 else 1
-            else:
-                kind, gs = 3, _matrix(gate, "gate", T, H, _BF16, index)
-            gp = gate.data_ptr()
+            gp, gs, kind = _gate(gate, T, H, index)
         if post is not None:
             post_w = _weight(post, "post", H, index)
-        x_out = _like(x_out, "x_out", x.dtype, (T, H), dev, stream)
-        os_, op = _matrix(x_out, "x_out", T, H, _STREAMS, index), x_out.data_ptr()
+        if x_out is None:
+            x_out = _new(shape, dt, x.device, stream)
+        os_, op = _matrix(x_out, "x_out", shape, index, dt), x_out.data_ptr()
     elif post is not None or gate is not None or x_out is not None:
         raise ValueError("post, gate and x_out need y")
-    pre_w = None
     if pre is not None:
         pre_w = _weight(pre, "pre", H, index)
-        z = _like(z, "z", torch.int8 if int8 else torch.bfloat16, (T, H), dev, stream)
+        z = _like(z, "z", torch.int8 if int8 else torch.bfloat16, shape, x.device, stream)
+        zp = z.data_ptr()
         if int8:
-            scales = _like(scales, "scales", torch.float32, (T,), dev, stream)
+            scales = _like(scales, "scales", torch.float32, (T,), x.device, stream)
+            sp = scales.data_ptr()
         elif scales is not None:
             raise ValueError("scales need int8")
         _on(index, z, scales)
     elif z is not None or scales is not None or int8:
         raise ValueError("z, scales and int8 need pre")
-    _run(lib().moe_norm_join, index, stream, x.data_ptr(), xs, DTYPE_F32 if x.dtype == torch.float32 else DTYPE_BF16, yp,
-         ys, 0 if post is None else 1, post_w, gp, gs, kind, 1 if sigmoid else 0, alpha, pre_w, offset, eps, T, H, op,
-         os_, 1 if int8 else 0, None if z is None else z.data_ptr(), None if scales is None else scales.data_ptr())
+    _run(lib().moe_norm_join, index, stream, x.data_ptr(), xs, DTYPE_BF16 if dt == torch.bfloat16 else DTYPE_F32, yp, ys,
+         post is not None, post_w, gp, gs, kind, bool(sigmoid), alpha, pre_w, offset, eps, T, H, op, os_, bool(int8), zp, sp)
     return x if y is None else x_out, z, scales
 
 
 def moe_quantize_int8(src, codes=None, scales=None, stream=None):
     """bf16 [T, K], rows in one piece -> (codes int8 [T, K], scales f32 [T])."""
-    T, K = src.shape
-    index = src.get_device()
-    row = _matrix(src, "src", T, K, _BF16, index)
-    codes = _like(codes, "codes", torch.int8, (T, K), src.device, stream)
+    shape, index = src.shape, src.get_device()
+    T, K = shape
+    row = _matrix(src, "src", shape, index)
+    codes = _like(codes, "codes", torch.int8, shape, src.device, stream)
     scales = _like(scales, "scales", torch.float32, (T,), src.device, stream)
     _on(index, codes, scales)
     _run(lib().moe_quantize_int8, index, stream, src.data_ptr(), row, T, K, codes.data_ptr(), scales.data_ptr())
@@ -838,39 +846,52 @@ def _int8_inputs(x, scales, w):
     T, K = x.shape
     if x.dtype != torch.int8 or scales.dtype != torch.float32:
         raise TypeError("x is int8 codes, its scales float32")
-    if scales.shape != (T,) or w.shape[1] != K:
+    N, wK = w.shape
+    if scales.shape != (T,) or wK != K:
         raise ValueError(f"scales {tuple(scales.shape)} or weights {w.shape} do not fit x [{T}, {K}]")
-    return T, w.shape[0], K
+    index = x.get_device()
+    if w.index != index:
+        raise ValueError("all tensors must be on one GPU")
+    return T, N, K, index
+
+
+def _scratch(ws, need, device, stream):
+    """Address and bytes of a given workspace, or of a new one where one is needed."""
+    if ws is None:
+        if not need:
+            return None, 0
+        ws = _new(need, torch.uint8, device, stream)
+    return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
 def moe_matmul_int8(x, scales, w, bias=None, y=None, ws=None, stream=None):
     """x codes int8 [T, K] and scales f32 [T], w Int8 [N, K], bias bf16 [N] or None -> y bf16 [T, N]."""
-    T, N, K = _int8_inputs(x, scales, w)
-    if bias is not None and (bias.dtype != torch.bfloat16 or bias.shape != (N,)):
-        raise ValueError(f"bias must be bf16 [{N}]")
+    T, N, K, index = _int8_inputs(x, scales, w)
+    bp = None
+    if bias is not None:
+        if bias.dtype != torch.bfloat16 or bias.shape != (N,):
+            raise ValueError(f"bias must be bf16 [{N}]")
+        bp = bias.data_ptr()
     y = _like(y, "y", torch.bfloat16, (T, N), x.device, stream)
-    if ws is None:
-        ws = _new(max(1, moe_matmul_int8_workspace_bytes(T, N, K)), torch.uint8, x.device, stream)
-    index = x.get_device()
-    _on(index, x, scales, w.codes, bias, y, ws)
-    _run(lib().moe_matmul_int8, index, stream, x.data_ptr(), scales.data_ptr(), w.codes.data_ptr(), w.scales.data_ptr(),
-         None if bias is None else bias.data_ptr(), T, N, K, y.data_ptr(), ws.data_ptr(), ws.numel())
+    _on(index, x, scales, bias, y, ws)
+    wp, wn = _scratch(ws, 0 if ws is not None else moe_matmul_int8_workspace_bytes(T, N, K), x.device, stream)
+    _run(lib().moe_matmul_int8, index, stream, x.data_ptr(), scales.data_ptr(), w.codes.data_ptr(), w.scales.data_ptr(), bp,
+         T, N, K, y.data_ptr(), wp, wn)
     return y
 
 
 def moe_gated_int8(x, scales, w_gate, w_up, h=None, ws=None, stream=None):
     """x codes int8 [T, K] and scales f32 [T], w_gate and w_up Int8 [F, K] -> h = silu(x Wg^T) * (x Wu^T), bf16 [T, F]."""
-    T, F, K = _int8_inputs(x, scales, w_gate)
+    T, F, K, index = _int8_inputs(x, scales, w_gate)
     if w_up.shape != w_gate.shape:
         raise ValueError(f"w_gate {w_gate.shape} and w_up {w_up.shape} differ")
+    if w_up.index != index:
+        raise ValueError("all tensors must be on one GPU")
     h = _like(h, "h", torch.bfloat16, (T, F), x.device, stream)
-    if ws is None:
-        ws = _new(max(1, moe_gated_int8_workspace_bytes(T, F, K)), torch.uint8, x.device, stream)
-    index = x.get_device()
-    _on(index, x, scales, w_gate.codes, w_up.codes, h, ws)
+    _on(index, x, scales, h, ws)
+    wp, wn = _scratch(ws, 0 if ws is not None else moe_gated_int8_workspace_bytes(T, F, K), x.device, stream)
     _run(lib().moe_gated_int8, index, stream, x.data_ptr(), scales.data_ptr(), w_gate.codes.data_ptr(),
-         w_gate.scales.data_ptr(), w_up.codes.data_ptr(), w_up.scales.data_ptr(), T, F, K, h.data_ptr(), ws.data_ptr(),
-         ws.numel())
+         w_gate.scales.data_ptr(), w_up.codes.data_ptr(), w_up.scales.data_ptr(), T, F, K, h.data_ptr(), wp, wn)
     return h
 
 

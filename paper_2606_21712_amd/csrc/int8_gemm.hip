@@ -78,6 +78,22 @@ __global__ __launch_bounds__(64 * KS) void few_int8_kernel(Int8Product p) {
   const auto bx = buffer_of(p.x + int64_t(t0) * p.K, int64_t(min(p.T - t0, 16)) * p.K);
   const int chunk = 16 * (lane >> 4);
   const int xat = (lane & 15) * p.K + chunk;      // past the last row: zeros
+  // what the wavefronts that finish a tile need besides: loaded first, not once the sums are there
+  const int t = t0 + (lane & 15), n = (rt + wave) * 16 + 4 * (lane >> 4);
+  const bool finish = wave < kTiles && t < p.T && n < p.N;
+  float sx = 0.f, s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
+  if (finish) {
+    sx = p.x_scales[t];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int ni = min(n + i, p.N - 1);
+      s0[i] = p.s0[ni];
+      if (GATED)
+        s1[i] = p.s1[ni];
+      else if (p.bias != nullptr)
+        s1[i] = bf16_to_f32(p.bias[ni]);
+    }
+  }
   i32x4 acc[NT];
 #pragma unroll
   for (int r = 0; r < NT; ++r) acc[r] = i32x4{0, 0, 0, 0};
@@ -108,29 +124,24 @@ __global__ __launch_bounds__(64 * KS) void few_int8_kernel(Int8Product p) {
 #pragma unroll
   for (int r = 0; r < NT; ++r) part[wave][r][lane] = acc[r];
   __syncthreads();
-  for (int q = wave; q < kTiles; q += KS) {
-    i32x4 s = part[0][q][lane], u = {0, 0, 0, 0};
+  if (!finish) return;
+  i32x4 s = part[0][wave][lane], u = {0, 0, 0, 0};
 #pragma unroll
-    for (int i = 1; i < KS; ++i) s += part[i][q][lane];
-    if (GATED) {
+  for (int i = 1; i < KS; ++i) s += part[i][wave][lane];
+  if (GATED) {
 #pragma unroll
-      for (int i = 0; i < KS; ++i) u += part[i][kTiles + q][lane];
-    }
-    const int t = t0 + (lane & 15), n = (rt + q) * 16 + 4 * (lane >> 4);
-    if (t >= p.T || n >= p.N) continue;
-    const float sx = p.x_scales[t];
-    float v[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int ni = min(n + i, p.N - 1);
-      v[i] = scaled(s[i], sx, p.s0[ni]);
-      if (GATED)
-        v[i] = silu(v[i]) * scaled(u[i], sx, p.s1[ni]);
-      else if (p.bias != nullptr)
-        v[i] = biased(v[i], bf16_to_f32(p.bias[ni]));
-    }
-    store4(p.y + int64_t(t) * p.N, n, p.N, v);
+    for (int i = 0; i < KS; ++i) u += part[i][kTiles + wave][lane];
   }
+  float v[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[i] = scaled(s[i], sx, s0[i]);
+    if (GATED)
+      v[i] = silu(v[i]) * scaled(u[i], sx, s1[i]);
+    else if (p.bias != nullptr)
+      v[i] = biased(v[i], s1[i]);
+  }
+  store4(p.y + int64_t(t) * p.N, n, p.N, v);
 }
 
 template <bool GATED, int NT>
@@ -199,11 +210,10 @@ typedef u32x4 __attribute__((aligned(2))) u32x4_any;
 // The results of 32 rows from tb on, NI x 32 sums a wavefront: a lane holds channels 8 b + 4 (lane / 32) + 0..3 of
 // row lane % 32 of each 32 x 32.  They go through LDS of the wavefront's own, to leave as whole pieces of rows.
 template <bool GATED, int NI>
-__device__ __forceinline__ void put_rows(const Int8Product& p, const i32x16 (&acc)[NI], int tb, int nb, const float* scale0,
-                                         const float* scale1, uint8_t* out, int lane) {
+__device__ __forceinline__ void put_rows(const Int8Product& p, const i32x16 (&acc)[NI], int tb, int nb, float sx,
+                                         const float* scale0, const float* scale1, uint8_t* out, int lane) {
   constexpr int kCols = GATED ? 16 * NI : 32 * NI, kPitch = kCols * 2 + 16;
   const int r32 = lane & 31, half = lane >> 5;
-  const float sx = p.x_scales[min(tb + r32, p.T - 1)];
 #pragma unroll
   for (int nc = 0; nc < (GATED ? NI / 2 : NI); ++nc)
 #pragma unroll
@@ -362,7 +372,10 @@ __global__ __launch_bounds__(256, 1) void int8_gemm_kernel(Int8Product p, int mt
     __builtin_amdgcn_sched_barrier(0);
   };
 
-  // this thread's share of the columns' scales: of w0; of w1, or the bias
+  // the scales of the wavefront's rows, and this thread's share of the columns': of w0; of w1, or the bias
+  float sx[MI];
+#pragma unroll
+  for (int mi = 0; mi < MI; ++mi) sx[mi] = p.x_scales[min(t0 + (wm * MI + mi) * 32 + r32, p.T - 1)];
   float scale0 = 0.f, scale1 = 0.f;
   if (tid < Tile::kCols && n0 + tid < p.N) {
     scale0 = p.s0[n0 + tid];
@@ -425,7 +438,7 @@ __global__ __launch_bounds__(256, 1) void int8_gemm_kernel(Int8Product p, int mt
   for (int mi = 0; mi < MI; ++mi) {
     const int tb = t0 + (wm * MI + mi) * 32;
     if (tb < p.T)
-      put_rows<GATED, NI>(p, acc[mi], tb, n0 + wn * Tile::kWaveCols, scales + wn * Tile::kWaveCols,
+      put_rows<GATED, NI>(p, acc[mi], tb, n0 + wn * Tile::kWaveCols, sx[mi], scales + wn * Tile::kWaveCols,
                           scales + Tile::kCols + wn * Tile::kWaveCols, out, lane);
   }
 }
@@ -447,6 +460,7 @@ __global__ __launch_bounds__(256) void int8_join_kernel(Int8Product p, int mtile
     scales[0][i] = n < p.N ? p.s0[n] : 0.f;
     scales[1][i] = n >= p.N ? 0.f : GATED ? p.s1[n] : p.bias != nullptr ? bf16_to_f32(p.bias[n]) : 0.f;
   }
+  const float sx = p.x_scales[min(tb + (lane & 31), p.T - 1)];
   i32x16 acc[NI];
 #pragma unroll
   for (int ni = 0; ni < NI; ++ni)
@@ -464,7 +478,7 @@ __global__ __launch_bounds__(256) void int8_join_kernel(Int8Product p, int mtile
   }
   __syncthreads();
   if (tb < p.T)
-    put_rows<GATED, NI>(p, acc, tb, n0 + wn * Tile::kWaveCols, &scales[0][wn * Tile::kWaveCols],
+    put_rows<GATED, NI>(p, acc, tb, n0 + wn * Tile::kWaveCols, sx, &scales[0][wn * Tile::kWaveCols],
                         &scales[1][wn * Tile::kWaveCols], rows + wave * 32 * Tile::kPitch, lane);
 }
 
