@@ -59,7 +59,7 @@ __device__ __forceinline__ void store4(uint16_t* row, int n, int N, const float 
 // the first operand, streamed from memory into registers, x the second, from the caches.  KS wavefronts deal the
 // steps of 128 columns along k among themselves (both halves of a line of x to one of them) and add their sums in
 // LDS; P steps are in flight.  More rows are other workgroups', which find the weights in the L2.
-template <bool GATED, int NT, int KS, int P>
+template <bool GATED, int NT, int KS, int P, int POLICY>
 __global__ __launch_bounds__(64 * KS) void few_int8_kernel(Int8Product p) {
   __shared__ i32x4 part[KS][NT][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -103,7 +103,7 @@ __global__ __launch_bounds__(64 * KS) void few_int8_kernel(Int8Product p) {
 #pragma unroll
     for (int r = 0; r < NT; ++r)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) w[q][r][h] = load16<kCached>(bw[r], i < mine, 16 * lane, at * 2048 + h * 1024);
+      for (int h = 0; h < 2; ++h) w[q][r][h] = load16<POLICY>(bw[r], i < mine, 16 * lane, at * 2048 + h * 1024);
 #pragma unroll
     for (int h = 0; h < 2; ++h)                   // columns past K: zeros, whatever the offset's range check counts
       x[q][h] = load16<kCached>(bx, i < mine, at * 128 + h * 64 + chunk < p.K ? xat : kPast, at * 128 + h * 64);
@@ -145,10 +145,14 @@ __global__ __launch_bounds__(64 * KS) void few_int8_kernel(Int8Product p) {
 }
 
 template <bool GATED, int NT>
-void few(const Int8Product& p, hipStream_t s) {
+void few(const Int8Product& p, bool stream, hipStream_t s) {
   const int tiles = (p.N + 15) / 16, each = GATED ? NT / 2 : NT;
-  MOE_LAUNCH(GATED ? "gated_int8_few" : "matmul_int8_few", (few_int8_kernel<GATED, NT, 8, 2>),
-             dim3((tiles + each - 1) / each, (p.T + 15) / 16), dim3(512), s, p);
+  const char* name = GATED ? "gated_int8_few" : "matmul_int8_few";
+  const dim3 grid((tiles + each - 1) / each, (p.T + 15) / 16), block(512);
+  if (stream)
+    MOE_LAUNCH(name, (few_int8_kernel<GATED, NT, 8, 2, kStream>), grid, block, s, p);
+  else
+    MOE_LAUNCH(name, (few_int8_kernel<GATED, NT, 8, 2, kCached>), grid, block, s, p);
 }
 
 // ------------------------------------------------------------------ many rows of x
@@ -163,8 +167,9 @@ __device__ __forceinline__ i32x16 mfma32_i8(u32x4 a, u32x4 b, i32x16 c) {
 }
 
 // 16 bytes a lane from global memory to 1 KB of LDS, or zeros.
+template <int POLICY>
 __device__ __forceinline__ void load_lds(const Buffer& b, bool on, uint8_t* to, int lane_at, int at) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(b.at(on), to, 16, lane_at, at, 0, 0);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(b.at(on), to, 16, lane_at, at, 0, POLICY);
 }
 
 // The order of a group: P products with R reads from LDS and V loads spread out between them.
@@ -247,7 +252,7 @@ __device__ __forceinline__ void put_rows(const Int8Product& p, const i32x16 (&ac
   }
 }
 
-template <bool GATED, int MI, int NI, int XS, int WS, bool SPLIT>
+template <bool GATED, int MI, int NI, int XS, int WS, bool SPLIT, int POLICY>
 __global__ __launch_bounds__(256, 1) void int8_gemm_kernel(Int8Product p, int mtiles, int ntiles, int parts) {
   using Tile = Int8Tile<GATED, MI, NI>;
   __shared__ __attribute__((aligned(1024))) uint8_t x0[Tile::kXBytes], x1[Tile::kXBytes], x2[XS > 2 ? Tile::kXBytes : 16],
@@ -294,13 +299,13 @@ __global__ __launch_bounds__(256, 1) void int8_gemm_kernel(Int8Product p, int mt
     const bool on = kt * 128 + 16 * chunk < K;                // columns past K: zeros
 #pragma unroll
     for (int i = 0; i < MI; ++i)
-      load_lds(bx, kt < KT, stage + (wave + 4 * (which * MI + i)) * 1024, on ? int(xat[which * MI + i]) : kPast, kt * 128);
+      load_lds<kCached>(bx, kt < KT, stage + (wave + 4 * (which * MI + i)) * 1024, on ? int(xat[which * MI + i]) : kPast, kt * 128);
   };
   auto issue_w = [&](uint8_t* stage, int kt, int which) {
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
       const int i = which * NI + j, tile16 = wave + 4 * (i >> 1);
-      load_lds(GATED && tile16 >= 2 * NI ? bw1 : bw0, kt < KT, stage + tile16 * 2048 + (i & 1) * 1024, int(wat[i >> 1]),
+      load_lds<POLICY>(GATED && tile16 >= 2 * NI ? bw1 : bw0, kt < KT, stage + tile16 * 2048 + (i & 1) * 1024, int(wat[i >> 1]),
                kt * 2048 + (i & 1) * 1024);
     }
   };
@@ -482,13 +487,13 @@ __global__ __launch_bounds__(256) void int8_join_kernel(Int8Product p, int mtile
                         &scales[1][wn * Tile::kWaveCols], rows + wave * 32 * Tile::kPitch, lane);
 }
 
-template <bool GATED, int MI, int NI, int XS, int WS, bool SPLIT>
+template <bool GATED, int MI, int NI, int XS, int WS, bool SPLIT = false, int POLICY = kCached>
 void gemm(const Int8Product& p, int parts, hipStream_t s) {
   using Tile = Int8Tile<GATED, MI, NI>;
   const int mtiles = (p.T + Tile::kRows - 1) / Tile::kRows, ntiles = (p.N + Tile::kCols - 1) / Tile::kCols;
   const int tiles = mtiles * ntiles;
 
-  MOE_LAUNCH(GATED ? "gated_int8" : "matmul_int8", (int8_gemm_kernel<GATED, MI, NI, XS, WS, SPLIT>), dim3(unsigned((int64_t(tiles) * parts + 7) / 8 * 8)), dim3(256), s, p,
+  MOE_LAUNCH(GATED ? "gated_int8" : "matmul_int8", (int8_gemm_kernel<GATED, MI, NI, XS, WS, SPLIT, POLICY>), dim3(unsigned((int64_t(tiles) * parts + 7) / 8 * 8)), dim3(256), s, p,
              mtiles, ntiles, parts);
   if constexpr (SPLIT)
     MOE_LAUNCH("int8_join", (int8_join_kernel<GATED, MI, NI>), dim3(unsigned(tiles * MI)), dim3(256), s, p, mtiles, ntiles,
@@ -500,16 +505,17 @@ void product(const Int8Product& p, const Int8Plan& plan, hipStream_t s) {
   const int parts = plan.parts;
   switch (plan.form) {
     case Int8Form::kFew1:
-      if constexpr (!GATED) return few<GATED, 1>(p, s);
+      if constexpr (!GATED) return few<GATED, 1>(p, plan.stream, s);
       [[fallthrough]];
-    case Int8Form::kFew2: return few<GATED, 2>(p, s);
+    case Int8Form::kFew2: return few<GATED, 2>(p, plan.stream, s);
     case Int8Form::k64x128:
-      return parts > 1 ? gemm<GATED, 1, 2, 3, 3, true>(p, parts, s) : gemm<GATED, 1, 2, 3, 3, false>(p, 1, s);
+      if (parts > 1) return gemm<GATED, 1, 2, 3, 3, true>(p, parts, s);
+      return plan.stream ? gemm<GATED, 1, 2, 3, 3, false, kStream>(p, 1, s) : gemm<GATED, 1, 2, 3, 3>(p, 1, s);
     case Int8Form::k128x128:
-      return parts > 1 ? gemm<GATED, 2, 2, 3, 3, true>(p, parts, s) : gemm<GATED, 2, 2, 3, 3, false>(p, 1, s);
-    case Int8Form::k128x128Two: return gemm<GATED, 2, 2, 2, 2, false>(p, 1, s);
-    case Int8Form::k192x256: return gemm<GATED, 3, 4, 3, 2, false>(p, 1, s);
-    case Int8Form::k256x256: return gemm<GATED, 4, 4, 3, 2, false>(p, 1, s);
+      return parts > 1 ? gemm<GATED, 2, 2, 3, 3, true>(p, parts, s) : gemm<GATED, 2, 2, 3, 3>(p, 1, s);
+    case Int8Form::k128x128Two: return gemm<GATED, 2, 2, 2, 2>(p, 1, s);
+    case Int8Form::k192x256: return gemm<GATED, 3, 4, 3, 2>(p, 1, s);
+    case Int8Form::k256x256: return gemm<GATED, 4, 4, 3, 2>(p, 1, s);
   }
 }
 

@@ -168,24 +168,29 @@ inline bool stream_nt(int64_t R, int E, int K, int N, bool swiglu, bool fp8, int
 
 // ---- rows that a workgroup keeps in registers (norm.hip)
 
-// Threads of a workgroup, and vectors of 8 elements that each keeps of a row of n elements (n % 8 == 0).
+// Threads of a workgroup, and vectors of 8 elements that each keeps of a row of n elements (n % 8 == 0, at
+// most 131072).  A row for each compute unit or less: as many threads as vectors, its latency is all
+// there is (one row of 4096: 3.2 us on 512 threads, 3.5 on 256).  More rows: two vectors a thread, which
+// leaves registers for the row ahead (2003 x 7168: 24.6 us on 512 threads, 26.5 with four vectors on 256), and
+// whole rows to a wavefront, without a barrier, while four vectors do it (16384 x 1024: 26.8 us, 33.7 on 256).
 struct RowShape {
   int threads, vectors;
 };
 inline RowShape row_shape(int n, int64_t rows, int num_cu) {
   const int nvec = (n + 7) / 8;
-  if (rows <= 2 * int64_t(num_cu)) {     // few rows: a row's latency counts
+  if (rows <= num_cu)
     for (int t : {64, 256, 512, 1024})
       if (nvec <= t) return {t, 1};
-    if (nvec <= 2048) return {1024, 2};
-  }
   for (int v : {1, 2, 4})
     if (nvec <= 64 * v) return {64, v};
-  if (nvec <= 512) return {256, 2};
-  if (nvec <= 1024) return {256, 4};
-  if (nvec <= 2048) return {512, 4};
+  for (int t : {256, 512, 1024})
+    if (nvec <= 2 * t) return {t, 2};
   return {1024, nvec <= 4096 ? 4 : 16};
 }
+
+// Workgroups of norm_join for each compute unit: rows of one wavefront, or 1024 threads' worth of others (of
+// 2048 threads' worth half waits for registers, and the last rows come unevenly: 2003 x 7168 26 us).
+inline int row_groups(const RowShape& f) { return f.threads == 64 ? 32 : 1024 / f.threads; }
 
 // ---- products of 8-bit codes (int8_gemm.hip)
 
@@ -199,6 +204,7 @@ struct Int8Plan {
   int parts;              // that tiles are cut into along k, their sums joined by a second kernel
   int64_t tiles;
   size_t part_bytes;      // of the sums of one part of every tile
+  bool stream;            // weights bypass the caches (the nt policy)
 };
 
 // Which kernel: the one that a model of their times, fitted to 4000 measurements of 500 sizes (1 to 16384 rows, 100
@@ -228,7 +234,7 @@ inline Int8Plan int8_plan(int64_t T, int64_t N, int64_t K, bool gated, int num_c
   const double mats = gated ? 2 : 1, weights = mats * double(N) * double(K);
   const double moved = (weights + double(T) * double(K) + 2.0 * double(T) * double(N)) / 3.9e6;
   const double stages = double(ceil_div(K, 128));
-  Int8Plan best{Int8Form::k256x256, 1, 0, 0};
+  Int8Plan best{Int8Form::k256x256, 1, 0, 0, false};
   double best_us = 1e300;
   for (const Tile& t : kTiles) {
     const int64_t tiles = ceil_div(T, t.rows) * ceil_div(N, gated ? t.wrows / 2 : t.wrows);
@@ -243,7 +249,7 @@ inline Int8Plan int8_plan(int64_t T, int64_t N, int64_t K, bool gated, int num_c
       us = 2.7 + (us > moved ? us + 0.25 * moved : moved + 0.25 * us);
       if (us < best_us) {
         best_us = us;
-        best = {t.form, parts, tiles, size_t(tiles) * t.rows * t.wrows * 4};
+        best = {t.form, parts, tiles, size_t(tiles) * t.rows * t.wrows * 4, false};
       }
     }
   }
@@ -255,9 +261,15 @@ inline Int8Plan int8_plan(int64_t T, int64_t N, int64_t K, bool gated, int num_c
       const double us = 3.7 + longest + 0.3 * std::fmin(alone, move);
       if (us < best_us) {
         best_us = us;
-        best = {nt == 1 ? Int8Form::kFew1 : Int8Form::kFew2, 1, 0, 0};
+        best = {nt == 1 ? Int8Form::kFew1 : Int8Form::kFew2, 1, 0, 0, false};
       }
     }
+  // Weights that one workgroup reads and no other, and that are too many to be found in the Infinity Cache by the
+  // next call: 8 rows, 28672 channels, K 4096 (117 MB) 24.0 us, 21.4 past the caches; 40 rows 24.4, 21.8.  59 MB
+  // that come back after two others 10.3, 12.5 past the caches.
+  const bool once = best.form == Int8Form::k64x128 ? best.parts == 1 && T <= 64
+                                                   : best.form <= Int8Form::kFew2 && T <= 16;
+  best.stream = once && weights >= double(96 << 20);
   return best;
 }
 

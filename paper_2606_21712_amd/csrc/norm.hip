@@ -70,39 +70,67 @@ __device__ __forceinline__ void block_sum(float& sum, uint32_t& top, float (*slo
   }
 }
 
+// A workgroup walks rows; while it works on one, the next one's x and y are on their way.  Norm weights and a gate of
+// the channels stay in registers (read again for each row, from the L2, they cost a third: 9001 x 7168 133 us
+// against 102).  Rows of more than 16384 leave no registers for either.
+//
+// Bound by memory: 9001 x 7168 with a post norm (516 MB) 97 us, 5.3 TB/s (without the row ahead 102), with codes
+// 85; 2003 x 7168 24.6 (30.9); one row of 4096 3.2 us, the latency of a load, two sums and a store.
 template <int NT, int V, bool F32, bool CODES>
 __global__ __launch_bounds__(NT) void norm_join_kernel(NormJoin a) {
   constexpr int kElt = F32 ? 4 : 2;
+  constexpr bool kRoom = NT * V <= 2048;
   __shared__ float s_part[4][NT / kWave][2];
   const int nvec = a.H / 8;
   const float per = 1.0f / float(a.H);
   const bool full = a.gate_kind == kGateFull, channel = a.gate_kind == kGateChannel;
   const char* const xs = static_cast<const char*>(a.x);
-  // weights: the same for every row
+  auto weights = [&](const uint16_t* w, int vec) {
+    const u32x4 zero = {0u, 0u, 0u, 0u};
+    return vec < nvec && w != nullptr ? reinterpret_cast<const u32x4*>(w)[vec] : zero;
+  };
   u32x4 w_post[V], w_pre[V], gate[V];
-  const u32x4 zero = {0u, 0u, 0u, 0u};
+  if (kRoom) {
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
-    const int vec = int(threadIdx.x) + i * NT;
-    const bool in = vec < nvec;
-    w_post[i] = in && a.w_post != nullptr ? reinterpret_cast<const u32x4*>(a.w_post)[vec] : zero;
-    w_pre[i] = in && a.w_pre != nullptr ? reinterpret_cast<const u32x4*>(a.w_pre)[vec] : zero;
-    gate[i] = in && channel ? reinterpret_cast<const u32x4*>(a.gate)[vec] : zero;
+    for (int i = 0; i < V; ++i) {
+      const int vec = int(threadIdx.x) + i * NT;
+      w_post[i] = weights(a.w_post, vec);
+      w_pre[i] = weights(a.w_pre, vec);
+      if (channel) gate[i] = weights(a.gate, vec);
+    }
   }
   // without weights the factors are 1
   const float post_add = a.w_post != nullptr ? a.offset : 1.0f, pre_add = a.w_pre != nullptr ? a.offset : 1.0f;
-  int turn = 0;
-  for (int64_t r = blockIdx.x; r < a.T; r += gridDim.x) {
-    Raw<F32> xr[V];
-    u32x4 yr[V];
+  Raw<F32> xr[V], xn[V];
+  u32x4 yr[V], yn[V];
+  auto fetch = [&](Raw<F32>(&x)[V], u32x4(&y)[V], int64_t r) {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const int vec = int(threadIdx.x) + i * NT;
       if (vec < nvec) {
-        xr[i].load(xs + r * a.x_stride * kElt, vec);
-        if (a.y != nullptr) yr[i] = reinterpret_cast<const u32x4*>(a.y + r * a.y_stride)[vec];
-        if (full) gate[i] = reinterpret_cast<const u32x4*>(a.gate + r * a.gate_stride)[vec];
+        x[i].load(xs + r * a.x_stride * kElt, vec);
+        if (a.y != nullptr) y[i] = reinterpret_cast<const u32x4*>(a.y + r * a.y_stride)[vec];
       }
+    }
+  };
+  if (kRoom) fetch(xn, yn, blockIdx.x);
+  int turn = 0;
+  for (int64_t r = blockIdx.x; r < a.T; r += gridDim.x) {
+    if (kRoom) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        xr[i] = xn[i];
+        yr[i] = yn[i];
+      }
+      if (r + gridDim.x < a.T) fetch(xn, yn, r + gridDim.x);
+    } else {
+      fetch(xr, yr, r);
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int vec = int(threadIdx.x) + i * NT;
+      if (full && vec < nvec) gate[i] = reinterpret_cast<const u32x4*>(a.gate + r * a.gate_stride)[vec];
+      if (!kRoom && channel) gate[i] = weights(a.gate, vec);
     }
     float scale = a.alpha;
     if (a.gate_kind == kGateToken) {
@@ -136,7 +164,7 @@ __global__ __launch_bounds__(NT) void norm_join_kernel(NormJoin a) {
         unpack_bf16(yr[i], f);
         if (a.post) {
           float w[8];
-          unpack_bf16(w_post[i], w);
+          unpack_bf16(kRoom ? w_post[i] : weights(a.w_post, vec), w);
 #pragma unroll
           for (int k = 0; k < 8; ++k) f[k] *= w[k] + post_add;
         }
@@ -151,7 +179,7 @@ __global__ __launch_bounds__(NT) void norm_join_kernel(NormJoin a) {
         Raw<F32>::store(static_cast<char*>(a.x_out) + r * a.x_out_stride * kElt, vec, x[i]);
       }
       float w[8];
-      unpack_bf16(w_pre[i], w);
+      unpack_bf16(kRoom ? w_pre[i] : weights(a.w_pre, vec), w);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         sum = fmaf(x[i][k], x[i][k], sum);
@@ -245,16 +273,15 @@ void quantize(const uint16_t* src, int64_t stride, int64_t rows, int K, int8_t* 
 
 hipError_t launch_norm_join(const NormJoin& a, int num_cu, hipStream_t s) {
   const RowShape f = row_shape(a.H, a.T, num_cu);
-  const int grid = int(std::min<int64_t>(a.T, int64_t(num_cu) * 2048 / f.threads));
+  const int grid = int(std::min<int64_t>(a.T, int64_t(num_cu) * row_groups(f)));
   switch (f.threads * 8 + f.vectors) {
     case 64 * 8 + 1: norm_join<64, 1>(a, grid, s); break;
     case 64 * 8 + 2: norm_join<64, 2>(a, grid, s); break;
     case 64 * 8 + 4: norm_join<64, 4>(a, grid, s); break;
     case 256 * 8 + 1: norm_join<256, 1>(a, grid, s); break;
     case 256 * 8 + 2: norm_join<256, 2>(a, grid, s); break;
-    case 256 * 8 + 4: norm_join<256, 4>(a, grid, s); break;
     case 512 * 8 + 1: norm_join<512, 1>(a, grid, s); break;
-    case 512 * 8 + 4: norm_join<512, 4>(a, grid, s); break;
+    case 512 * 8 + 2: norm_join<512, 2>(a, grid, s); break;
     case 1024 * 8 + 1: norm_join<1024, 1>(a, grid, s); break;
     case 1024 * 8 + 2: norm_join<1024, 2>(a, grid, s); break;
     default: norm_join<1024, 4>(a, grid, s); break;
@@ -272,9 +299,8 @@ hipError_t launch_quantize_int8(const uint16_t* src, int64_t stride, int64_t row
     case 64 * 32 + 4: quantize<64, 4>(src, stride, rows, K, codes, scales, grid, s); break;
     case 256 * 32 + 1: quantize<256, 1>(src, stride, rows, K, codes, scales, grid, s); break;
     case 256 * 32 + 2: quantize<256, 2>(src, stride, rows, K, codes, scales, grid, s); break;
-    case 256 * 32 + 4: quantize<256, 4>(src, stride, rows, K, codes, scales, grid, s); break;
     case 512 * 32 + 1: quantize<512, 1>(src, stride, rows, K, codes, scales, grid, s); break;
-    case 512 * 32 + 4: quantize<512, 4>(src, stride, rows, K, codes, scales, grid, s); break;
+    case 512 * 32 + 2: quantize<512, 2>(src, stride, rows, K, codes, scales, grid, s); break;
     case 1024 * 32 + 1: quantize<1024, 1>(src, stride, rows, K, codes, scales, grid, s); break;
     case 1024 * 32 + 2: quantize<1024, 2>(src, stride, rows, K, codes, scales, grid, s); break;
     case 1024 * 32 + 4: quantize<1024, 4>(src, stride, rows, K, codes, scales, grid, s); break;
