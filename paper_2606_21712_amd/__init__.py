@@ -701,11 +701,16 @@ def moe_int8_code_bytes(rows, K) -> int:
     return lib().moe_int8_code_bytes(rows, K)
 
 
+_I8, _F32, _BF16 = torch.int8, torch.float32, torch.bfloat16
+
+
 def _on(index, *ts):
     """All tensors are on the GPU of that index, and contiguous."""
     for t in ts:
-        if t is not None and not (t.get_device() == index >= 0 and t.is_contiguous()):
-            raise ValueError("all tensors must be " + ("contiguous" if t.get_device() == index >= 0 else "on one GPU"))
+        if t is not None and (t.get_device() != index or not t.is_contiguous()):
+            raise ValueError("all tensors must be " + ("contiguous" if t.get_device() == index else "on one GPU"))
+    if index < 0:
+        raise ValueError("all tensors must be on one GPU")
 
 
 def _run(fn, index, stream, *args):
@@ -719,29 +724,32 @@ def _run(fn, index, stream, *args):
         _run(fn, index, stream, *args)
 
 
-def _matrix(t, name, shape, index, dtype=torch.bfloat16):
+def _matrix(t, name, shape, index, dtype=_BF16):
     """Row stride of a tensor [T, H] whose rows are in one piece."""
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}")
     if t.shape != shape:
         raise ValueError(f"{name} must be {tuple(shape)}")
-    if t.get_device() != index or index < 0:
+    if t.get_device() != index:
         raise ValueError("all tensors must be on one GPU")
-    if t.is_contiguous():
-        return shape[1]
+    return shape[1] if t.is_contiguous() else _row_stride(t, name)
+
+
+def _row_stride(t, name):
     row, one = t.stride()
     if one != 1:
         raise ValueError(f"{name}: rows must be in one piece")
     return row
 
 
-def _weight(w, name, H, index):
+def _weight(w, name, shape, index):
     """Address of a norm's weight: a tensor bf16 [H], or True for none."""
     if w is True:
         return None
-    if w.dtype != torch.bfloat16 or w.shape != (H,):
-        raise ValueError(f"{name} must be bf16 [{H}], or True")
-    _on(index, w)
+    if w.dtype is not _BF16 or w.shape != shape:
+        raise ValueError(f"{name} must be bf16 {shape}, or True")
+    if w.get_device() != index or not w.is_contiguous():
+        raise ValueError("all tensors must be contiguous, and on one GPU")
     return w.data_ptr()
 
 
@@ -772,9 +780,11 @@ def moe_norm_join(x, y=None, post=None, gate=None, sigmoid=False, alpha=1.0, pre
     x_out may be slices with rows in one piece."""
     shape, dt, index = x.shape, x.dtype, x.get_device()
     T, H = shape
-    if dt != torch.bfloat16 and dt != torch.float32:
+    if dt is not _BF16 and dt is not _F32:
         raise TypeError("x must be bf16 or f32")
-    xs = _matrix(x, "x", shape, index, dt)
+    if index < 0:
+        raise ValueError("all tensors must be on one GPU")
+    xs = H if x.is_contiguous() else _row_stride(x, "x")
     yp = gp = post_w = op = pre_w = zp = sp = None
     ys = gs = os_ = kind = 0
     if y is not None:
@@ -782,25 +792,28 @@ def moe_norm_join(x, y=None, post=None, gate=None, sigmoid=False, alpha=1.0, pre
         if gate is not None:
             gp, gs, kind = _gate(gate, T, H, index)
         if post is not None:
-            post_w = _weight(post, "post", H, index)
+            post_w = _weight(post, "post", (H,), index)
         if x_out is None:
             x_out = _new(shape, dt, x.device, stream)
         os_, op = _matrix(x_out, "x_out", shape, index, dt), x_out.data_ptr()
     elif post is not None or gate is not None or x_out is not None:
         raise ValueError("post, gate and x_out need y")
     if pre is not None:
-        pre_w = _weight(pre, "pre", H, index)
-        z = _like(z, "z", torch.int8 if int8 else torch.bfloat16, shape, x.device, stream)
+        pre_w = _weight(pre, "pre", (H,), index)
+        if z is None:
+            z = _new(shape, _I8 if int8 else _BF16, x.device, stream)
+        if _matrix(z, "z", shape, index, _I8 if int8 else _BF16) != H and T > 1:
+            raise ValueError("z must be contiguous")
         zp = z.data_ptr()
         if int8:
-            scales = _like(scales, "scales", torch.float32, (T,), x.device, stream)
+            scales = _like(scales, "scales", _F32, (T,), x.device, stream)
+            _on(index, scales)
             sp = scales.data_ptr()
         elif scales is not None:
             raise ValueError("scales need int8")
-        _on(index, z, scales)
     elif z is not None or scales is not None or int8:
         raise ValueError("z, scales and int8 need pre")
-    _run(lib().moe_norm_join, index, stream, x.data_ptr(), xs, DTYPE_BF16 if dt == torch.bfloat16 else DTYPE_F32, yp, ys,
+    _run(lib().moe_norm_join, index, stream, x.data_ptr(), xs, DTYPE_BF16 if dt is _BF16 else DTYPE_F32, yp, ys,
          post is not None, post_w, gp, gs, kind, bool(sigmoid), alpha, pre_w, offset, eps, T, H, op, os_, bool(int8), zp, sp)
     return x if y is None else x_out, z, scales
 
@@ -844,7 +857,7 @@ def moe_gated_int8_workspace_bytes(T, F, K) -> int:
 
 def _int8_inputs(x, scales, w):
     T, K = x.shape
-    if x.dtype != torch.int8 or scales.dtype != torch.float32:
+    if x.dtype is not _I8 or scales.dtype is not _F32:
         raise TypeError("x is int8 codes, its scales float32")
     N, wK = w.shape
     if scales.shape != (T,) or wK != K:
@@ -861,7 +874,7 @@ def _scratch(ws, need, device, stream):
         if not need:
             return None, 0
         ws = _new(need, torch.uint8, device, stream)
-    return ws.data_ptr(), ws.numel() * ws.element_size()
+    return ws.data_ptr(), ws.nbytes
 
 
 def moe_matmul_int8(x, scales, w, bias=None, y=None, ws=None, stream=None):
