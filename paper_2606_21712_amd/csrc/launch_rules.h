@@ -194,10 +194,9 @@ inline int row_groups(const RowShape& f) { return f.threads == 64 ? 32 : 1024 / 
 
 // ---- products of 8-bit codes (int8_gemm.hip)
 
-// The kernels: 16 rows of x with one or two tiles of 16 weight rows a wavefront, or LDS tiles of rows of x
-// by weight rows (gated: half of either matrix); of 128 x 128 one with a ring of three stages and one with
-// two stages, of which two workgroups share a compute unit.
-enum class Int8Form { kFew1, kFew2, k64x128, k128x128, k128x128Two, k192x256, k256x256 };
+// The kernels: 16 rows of x with one or two tiles of 16 weight rows a wavefront, or tiles of rows of x by weight
+// rows (gated: half of either matrix), the last two through LDS.
+enum class Int8Form { kFew1, kFew2, k32x128, k64x128, k96x128, k128x128, k160x256, k192x256, k256x256 };
 
 struct Int8Plan {
   Int8Form form;
@@ -207,69 +206,77 @@ struct Int8Plan {
   bool stream;            // weights bypass the caches (the nt policy)
 };
 
-// Which kernel: the one that a model of their times, fitted to 4000 measurements of 500 sizes (1 to 16384 rows, 100
-// to 30000 channels, K 256 to 16384, plain and gated), thinks the fastest.  Over these sizes its choice takes 2% more
-// than the fastest of all measured ones on average, 6% in one of ten.  us; a stage is 128 columns.
-//   LDS tiles: rounds of as many workgroups as run at once, each its stages and a rest, the last round
-//   with compute units to spare cheaper by the stage; operands and results at 3.9 TB/s beside it.
+// Which kernel: the one that a model of their times, fitted to 11000 measurements of 1100 sizes (1 to 16384 rows, 100
+// to 30000 channels, K 256 to 16384, plain and gated), thinks the fastest.  Over these sizes its choice takes 1.8% more
+// than the fastest of all measured ones on average, at most 36%.  us; a stage is 128 columns.
+//   Tiles: rounds of as many workgroups as run at once.  A stage takes what its operands take to pass
+//   through a compute unit, once for each workgroup there, and a tile a rest; all operands and results move
+//   once besides, and the weights a quarter more for each further tile of rows.
 //   Parts: another launch, and the sums written and read.
-//   Few rows: the latency of a wavefront's stages, the 1 KB pieces that pass through a compute unit, and
-//   the weights at 5.1 TB/s.
-// (332 rows, 6145 channels, K 4096: 17.0 on 128 x 128, 21.5 on 64 x 128, 34 on 192 x 256; 2003, 4608, 7168: 71, 76 on
-// 256 x 256, 112 on 128 x 128 with two workgroups; 128, 4096, 14336: 25.5 on 64 x 128 in four parts, 33.9 in two,
-// 51 whole; 16384, 4096, 14336: 754 on 256 x 256, 833 on 192 x 256, 923 on 128 x 128 with two.)
+//   Few rows: the latency of a wavefront's steps, or what passes through a compute unit, or the weights
+//   from memory, four fifths of that again for each further 16 rows.
+// (333 rows, 6145 channels, K 4096: 16.2 on 96 x 128, 18.8 on 128 x 128, 20.5 on 64 x 128, 70 on 192 x 256; 2003, 4608,
+// 7168: 64 on 160 x 256, 70 on 192 x 256, 76 on 256 x 256, 83 on 128 x 128; 64, 4096, 14336: 20.9 on 32 x 128 in four
+// parts, 22.6 in eight, 44 whole; 16384, 4096, 14336: 738 on 256 x 256, 813 on 192 x 256, 828 on 160 x 256.)
 inline Int8Plan int8_plan(int64_t T, int64_t N, int64_t K, bool gated, int num_cu) {
   struct Tile {
     Int8Form form;
-    int rows, wrows, together;     // workgroups of a compute unit
-    double alone, busy, rest;      // a stage with compute units to spare, and with all at work; the rest of a tile
+    int rows, wrows, together;     // workgroups that a compute unit holds
+    double alone, each, rest;      // a stage of one workgroup, of several for each of them; the rest of a tile
     int most_parts;
   };
   static constexpr Tile kTiles[] = {
-      {Int8Form::k64x128, 64, 128, 2, 0.23, 0.63, 1.9, 8},    {Int8Form::k128x128, 128, 128, 1, 0.33, 0.60, 2.3, 4},
-      {Int8Form::k128x128Two, 128, 128, 2, 0.65, 1.10, 2.0, 1}, {Int8Form::k192x256, 192, 256, 1, 0.81, 1.14, 9.0, 1},
-      {Int8Form::k256x256, 256, 256, 1, 1.03, 1.46, 12.3, 1},
+      {Int8Form::k32x128, 32, 128, 4, 0.096, 0.102, 2.0, 8},  {Int8Form::k64x128, 64, 128, 3, 0.183, 0.186, 1.8, 8},
+      {Int8Form::k96x128, 96, 128, 3, 0.204, 0.270, 1.8, 4},  {Int8Form::k128x128, 128, 128, 2, 0.299, 0.336, 2.1, 4},
+      {Int8Form::k160x256, 160, 256, 1, 0.65, 0.74, 5.5, 1}, {Int8Form::k192x256, 192, 256, 1, 0.80, 0.81, 6.8, 1},
+      {Int8Form::k256x256, 256, 256, 1, 1.06, 0.96, 9.1, 1},
   };
   const int64_t most = int64_t(1) << 23;     // workgroups of a launch
   const double mats = gated ? 2 : 1, weights = mats * double(N) * double(K);
-  const double moved = (weights + double(T) * double(K) + 2.0 * double(T) * double(N)) / 3.9e6;
+  const double others = double(T) * double(K) + 2.0 * double(T) * double(N);
   const double stages = double(ceil_div(K, 128));
   Int8Plan best{Int8Form::k256x256, 1, 0, 0, false};
   double best_us = 1e300;
+  int64_t rows = 0;
   for (const Tile& t : kTiles) {
-    const int64_t tiles = ceil_div(T, t.rows) * ceil_div(N, gated ? t.wrows / 2 : t.wrows);
+    const int64_t mtiles = ceil_div(T, t.rows), tiles = mtiles * ceil_div(N, gated ? t.wrows / 2 : t.wrows);
+    const double moved = (weights * (1 + 0.28 * double(mtiles - 1)) + others) / 10.0e6;
     for (int parts = 1; parts <= t.most_parts; parts *= 2) {
       const int64_t blocks = tiles * parts, round = int64_t(num_cu) * t.together;
       if (blocks > most && t.form != Int8Form::k256x256) continue;
       if (parts > 1 && (parts > stages || blocks > 4 * round)) continue;
-      const double full = t.busy * stages / parts + t.rest, left = double(blocks % round);
-      double us = double(blocks / round) * full;
-      if (left > 0) us += left <= num_cu ? t.alone * stages / parts + t.rest : full;
-      if (parts > 1) us += 4.4 + 1.15e-6 * mats * double(T) * double(N) * parts;
-      us = 2.7 + (us > moved ? us + 0.25 * moved : moved + 0.25 * us);
+      const auto some = [&](int64_t n) {     // workgroups, up to a round of them
+        return stages / parts * std::fmax(t.alone, double(ceil_div(n, num_cu)) * t.each) + t.rest;
+      };
+      double us = 2.8 + moved + double(blocks / round) * some(round);
+      if (blocks % round) us += some(blocks % round);
+      if (parts > 1) us += 2.7 + 1.17e-6 * mats * double(T) * double(N) * parts;
       if (us < best_us) {
         best_us = us;
         best = {t.form, parts, tiles, size_t(tiles) * t.rows * t.wrows * 4, false};
+        rows = t.rows;
       }
     }
   }
-  if (T <= 128)
-    for (int nt = gated ? 2 : 1; nt <= 2; ++nt) {
-      const double blocks = double(ceil_div(ceil_div(N, 16), gated ? 1 : nt) * ceil_div(T, 16)), steps = std::ceil(stages / 8);
-      const double alone = 0.48 * steps + 1.2, move = blocks / num_cu * steps * 8 * (0.31 * nt + 0.014) * 2.048 / 13.8;
-      const double longest = std::fmax(std::fmax(alone, move), weights / 5.1e6);
-      const double us = 3.7 + longest + 0.3 * std::fmin(alone, move);
-      if (us < best_us) {
-        best_us = us;
-        best = {nt == 1 ? Int8Form::kFew1 : Int8Form::kFew2, 1, 0, 0, false};
-      }
+  if (T <= 128) {
+    // two tiles of weights a wavefront, unless that left compute units without any (1, 4096, 14336: 12.1 us on 256
+    // workgroups, 14.0 on 128)
+    const double more = double(ceil_div(T, 16)), steps = std::ceil(stages / 8), units = double(ceil_div(N, 16)) * more;
+    const int nt = gated || units > num_cu ? 2 : 1;
+    const double blocks = gated ? units : std::ceil(units / nt);
+    const double alone = 0.116 * steps + 2.6, move = blocks / num_cu * steps * (0.364 * nt + 0.132);
+    const double memory = weights / 6.2e6 * (1 + 0.8 * (more - 1));
+    const double first = std::fmax(alone, std::fmax(move, memory));
+    const double second = std::fmax(std::fmin(alone, move), std::fmin(std::fmax(alone, move), memory));
+    if (2.95 + first + 0.115 * second < best_us) {
+      best = {nt == 1 ? Int8Form::kFew1 : Int8Form::kFew2, 1, 0, 0, false};
+      rows = 16;
     }
+  }
   // Weights that one workgroup reads and no other, and that are too many to be found in the Infinity Cache by the
-  // next call: 8 rows, 28672 channels, K 4096 (117 MB) 24.0 us, 21.4 past the caches; 40 rows 24.4, 21.8.  59 MB
-  // that come back after two others 10.3, 12.5 past the caches.
-  const bool once = best.form == Int8Form::k64x128 ? best.parts == 1 && T <= 64
-                                                   : best.form <= Int8Form::kFew2 && T <= 16;
-  best.stream = once && weights >= double(96 << 20);
+  // next call: 8 rows, 28672 channels, K 4096 (117 MB) 24.0 us, 21.4 past the caches; 2 rows, 8441, 10928 (92 MB) 25.5,
+  // 20.3.  59 MB that come back after two others 10.3, 12.5 past the caches.
+  best.stream = best.parts == 1 && T <= rows && T <= 128 && weights >= double(64 << 20);
   return best;
 }
 

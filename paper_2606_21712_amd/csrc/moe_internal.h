@@ -213,6 +213,7 @@ struct Int8Product {
   int steps;                              // of 64 columns, an even number
   int __attribute__((ext_vector_type(4)))* partial;   // sums of tiles that are cut along k
 };
+void launch_int8_large(const Int8Product& p, bool rows256, hipStream_t s);   // tiles of 256 or 192 rows by 256
 struct Int8Plan;                          // launch_rules.h
 hipError_t launch_int8_product(const Int8Product& p, const Int8Plan& plan, hipStream_t s);
 

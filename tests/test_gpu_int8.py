@@ -9,6 +9,7 @@ import torch
 
 import paper_2606_21712_amd as moe
 from gpu_util import log
+from int8_forms import FORMS, STREAMED
 
 pytestmark = pytest.mark.gpu
 BF, F32, F64 = torch.bfloat16, torch.float32, torch.float64
@@ -158,6 +159,67 @@ def test_gated(T, F, K):
     ref = g * torch.sigmoid(g) * u
     err = (h.cpu().double() - ref).abs()
     assert (err <= gated_tolerance(g, u, ref)).all(), float((err / gated_tolerance(g, u, ref)).max())
+
+
+@pytest.fixture
+def budget():
+    yield moe.set_cu_budget
+    moe.set_cu_budget(0)
+
+
+def check_product(T, N, K, gated, sparse=False):
+    """One product of each kind, bit for bit or (gated) within its tolerance, and the rows around the output untouched."""
+    x, sx = random_int8(T, K, T + K)
+    w, sw = random_int8(N, K, N)
+    around = torch.full((T + 16, N), 5.0, dtype=BF, device="cuda")
+    out = around[8:8 + T]
+    pw = moe.moe_pack_int8(w.cuda(), sw.cuda())
+    if gated:
+        v, sv = random_int8(N, K, N + 3)
+        moe.moe_gated_int8(x.cuda(), sx.cuda(), pw, moe.moe_pack_int8(v.cuda(), sv.cuda()), h=out)
+        g, u = (sums(x, a) * sx.double()[:, None] * s.double() for a, s in ((w, sw), (v, sv)))
+        ref = g * torch.sigmoid(g) * u
+        assert ((out.cpu().double() - ref).abs() <= gated_tolerance(g, u, ref)).all()
+    else:
+        bias = torch.randn(N, generator=gen(N)).to(BF)
+        moe.moe_matmul_int8(x.cuda(), sx.cuda(), pw, bias.cuda(), y=out)
+        assert torch.equal(bits(out.cpu()), bits(matmul_plain(x, sx, w, sw, bias)))
+    assert (around[:8] == 5).all() and (around[8 + T:] == 5).all()
+
+
+@pytest.mark.parametrize("form,parts,T,N,K,gated,cus", FORMS)
+def test_every_kernel(budget, form, parts, T, N, K, gated, cus):
+    """Every kernel at every end of its ring's loop, whole and cut along k."""
+    log(f"[gpu] int8 {form} in {parts}: {T} x {N} x {K} gated={gated} cus={cus}")
+    budget(cus)
+    check_product(T, N, K, gated)
+
+
+@pytest.mark.parametrize("form,parts,T,N,K,gated,cus", STREAMED)
+def test_every_streaming_kernel(form, parts, T, N, K, gated, cus):
+    log(f"[gpu] int8 {form} past the caches: {T} x {N} x {K} gated={gated}")
+    check_product(T, N, K, gated)
+
+
+@pytest.mark.parametrize("cus", [1, 8, 304])
+def test_workspaces_by_budget(budget, cus):
+    """The workspace is what the query says, no more is touched, and the result does not depend on the budget."""
+    log(f"[gpu] int8 workspaces: budget {cus}")
+    T, N, K = 100, 260, 8208
+    x, sx = (t.cuda() for t in random_int8(T, K, 1))
+    w = moe.moe_pack_int8(*(t.cuda() for t in random_int8(N, K, 2)))
+    want = moe.moe_matmul_int8(x, sx, w), moe.moe_gated_int8(x, sx, w, w)
+    budget(cus)
+    for i, (call, size) in enumerate([(moe.moe_matmul_int8, moe.moe_matmul_int8_workspace_bytes),
+                                      (moe.moe_gated_int8, moe.moe_gated_int8_workspace_bytes)]):
+        n = size(T, N, K)
+        ws = torch.full((n + 512,), 77, dtype=torch.uint8, device="cuda")
+        got = call(x, sx, w, *[w] * i, ws=ws[:n])
+        assert torch.equal(bits(got), bits(want[i])) and (ws[n:] == 77).all()
+        if n:
+            with pytest.raises(moe.MoEError) as e:
+                call(x, sx, w, *[w] * i, ws=ws[:n - 16])
+            assert e.value.status == 3
 
 
 @pytest.mark.parametrize("T", [1, 40, 300])
