@@ -567,14 +567,16 @@ moe_status moe_kv8_attention(const void* q, int64_t T, int32_t q_heads, const mo
  *   y           bf16 [T, H]    a block's output; NULL: x' = x, and post, w_post, gate and x_out are 0 or NULL
  *   w_post, w_pre  bf16 [H]    NULL: factors of 1 (without offset).  offset: 0, or 1 for weights stored less 1
  *   gate        bf16, by gate_kind: MOE_GATE_CHANNEL [H], MOE_GATE_TOKEN [T] (gate_stride elements
- *               apart), MOE_GATE_FULL [T, H]; with sigmoid = 1 the gate is 1 / (1 + exp(-gate))
- *   x_out       dt [T, H]      out: x'; may be x itself (then x_out_stride = x_stride)
+ *               apart, a column at any element), MOE_GATE_FULL [T, H]; with sigmoid = 1 a gate counts as
+ *               1 / (1 + exp(-gate))
+ *   x_out       dt [T, H]      out: x'; may be x itself (then x_out_stride = x_stride), and overlaps nothing else
  *   z           out: bf16 [T, H], or with z_codes = 1 int8 [T, H] and z_scales f32 [T].  NULL: not computed
  *   *_stride    elements from a row to the next, rows in whole 16-byte pieces
  *
  * Arithmetic is fp32, x' and z are rounded once; z is taken of x' before its rounding.  The codes of z
  * are those of x' (offset + w_pre), the norm's factor is in the scale alone.  Squares are summed in fp32:
- * rows of more than 2^60 in size overflow.  A NaN or infinity stays in its row.
+ * rows of more than 2^60 in size overflow.  A NaN or infinity stays in its row.  The order of the sums depends on H, T
+ * and the compute-unit budget (moe_set_cu_budget), on nothing else.
  * Errors: INVALID_ARGUMENT for H not a positive multiple of 8, T < 0, eps < 0, numbers that are not
  * finite, flags that are not 0 or 1, an unknown gate_kind, bad strides, arguments without the one they belong to,
  * null or misaligned pointers; UNSUPPORTED for H > 32768 or an unknown dtype.
@@ -614,7 +616,8 @@ moe_status moe_pack_int8(const int8_t* codes, int64_t rows, int32_t K, int8_t* o
  *   ws, ws_bytes  device scratch of at least moe_matmul_int8_workspace_bytes(); not to be shared by
  *                 calls that overlap
  *
- * The integer sums are exact, so results depend neither on how a call is cut up nor on the other rows;
+ * The integer sums are exact, so results depend neither on how a call is cut up (by its sizes and the
+ * compute-unit budget, which the workspace's size depends on too) nor on the other rows;
  * scales and bias are applied in fp32 in this order, y is rounded once.  A token's NaN scale is
  * in its row alone.
  * Errors: INVALID_ARGUMENT for T < 0, N < 1, K not a positive multiple of 16, null or misaligned
@@ -668,7 +671,8 @@ moe_status moe_profiler_record(int i, const char** name, float* ms);
  * caller can leave compute units to concurrent streams; the grouped GEMMs then run
  * these kernels for small groups too, where a kernel with one workgroup per tile is
  * otherwise faster.  The fp32 GEMMs, the fused router and moe_matvec_int4 choose their tiles
- * by it.  The first kernel of moe_few_tokens is persistent too; its down projection, and
+ * by it, as do moe_matmul_int8 and moe_gated_int8; moe_norm_join and moe_quantize_int8 share out their rows.  The first
+ * kernel of moe_few_tokens is persistent too; its down projection, and
  * moe_kv8_attention over long sequences, are cut into parts for n compute units (with more
  * tiles than that, a workgroup for each tile).
  * n = 0 restores the device's count.  Results do not depend on it beyond fp32

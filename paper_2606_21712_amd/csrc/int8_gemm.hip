@@ -156,12 +156,14 @@ __device__ __forceinline__ void put_strip(const Int8Product& p, const i32x4 (&ac
     *reinterpret_cast<u32x2*>(out + (lane & 15) * kPitch + f * 32 + (lane >> 4) * 8) =
         u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
   }
+  wave_order();
   constexpr int kPieces = 2 * kFrags;                        // of a row
 #pragma unroll
   for (int i = lane; i < 16 * kPieces; i += 64) {
     const int r = i / kPieces, piece = i % kPieces;
     if (tb + r < p.T) put_piece(p.y + int64_t(tb + r) * p.N, nb + 8 * piece, p.N, out + r * kPitch + piece * 16);
   }
+  wave_order();
 }
 
 template <bool GATED, int A, int B, int XS, bool SPLIT, int POLICY>
@@ -281,6 +283,7 @@ __global__ __launch_bounds__(256, A * B <= 16 ? 2 : 1) void int8_direct_kernel(I
   for (int j = 0; j < XS - 1; ++j)
     if (kt + j < KT) step(xs[j], xs[(j + 1) % XS], w[(2 * j + kSlots - 1) % kSlots], w[2 * j], w[2 * j + 1], kt + j);
 
+  __builtin_amdgcn_s_waitcnt(wait_all_but(0));                // for the zeros that are on their way to LDS
   if constexpr (SPLIT) {
     i32x4* const to = p.partial + (int64_t(L) * 4 + wave) * (A * B * 64) + lane;
 #pragma unroll

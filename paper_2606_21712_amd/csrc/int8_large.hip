@@ -46,12 +46,14 @@ __device__ __forceinline__ void put_rows(const Int8Product& p, const i32x16 (&ac
                              p.bias != nullptr);
       *reinterpret_cast<u32x2*>(out + r32 * kPitch + at * 2) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
     }
+  wave_order();
   constexpr int kPieces = kCols / 8;                         // of a row
 #pragma unroll
   for (int i = lane; i < 32 * kPieces; i += 64) {
     const int r = i / kPieces, piece = i % kPieces;
     if (tb + r < p.T) put_piece(p.y + int64_t(tb + r) * p.N, nb + 8 * piece, p.N, out + r * kPitch + piece * 16);
   }
+  wave_order();
 }
 
 template <bool GATED, int MI, int NI>

@@ -78,6 +78,13 @@ struct Mix {
   }
 };
 
+// What the lanes of a wavefront wrote to LDS is read by others of them after this, and the other way about: they
+// run together, only the compiler must not move either past it.
+__device__ __forceinline__ void wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // s_waitcnt: every LDS read done, and all but the last n loads.
 constexpr int wait_all_but(int n) { return 0x0070 | (n & 15) | ((n >> 4) << 14); }
 

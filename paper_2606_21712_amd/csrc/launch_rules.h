@@ -244,7 +244,7 @@ inline Int8Plan int8_plan(int64_t T, int64_t N, int64_t K, bool gated, int num_c
     for (int parts = 1; parts <= t.most_parts; parts *= 2) {
       const int64_t blocks = tiles * parts, round = int64_t(num_cu) * t.together;
       if (blocks > most && t.form != Int8Form::k256x256) continue;
-      if (parts > 1 && (parts > stages || blocks > 4 * round)) continue;
+      if (parts > 1 && (parts > stages || blocks > 4 * round || blocks > 1 << 20)) continue;
       const auto some = [&](int64_t n) {     // workgroups, up to a round of them
         return stages / parts * std::fmax(t.alone, double(ceil_div(n, num_cu)) * t.each) + t.rest;
       };

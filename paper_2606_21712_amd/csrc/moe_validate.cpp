@@ -724,11 +724,19 @@ Check validate_norm_join(const void* x, int64_t x_stride, int x_dt, const void* 
     MOE_TRY(stride_of(fn, "y_stride", y_stride, H, 8));
     MOE_TRY(ptr(fn, "x_out", x_out));
     MOE_TRY(stride_of(fn, "x_out_stride", x_out_stride, H, per16));
+    // in place a row is read before it is written, but not before the rows of other workgroups are
+    if (x_out == x && x_out_stride != x_stride && T > 1)
+      return fail(MOE_ERR_INVALID_ARGUMENT, fn, "x_out is x, with x_out_stride=%lld and not %lld", x_out_stride, x_stride);
     if (w_post != nullptr && !post) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "w_post without post");
     if (w_post != nullptr) MOE_TRY(ptr(fn, "w_post", w_post));
     if ((gate != nullptr) != (gate_kind != 0))
       return fail(MOE_ERR_INVALID_ARGUMENT, fn, "gate and gate_kind=%lld do not fit", gate_kind);
-    if (gate != nullptr) MOE_TRY(ptr(fn, "gate", gate));
+    if (gate_kind == MOE_GATE_TOKEN) {           // a column of a wider matrix
+      if (reinterpret_cast<uintptr_t>(gate) % 2 != 0)
+        return fail(MOE_ERR_INVALID_ARGUMENT, fn, "gate is not 2-byte aligned");
+    } else if (gate != nullptr) {
+      MOE_TRY(ptr(fn, "gate", gate));
+    }
     if (gate_kind == MOE_GATE_FULL) MOE_TRY(stride_of(fn, "gate_stride", gate_stride, H, 8));
     if (gate_kind == MOE_GATE_TOKEN && (gate_stride < 1 || gate_stride >= (int64_t(1) << 40)))
       return fail(MOE_ERR_INVALID_ARGUMENT, fn, "gate_stride=%lld must be >= 1", gate_stride);

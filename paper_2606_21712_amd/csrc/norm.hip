@@ -271,9 +271,12 @@ void quantize(const uint16_t* src, int64_t stride, int64_t rows, int K, int8_t* 
 
 }  // namespace
 
+// Of a launch, whatever the budget: under 2^32 threads.
+constexpr int64_t kMostGroups = 1 << 21;
+
 hipError_t launch_norm_join(const NormJoin& a, int num_cu, hipStream_t s) {
   const RowShape f = row_shape(a.H, a.T, num_cu);
-  const int grid = int(std::min<int64_t>(a.T, int64_t(num_cu) * row_groups(f)));
+  const int grid = int(std::min<int64_t>(std::min(a.T, kMostGroups), int64_t(num_cu) * row_groups(f)));
   switch (f.threads * 8 + f.vectors) {
     case 64 * 8 + 1: norm_join<64, 1>(a, grid, s); break;
     case 64 * 8 + 2: norm_join<64, 2>(a, grid, s); break;
@@ -292,7 +295,7 @@ hipError_t launch_norm_join(const NormJoin& a, int num_cu, hipStream_t s) {
 hipError_t launch_quantize_int8(const uint16_t* src, int64_t stride, int64_t rows, int K, int8_t* codes, float* scales,
                                 int num_cu, hipStream_t s) {
   const RowShape f = row_shape(K, rows, num_cu);
-  const int grid = int(std::min<int64_t>(rows, int64_t(num_cu) * 2048 / f.threads));
+  const int grid = int(std::min<int64_t>(std::min(rows, kMostGroups), int64_t(num_cu) * 2048 / f.threads));
   switch (f.threads * 32 + f.vectors) {
     case 64 * 32 + 1: quantize<64, 1>(src, stride, rows, K, codes, scales, grid, s); break;
     case 64 * 32 + 2: quantize<64, 2>(src, stride, rows, K, codes, scales, grid, s); break;

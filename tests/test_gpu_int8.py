@@ -167,7 +167,7 @@ def budget():
     moe.set_cu_budget(0)
 
 
-def check_product(T, N, K, gated, sparse=False):
+def check_product(T, N, K, gated):
     """One product of each kind, bit for bit or (gated) within its tolerance, and the rows around the output untouched."""
     x, sx = random_int8(T, K, T + K)
     w, sw = random_int8(N, K, N)
@@ -418,6 +418,11 @@ def test_norm_join_slices_in_place_and_streams():
         a = moe.moe_norm_join(x, y, gate=tok[:, 8:9], pre=w2)[1]
         b = moe.moe_norm_join(x, y, gate=tok[:, 8:9].contiguous(), pre=w2)[1]
         assert torch.equal(bits(a), bits(b))
+        a = moe.moe_norm_join(x, y, gate=tok[:, 13:14], pre=w2)[1]              # not at a whole piece
+        b = moe.moe_norm_join(x, y, gate=tok[:, 13:14].contiguous(), pre=w2)[1]
+        assert torch.equal(bits(a), bits(b))
+        with pytest.raises(moe.MoEError):
+            moe.moe_norm_join(wide_x[:, :H], sy, x_out=wide_x.view(-1)[:2 * T * H].view(T, 2 * H)[:, :H])   # in place, other rows
     assert moe.moe_norm_join(x[:0], y[:0], pre=w2)[1].shape == (0, H)
 
 
@@ -511,3 +516,48 @@ def test_block_in_a_graph():
         torch.cuda.synchronize()
         for a, b in zip(out, want):
             assert torch.equal(bits(a), bits(b)), (i, x.shape)
+
+
+def test_blocks_on_two_streams_at_once():
+    """Blocks of two sizes on two streams, none waiting for the other, on the same weights: each the bits that it
+    has alone.  New outputs and workspaces are the streams' own."""
+    log("[gpu] dense blocks on two streams")
+    _, w = block_weights(1024, 2816, 70)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    xs = [torch.randn(T, 1024, generator=gen(T)).to(BF).cuda() for T in (24, 90)]
+    want = [block(x, x, w) for x in xs]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(8):
+        for i, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                got[i].append(block(xs[i], xs[i], w))
+    torch.cuda.synchronize()
+    for g, one in zip(got, want):
+        assert all(torch.equal(bits(a), bits(b)) for o in g for a, b in zip(o, one))
+
+
+def test_refusals_of_tensors():
+    """What the binding turns away on the GPU: other types, shapes, devices, rows in pieces, workspaces too small."""
+    log("[gpu] int8: refusals")
+    x, y = (torch.zeros(4, 64, dtype=BF, device="cuda") for _ in range(2))
+    w, q, s = torch.ones(64, dtype=BF, device="cuda"), torch.zeros(4, 64, dtype=torch.int8, device="cuda"), torch.ones(4, device="cuda")
+    p, odd = moe.moe_pack_int8(q, s), moe.moe_pack_int8(q[:3].contiguous(), s[:3])
+    for error, call in [
+            (ValueError, lambda: moe.moe_norm_join(x, y.cpu(), pre=w)), (ValueError, lambda: moe.moe_norm_join(x, y[:3], pre=w)),
+            (TypeError, lambda: moe.moe_norm_join(x, y.half(), pre=w)), (ValueError, lambda: moe.moe_norm_join(x, y, pre=w[:8])),
+            (ValueError, lambda: moe.moe_norm_join(x, y, pre=w.float())), (ValueError, lambda: moe.moe_norm_join(x, post=w)),
+            (ValueError, lambda: moe.moe_norm_join(x, y.t().contiguous().t())), (ValueError, lambda: moe.moe_norm_join(x, y, int8=True)),
+            (ValueError, lambda: moe.moe_norm_join(x, y, gate=x[:3])), (TypeError, lambda: moe.moe_norm_join(x, y, gate=x.float())),
+            (ValueError, lambda: moe.moe_norm_join(x, y, pre=w, z=torch.zeros(4, 128, dtype=BF, device="cuda")[:, :64])),
+            (ValueError, lambda: moe.moe_norm_join(x, y, pre=w, scales=s)), (moe.MoEError, lambda: moe.moe_norm_join(x)),
+            (moe.MoEError, lambda: moe.moe_norm_join(x[:, :12], y[:, :12])), (moe.MoEError, lambda: moe.moe_norm_join(x[:1].expand(4, 64), y)),
+            (TypeError, lambda: moe.moe_quantize_int8(q)), (moe.MoEError, lambda: moe.moe_quantize_int8(x[:, :24])),
+            (ValueError, lambda: moe.moe_pack_int8(q[:, ::2], s)), (ValueError, lambda: moe.moe_pack_int8(q, s[:3])),
+            (TypeError, lambda: moe.moe_matmul_int8(x, s, p)), (TypeError, lambda: moe.moe_matmul_int8(q, s.to(BF), p)),
+            (ValueError, lambda: moe.moe_matmul_int8(q, s[:3], p)), (ValueError, lambda: moe.moe_matmul_int8(q[:, :32], s, p)),
+            (ValueError, lambda: moe.moe_matmul_int8(q.cpu(), s.cpu(), p)), (ValueError, lambda: moe.moe_matmul_int8(q, s, p, bias=s)),
+            (ValueError, lambda: moe.moe_matmul_int8(q[:, ::2], s, moe.moe_pack_int8(q[:, :32].contiguous(), s))),
+            (ValueError, lambda: moe.moe_gated_int8(q, s, p, odd))]:
+        with pytest.raises(error):
+            call()

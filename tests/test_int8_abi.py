@@ -66,6 +66,9 @@ def test_norm_join(L):
                 dict(y=None, post=0, wpost=None, gate=None, kind=0, out=None, z=None, zs=None, wpre=None, codes=0)):
         assert join(L, **bad) == INVALID, bad
         assert b"moe_norm_join" in L.moe_last_error()
+    # in place only with the same rows; a column of gates anywhere, but at a whole element
+    for bad in (dict(out=P, os_=512), dict(out=P, xs=512, os_=256), dict(kind=2, gate=P + 1)):
+        assert join(L, **bad) == INVALID, bad
     for bad in (dict(H=32776, xs=1 << 16), dict(dt=7), dict(T=(1 << 31) + 1)):
         assert join(L, **bad) == UNSUPPORTED, bad
     assert join(L, T=0, x=None, y=None, out=None, z=None, zs=None) == 0
