@@ -15,7 +15,8 @@ __device__ __forceinline__ i32x4 mfma_i8(u32x4 a, u32x4 b, i32x4 c) {
 }
 
 // ------------------------------------------------------------------ pack
-// One wavefront a step of 16 rows x 64 columns.
+// One wavefront a step of 16 rows x 64 columns: 16 pieces of 64 bytes in, one of 1 KB out.  Bound by memory, once
+// for each matrix.
 __global__ __launch_bounds__(64) void pack_int8_kernel(const int8_t* __restrict__ codes, int64_t rows, int K, int steps,
                                                        int8_t* __restrict__ out) {
   const int lane = threadIdx.x;
@@ -45,6 +46,11 @@ __device__ __forceinline__ void store4(uint16_t* row, int n, int N, const float 
 // the first operand, streamed from memory into registers, x the second, from the caches.  KS wavefronts deal the
 // steps of 128 columns along k among themselves (both halves of a line of x to one of them) and add their sums in
 // LDS; P steps are in flight.  More rows are other workgroups', which find the weights in the L2.
+//
+// Bound by the reads of the weights, after a launch and its ramp: one row, 4096 channels, K 14336 (59 MB) 10.0 us, 5.9
+// TB/s; eight rows gated, 2048, 7168 (29 MB) 7.5; eight rows, 28672, 4096 past the caches (117 MB) 21.4, 5.5 TB/s.  Two
+// tiles a wavefront halve the reads of x, eight wavefronts and two steps keep 32 KB of a tile in flight.  Two to eight
+// groups of 16 rows a wavefront, which read the weights once for all, were slower than the tiles below.
 template <bool GATED, int NT, int KS, int P, int POLICY>
 __global__ __launch_bounds__(64 * KS) void few_int8_kernel(Int8Product p) {
   __shared__ i32x4 part[KS][NT][64];
@@ -132,7 +138,13 @@ void few(const Int8Product& p, bool stream, hipStream_t s) {
 // Tiles of 16 A rows of x by 64 B weight rows (GATED: 32 B of either matrix), 16 B for each of four wavefronts: no
 // two read the same weights, which go from memory straight to registers, in the packed pieces that are the
 // products' operands as they lie.  x, which all four read, passes through LDS, in a ring of XS stages of 128 columns
-// as above.  A step is 64 columns; a ring of 2 XS steps of weights is in flight.
+// of the large tiles.  A step is 64 columns; a ring of 2 XS steps of weights is in flight.
+//
+// Bound by what passes into a compute unit, 64 bytes a clock: 333 rows, 6145 channels, K 4096 15.4 us on 96 x 128 (196
+// tiles; 28 KB a stage are 0.20 us of its 0.26; matrix cores 41% busy; 17.5 with the weights through LDS too); gated
+// 700, 1408, 2816 9.5 us on 64 x 128.  At 160 x 256 the matrix cores share it: 2003, 4608, 7168 61 us, 2.17 P
+// operations/s, 57% busy (70 on 192 x 256 through LDS).  Longer rings and unrolled loops lost at short K to the fetch of
+// instructions; k starts of each tile's own, so that rows of x a power of two apart do not meet, gained nothing.
 template <int A, int B, int XS>
 struct Direct {
   static constexpr int kRows = 16 * A, kWRows = 64 * B;
@@ -297,7 +309,8 @@ __global__ __launch_bounds__(256, A * B <= 16 ? 2 : 1) void int8_direct_kernel(I
     if (t0 + 16 * a < p.T) put_strip<GATED, B>(p, acc[a], t0 + 16 * a, nb, sx[a], s0, s1, s_out[wave], lane);
 }
 
-// Adds the parts of tiles that were cut along k: one workgroup for 16 rows of a tile.
+// Adds the parts of tiles that were cut along k: one workgroup for 16 rows of a tile.  64 rows, 4096 channels, K 14336
+// in four parts: 4.8 us after the products' 13.3 (9 MB, mostly from the L2), the latency of one load and one store.
 template <bool GATED, int A, int B>
 __global__ __launch_bounds__(256) void int8_join_kernel(Int8Product p, int mtiles, int ntiles, int parts) {
   constexpr int kFrags = GATED ? B / 2 : B, kPitch = 32 * kFrags + 16;

@@ -7,9 +7,18 @@ namespace {
 // Tiles of 64 MI rows of x by 64 NI weight rows (GATED: 32 NI of either matrix) for four wavefronts, 2 x 2, of
 // 32 MI x 32 NI each.  A stage holds 128 columns of both operands in LDS, the weights in their packed pieces,
 // x in rows of 128 bytes whose 16-byte chunks are permuted so that 16 rows of one column lie in different banks;
-// global -> LDS loads fill rings of three stages of x and two of weights, all of the LDS at MI = 4.  A stage is four groups of 32 columns; a group's operands are
-// read from LDS while the one before it is multiplied, also across the border of two stages: the barrier that
-// hands over a stage stands before the last group, whose operands are in registers by then.
+// global -> LDS loads fill rings of three stages of x and two of weights, all of the LDS at MI = 4.  A stage is four
+// groups of 32 columns; a group's operands are read from LDS while the one before it is multiplied, also across the
+// border of two stages: the barrier that hands over a stage stands before the last group, whose operands are in
+// registers by then.
+//
+// Bound by the matrix cores, at the clock that the board's power leaves: 16384 rows, 4096 channels, K 14336 712 to 740
+// us (2.60 to 2.70 P operations/s; a large library product of this size 2.49), matrix cores 83% busy at 1.62 GHz; gated
+// 8192, 14336, 4096 766 to 790 us (2.44 to 2.51 P), 71% at 1.70 GHz: a tile takes 1.55 us a stage and some 4 us at its
+// ends.  The largest tile that registers hold moves the fewest bytes through LDS; 192 rows (813 us) fill the last
+// round better where that counts.  Measured against (16384, 4096, 14336): two stages of x 760 us; a stage's loads in
+// one of its groups, 832; workgroups that stay and load their next tile's first stages while this one's results
+// leave, 750 (gated 830, for 785 then): they need registers that the sums take, and spill.
 __device__ __forceinline__ i32x16 mfma32_i8(u32x4 a, u32x4 b, i32x16 c) {
   return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
 }
@@ -96,14 +105,15 @@ __global__ __launch_bounds__(256, 1) void int8_large_kernel(Int8Product p, int m
     const bool on = kt * 128 + 16 * chunk < K;                // columns past K: zeros
 #pragma unroll
     for (int i = 0; i < MI; ++i)
-      load_lds<kCached>(bx, kt < KT, stage + (wave + 4 * (which * MI + i)) * 1024, on ? int(xat[which * MI + i]) : kPast, kt * 128);
+      load_lds<kCached>(bx, kt < KT, stage + (wave + 4 * (which * MI + i)) * 1024,
+                        on ? int(xat[which * MI + i]) : kPast, kt * 128);
   };
   auto issue_w = [&](uint8_t* stage, int kt, int which) {
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
       const int i = which * NI + j, tile16 = wave + 4 * (i >> 1);
-      load_lds<kCached>(GATED && tile16 >= 2 * NI ? bw1 : bw0, kt < KT, stage + tile16 * 2048 + (i & 1) * 1024, int(wat[i >> 1]),
-               kt * 2048 + (i & 1) * 1024);
+      load_lds<kCached>(GATED && tile16 >= 2 * NI ? bw1 : bw0, kt < KT, stage + tile16 * 2048 + (i & 1) * 1024,
+                        int(wat[i >> 1]), kt * 2048 + (i & 1) * 1024);
     }
   };
 

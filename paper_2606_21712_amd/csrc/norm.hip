@@ -74,8 +74,8 @@ __device__ __forceinline__ void block_sum(float& sum, uint32_t& top, float (*slo
 // the channels stay in registers (read again for each row, from the L2, they cost a third: 9001 x 7168 133 us
 // against 102).  Rows of more than 16384 leave no registers for either.
 //
-// Bound by memory: 9001 x 7168 with a post norm (516 MB) 97 us, 5.3 TB/s (without the row ahead 102), with codes
-// 85; 2003 x 7168 24.6 (30.9); one row of 4096 3.2 us, the latency of a load, two sums and a store.
+// Bound by memory: 9001 x 7168 with a post norm (516 MB) 98 us, 5.3 TB/s (without the row ahead 102), with codes
+// 85; 2003 x 7168 24.6 (30.9); one row of 4096 3.3 us, the latency of a load, two sums and a store.
 template <int NT, int V, bool F32, bool CODES>
 __global__ __launch_bounds__(NT) void norm_join_kernel(NormJoin a) {
   constexpr int kElt = F32 ? 4 : 2;
@@ -210,6 +210,8 @@ __global__ __launch_bounds__(NT) void norm_join_kernel(NormJoin a) {
 }
 
 // ------------------------------------------------------------------ rows to codes
+// A row stays in registers between its largest magnitude and its codes: read once, written once.  Bound by memory:
+// 8192 x 14336 (352 MB) 65.5 us, 5.4 TB/s; nine rows of 7168 3.3 us, the latency of a load, a maximum and a store.
 template <int NT, int V>
 __global__ __launch_bounds__(NT) void quantize_int8_kernel(const uint16_t* __restrict__ src, int64_t stride,
                                                            int64_t rows, int K, int8_t* __restrict__ codes,
