@@ -290,6 +290,65 @@ def test_products_past_32_bits(T, N, K):
     assert torch.equal(bits(y[at.cuda()].cpu()), bits(matmul_plain(x[at.cuda()].cpu(), sx[at.cuda()].cpu(), w, sw)))
 
 
+@pytest.mark.parametrize("T", [2, 130])
+def test_products_with_the_most_channels(T):
+    """2^24 channels, whose packed weights pass 2^31 bytes, as does y at 130 rows: the first and last channels, and some."""
+    N, K = 1 << 24, 16
+    log(f"[gpu] matmul int8 T={T} {N}x{K}")
+    x, sx = random_int8(T, K, 3)
+    w = torch.randint(-128, 128, (N, K), dtype=torch.int8, device="cuda")
+    sw = torch.rand(N, device="cuda") + 0.5
+    y = moe.moe_matmul_int8(x.cuda(), sx.cuda(), moe.moe_pack_int8(w, sw))
+    at = torch.cat([torch.arange(200), torch.randint(0, N, (2000,), generator=gen(4)), torch.arange(N - 200, N)]).cuda()
+    assert torch.equal(bits(y[:, at].cpu()), bits(matmul_plain(x, sx, w[at].cpu(), sw[at].cpu())))
+
+
+def test_products_in_parts_in_a_graph():
+    """Products cut along k, plain and gated, captured together and on their own, replayed with other inputs between
+    eager calls: the eager bits every time."""
+    log("[gpu] int8 products in parts in graphs")
+    T, N, K = 150, 520, 8208
+    w, v = (moe.moe_pack_int8(*(t.cuda() for t in random_int8(N, K, i))) for i in (20, 21))
+    assert moe.moe_matmul_int8_workspace_bytes(T, N, K) and moe.moe_gated_int8_workspace_bytes(T, N, K)
+    calls = [lambda x, s: (moe.moe_matmul_int8(x, s, w), moe.moe_gated_int8(x, s, w, v), moe.moe_matmul_int8(x, s, v)),
+             lambda x, s: (moe.moe_gated_int8(x, s, v, w),)]
+    graphs = []
+    for call in calls:
+        x, s = (t.cuda() for t in random_int8(T, K, 1))
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            call(x, s)
+        torch.cuda.current_stream().wait_stream(side)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = call(x, s)
+        graphs.append((graph, call, x, s, out))
+    for i, (graph, call, x, s, out) in itertools.product(range(4), graphs):
+        for dst, src in zip((x, s), random_int8(T, K, 100 + i)):
+            dst.copy_(src)
+        graph.replay()
+        want = call(x, s)
+        torch.cuda.synchronize()
+        assert all(torch.equal(bits(a), bits(b)) for a, b in zip(out, want)), i
+
+
+def test_any_budget(budget):
+    """A budget of more compute units than there are changes no bit of a product or of codes."""
+    log("[gpu] int8: a large budget")
+    x, sx = (t.cuda() for t in random_int8(300, 4112, 1))
+    w = moe.moe_pack_int8(*(t.cuda() for t in random_int8(520, 4112, 2)))
+    v = torch.randn(300, 4112, generator=gen(3)).to(BF).cuda()
+    run = lambda: (moe.moe_matmul_int8(x, sx, w), moe.moe_gated_int8(x, sx, w, w), moe.moe_matmul_int8(x[:7], sx[:7], w),
+                   *moe.moe_quantize_int8(v))
+    want = run()
+    for cus in (1 << 12, 1 << 22):
+        budget(cus)
+        assert all(torch.equal(bits(a), bits(b)) for a, b in zip(run(), want))
+        args = (v.cpu(), v.cpu(), None, None, False, 1.0, True, 0.0, 1e-6, True)
+        check_join(join(*args), *args)
+
+
 # --------------------------------------------------------------------------- the norms
 def norm64(v, w, offset, eps):
     n = v / (v.square().mean(1, keepdim=True) + eps).sqrt()

@@ -82,3 +82,19 @@ LINES = [
 @pytest.mark.parametrize("case,form", LINES)
 def test_lines(plan, case, form):
     assert plan([(*case, 256)])[0][0] == form
+
+
+def test_launches_fit_whatever_the_budget(plan):
+    """A budget may say more compute units than any device has: launches stay under 2^32 threads, the joins' (16 rows
+    of a tile a workgroup of 256) among them."""
+    r = random.Random(6)
+    cases = []
+    for _ in range(5000):
+        T, N, K = (int(m ** r.random()) for m in (MOST_T, MOST_N, MOST_K // 16))
+        if T * N <= MOST_OUT:
+            cases.append((T, N, 16 * K, r.randint(0, 1), r.choice((1 << 12, 1 << 20, (1 << 31) - 1))))
+    cases += [(MOST_T, 4096, MOST_K, g, (1 << 31) - 1) for g in (0, 1)] + [(2048, MOST_N, MOST_K, 0, (1 << 31) - 1)]
+    for c, (form, parts, tiles, part_bytes, stream) in zip(cases, plan(cases)):
+        assert tiles * parts * 256 < 1 << 32, c
+        if parts > 1:
+            assert tiles * (int(form.split("x")[0]) // 16) * 256 < 1 << 32 and parts * part_bytes < 1 << 63, c
