@@ -42,24 +42,27 @@ __device__ __forceinline__ void store4(uint16_t* row, int n, int N, const float 
 }
 
 // ------------------------------------------------------------------ few rows of x
-// A wavefront multiplies NT tiles of 16 weight rows (GATED: one of either matrix) with 16 rows of x: the weights are
-// the first operand, streamed from memory into registers, x the second, from the caches.  KS wavefronts deal the
-// steps of 128 columns along k among themselves (both halves of a line of x to one of them) and add their sums in
+// A wavefront multiplies NT tiles of 16 weight rows (GATED: one of either matrix) with C groups of 16 rows of x: the
+// weights are the first operand, streamed from memory into registers, x the second, from the caches.  KS wavefronts deal
+// the steps of 128 columns along k among themselves (both halves of a line of x to one of them) and add their sums in
 // LDS; P steps are in flight.  More rows are other workgroups', which find the weights in the L2.
 //
 // Bound by the reads of the weights, after a launch and its ramp: one row, 4096 channels, K 14336 (59 MB) 10.0 us, 5.9
 // TB/s; eight rows gated, 2048, 7168 (29 MB) 7.5; eight rows, 28672, 4096 past the caches (117 MB) 21.4, 5.5 TB/s.  Two
-// tiles a wavefront halve the reads of x, eight wavefronts and two steps keep 32 KB of a tile in flight.  Two to eight
-// groups of 16 rows a wavefront, which read the weights once for all, were slower than the tiles below.
-template <bool GATED, int NT, int KS, int P, int POLICY>
+// tiles a wavefront halve the reads of x, eight wavefronts and two steps keep 32 KB of a tile in flight (four steps: 16
+// rows, 4096, 14336 14.4 us for 13.6).  Two groups read the weights once for both: 32 rows, 6144, 4096 8.0 us, 10.1 in
+// two workgroups; four were faster nowhere (64 rows 11.9 us, 10.0 on the tiles below).
+template <bool GATED, int NT, int C, int KS, int P, int POLICY>
 __global__ __launch_bounds__(64 * KS) void few_int8_kernel(Int8Product p) {
-  __shared__ i32x4 part[KS][NT][64];
+  __shared__ i32x4 part[KS][NT][C][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int t0 = int(blockIdx.y) * 16;
+  const int t0 = int(blockIdx.y) * 16 * C;
   constexpr int kTiles = GATED ? NT / 2 : NT;     // of a matrix
+  static_assert(kTiles * C <= KS, "a wavefront finishes a tile");
   const int pairs = p.steps / 2;
   const int mine = (pairs - wave + KS - 1) / KS;
   const int tiles = (p.N + 15) / 16, rt = int(blockIdx.x) * kTiles;
+  if (rt >= tiles) return;
   const int64_t tile_bytes = int64_t(p.steps) * 1024;
   Buffer bw[NT];
 #pragma unroll
@@ -67,22 +70,27 @@ __global__ __launch_bounds__(64 * KS) void few_int8_kernel(Int8Product p) {
     const int tile = rt + r % kTiles;
     bw[r] = buffer_of((GATED && r >= kTiles ? p.w1 : p.w0) + tile * tile_bytes, tile < tiles ? tile_bytes : 0);
   }
-  const auto bx = buffer_of(p.x + int64_t(t0) * p.K, int64_t(min(p.T - t0, 16)) * p.K);
+  const auto bx = buffer_of(p.x + int64_t(t0) * p.K, int64_t(min(p.T - t0, 16 * C)) * p.K);
   const int chunk = 16 * (lane >> 4);
-  const int xat = (lane & 15) * p.K + chunk;      // past the last row: zeros
+  int xat[C];                                     // past the last row: zeros
+#pragma unroll
+  for (int c = 0; c < C; ++c) xat[c] = (16 * c + (lane & 15)) * p.K + chunk;
   // what the wavefronts that finish a tile need besides: loaded first, not once the sums are there
-  const int t = t0 + (lane & 15), n = (rt + wave) * 16 + 4 * (lane >> 4);
-  const bool finish = wave < kTiles && t < p.T && n < p.N;
+  const int fr = wave % kTiles, fc = wave / kTiles;
+  const int t = t0 + 16 * fc + (lane & 15), n = (rt + fr) * 16 + 4 * (lane >> 4);
+  const bool finish = wave < kTiles * C && t < p.T && n < p.N;
   float sx = 0.f, s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
   if (finish) {
     sx = p.x_scales[t];
 #pragma unroll
     for (int i = 0; i < 4; ++i) channel_scales<GATED>(p, n + i, s0[i], s1[i]);
   }
-  i32x4 acc[NT];
+  i32x4 acc[NT][C];
 #pragma unroll
-  for (int r = 0; r < NT; ++r) acc[r] = i32x4{0, 0, 0, 0};
-  u32x4 w[P][NT][2], x[P][2];
+  for (int r = 0; r < NT; ++r)
+#pragma unroll
+    for (int c = 0; c < C; ++c) acc[r][c] = i32x4{0, 0, 0, 0};
+  u32x4 w[P][NT][2], x[P][C][2];
   auto load = [&](int q, int i) {
     const int at = wave + i * KS;
 #pragma unroll
@@ -90,8 +98,10 @@ __global__ __launch_bounds__(64 * KS) void few_int8_kernel(Int8Product p) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) w[q][r][h] = load16<POLICY>(bw[r], i < mine, 16 * lane, at * 2048 + h * 1024);
 #pragma unroll
-    for (int h = 0; h < 2; ++h)                   // columns past K: zeros, whatever the offset's range check counts
-      x[q][h] = load16<kCached>(bx, i < mine, at * 128 + h * 64 + chunk < p.K ? xat : kPast, at * 128 + h * 64);
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)                 // columns past K: zeros, whatever the offset's range check counts
+        x[q][c][h] = load16<kCached>(bx, i < mine, at * 128 + h * 64 + chunk < p.K ? xat[c] : kPast, at * 128 + h * 64);
   };
 #pragma unroll
   for (int q = 0; q < P; ++q) load(q, q);
@@ -101,21 +111,25 @@ __global__ __launch_bounds__(64 * KS) void few_int8_kernel(Int8Product p) {
 #pragma unroll
       for (int r = 0; r < NT; ++r)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) acc[r] = mfma_i8(w[q][r][h], x[q][h], acc[r]);
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) acc[r][c] = mfma_i8(w[q][r][h], x[q][c][h], acc[r][c]);
       load(q, i + q + P);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
 #pragma unroll
-  for (int r = 0; r < NT; ++r) part[wave][r][lane] = acc[r];
+  for (int r = 0; r < NT; ++r)
+#pragma unroll
+    for (int c = 0; c < C; ++c) part[wave][r][c][lane] = acc[r][c];
   __syncthreads();
   if (!finish) return;
-  i32x4 s = part[0][wave][lane], u = {0, 0, 0, 0};
+  i32x4 s = part[0][fr][fc][lane], u = {0, 0, 0, 0};
 #pragma unroll
-  for (int i = 1; i < KS; ++i) s += part[i][wave][lane];
+  for (int i = 1; i < KS; ++i) s += part[i][fr][fc][lane];
   if (GATED) {
 #pragma unroll
-    for (int i = 0; i < KS; ++i) u += part[i][kTiles + wave][lane];
+    for (int i = 0; i < KS; ++i) u += part[i][kTiles + fr][fc][lane];
   }
   float v[4];
 #pragma unroll
@@ -123,15 +137,16 @@ __global__ __launch_bounds__(64 * KS) void few_int8_kernel(Int8Product p) {
   store4(p.y + int64_t(t) * p.N, n, p.N, v);
 }
 
-template <bool GATED, int NT>
+template <bool GATED, int NT, int C = 1>
 void few(const Int8Product& p, bool stream, hipStream_t s) {
   const int tiles = (p.N + 15) / 16, each = GATED ? NT / 2 : NT;
   const char* name = GATED ? "gated_int8_few" : "matmul_int8_few";
-  const dim3 grid((tiles + each - 1) / each, (p.T + 15) / 16), block(512);
+  // all groups of rows of a tile of weights on one XCD, whose L2 has it: number n of a launch runs on XCD n % 8
+  const dim3 grid(((tiles + each - 1) / each + 7) / 8 * 8, (p.T + 16 * C - 1) / (16 * C)), block(512);
   if (stream)
-    MOE_LAUNCH(name, (few_int8_kernel<GATED, NT, 8, 2, kStream>), grid, block, s, p);
+    MOE_LAUNCH(name, (few_int8_kernel<GATED, NT, C, 8, 2, kStream>), grid, block, s, p);
   else
-    MOE_LAUNCH(name, (few_int8_kernel<GATED, NT, 8, 2, kCached>), grid, block, s, p);
+    MOE_LAUNCH(name, (few_int8_kernel<GATED, NT, C, 8, 2, kCached>), grid, block, s, p);
 }
 
 // ------------------------------------------------------------------ more rows: weights past LDS
@@ -366,6 +381,7 @@ void product(const Int8Product& p, const Int8Plan& plan, hipStream_t s) {
       if constexpr (!GATED) return few<GATED, 1>(p, plan.stream, s);
       [[fallthrough]];
     case Int8Form::kFew2: return few<GATED, 2>(p, plan.stream, s);
+    case Int8Form::kFew2x32: return few<GATED, 2, 2>(p, plan.stream, s);
     case Int8Form::k32x128: return tiles<GATED, 2, 4>(p, plan, s);
     case Int8Form::k64x128: return tiles<GATED, 4, 3>(p, plan, s);
     case Int8Form::k96x128: return tiles<GATED, 6, 3>(p, plan, s);

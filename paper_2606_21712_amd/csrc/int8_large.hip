@@ -12,9 +12,9 @@ namespace {
 // border of two stages: the barrier that hands over a stage stands before the last group, whose operands are in
 // registers by then.
 //
-// Bound by the matrix cores, at the clock that the board's power leaves: 16384 rows, 4096 channels, K 14336 712 to 740
-// us (2.60 to 2.70 P operations/s; a large library product of this size 2.49), matrix cores 83% busy at 1.62 GHz; gated
-// 8192, 14336, 4096 766 to 790 us (2.44 to 2.51 P), 71% at 1.70 GHz: a tile takes 1.55 us a stage and some 4 us at its
+// Bound by the matrix cores, at the clock that the board's power leaves: 16384 rows, 4096 channels, K 14336 712 to 743
+// us (2.59 to 2.70 P operations/s; a large library product of this size 2.49), matrix cores 83% busy at 1.62 GHz; gated
+// 8192, 14336, 4096 766 to 813 us (2.37 to 2.51 P), 71% at 1.70 GHz: a tile takes 1.55 us a stage and some 4 us at its
 // ends.  The largest tile that registers hold moves the fewest bytes through LDS; 192 rows (813 us) fill the last
 // round better where that counts.  Measured against (16384, 4096, 14336): two stages of x 760 us; a stage's loads in
 // one of its groups, 832; workgroups that stay and load their next tile's first stages while this one's results

@@ -194,9 +194,9 @@ inline int row_groups(const RowShape& f) { return f.threads == 64 ? 32 : 1024 / 
 
 // ---- products of 8-bit codes (int8_gemm.hip)
 
-// The kernels: 16 rows of x with one or two tiles of 16 weight rows a wavefront, or tiles of rows of x by weight
-// rows (gated: half of either matrix), the last two through LDS.
-enum class Int8Form { kFew1, kFew2, k32x128, k64x128, k96x128, k128x128, k160x256, k192x256, k256x256 };
+// The kernels: 16 rows of x with one or two tiles of 16 weight rows a wavefront, 32 with two, or tiles of rows of x by
+// weight rows (gated: half of either matrix), the last two through LDS.
+enum class Int8Form { kFew1, kFew2, kFew2x32, k32x128, k64x128, k96x128, k128x128, k160x256, k192x256, k256x256 };
 
 struct Int8Plan {
   Int8Form form;
@@ -206,51 +206,55 @@ struct Int8Plan {
   bool stream;            // weights bypass the caches (the nt policy)
 };
 
-// Which kernel: the one that a model of their times, fitted to 11000 measurements of 1100 sizes (1 to 16384 rows, 100
-// to 30000 channels, K 256 to 16384, plain and gated), thinks the fastest.  Over these sizes its choice takes 1.8% more
-// than the fastest of all measured ones on average, at most 36%.  us; a stage is 128 columns.
+// Which kernel: the one that a model of their times, fitted to 21000 measurements of 1950 sizes (1 to 16384 rows, 200 to
+// 30000 channels, K 256 to 16384, plain and gated, replayed in graphs), thinks the fastest.  On 400 sizes apart from
+// these, of up to 128 rows, its choice takes 0.9% more than the fastest of all kernels on average, at most 22%.  us; a
+// stage is 128 columns.
 //   Tiles: rounds of as many workgroups as run at once.  A stage takes what its operands take to pass
-//   through a compute unit, once for each workgroup there, and a tile a rest; all operands and results move
+//   through a compute unit, once for each workgroup there, and so does a tile's end; all operands and results move
 //   once besides, and the weights a quarter more for each further tile of rows.
 //   Parts: another launch, and the sums written and read.
-//   Few rows: the latency of a wavefront's steps, or what passes through a compute unit, or the weights
-//   from memory, four fifths of that again for each further 16 rows.
+//   Few rows: a wavefront's steps, what passes into a compute unit, and the weights from memory, a fifth of that
+//   again for each further group of rows at the same time, half for a later one.
 // (333 rows, 6145 channels, K 4096: 16.2 on 96 x 128, 18.8 on 128 x 128, 20.5 on 64 x 128, 70 on 192 x 256; 2003, 4608,
-// 7168: 64 on 160 x 256, 70 on 192 x 256, 76 on 256 x 256, 83 on 128 x 128; 64, 4096, 14336: 20.9 on 32 x 128 in four
-// parts, 22.6 in eight, 44 whole; 16384, 4096, 14336: 738 on 256 x 256, 813 on 192 x 256, 828 on 160 x 256.)
+// 7168: 64 on 160 x 256, 70 on 192 x 256, 76 on 256 x 256, 83 on 128 x 128; 64, 4096, 14336: 18.2 on 64 x 128 in eight
+// parts, 26.7 with few rows, 44 on 32 x 128 whole; 16384, 4096, 14336: 738 on 256 x 256, 813 on 192 x 256, 828 on 160 x
+// 256; 32, 7168, 2048: 5.9 with 32 rows, 7.1 with 16; 16, 4096, 14336: 13.6 with one tile on 256 workgroups, 17.1 with two.)
 inline Int8Plan int8_plan(int64_t T, int64_t N, int64_t K, bool gated, int num_cu) {
   struct Tile {
     Int8Form form;
     int rows, wrows, together;     // workgroups that a compute unit holds
-    double alone, each, rest;      // a stage of one workgroup, of several for each of them; the rest of a tile
+    double alone, each, end, start;   // a stage of one workgroup, of several for each of them; a tile's end for each, its start
     int most_parts;
   };
   static constexpr Tile kTiles[] = {
-      {Int8Form::k32x128, 32, 128, 4, 0.096, 0.102, 2.0, 8},  {Int8Form::k64x128, 64, 128, 3, 0.183, 0.186, 1.8, 8},
-      {Int8Form::k96x128, 96, 128, 3, 0.204, 0.270, 1.8, 4},  {Int8Form::k128x128, 128, 128, 2, 0.299, 0.336, 2.1, 4},
-      {Int8Form::k160x256, 160, 256, 1, 0.65, 0.74, 5.5, 1}, {Int8Form::k192x256, 192, 256, 1, 0.80, 0.81, 6.8, 1},
-      {Int8Form::k256x256, 256, 256, 1, 1.06, 0.96, 9.1, 1},
+      {Int8Form::k32x128, 32, 128, 4, 0.108, 0.160, 0.40, 0.91, 8},  {Int8Form::k64x128, 64, 128, 3, 0.160, 0.203, 0.63, 1.12, 8},
+      {Int8Form::k96x128, 96, 128, 3, 0.200, 0.266, 0.84, 1.38, 4},  {Int8Form::k128x128, 128, 128, 2, 0.300, 0.330, 1.32, 1.51, 4},
+      {Int8Form::k160x256, 160, 256, 1, 0.650, 0.765, 5.61, 0, 1}, {Int8Form::k192x256, 192, 256, 1, 0.800, 0.822, 7.78, 0, 1},
+      {Int8Form::k256x256, 256, 256, 1, 1.086, 0.960, 10.07, 0, 1},
   };
+  const auto beside = [](double a, double b, double both) { return std::fmax(a, b) + both * std::fmin(a, b); };
   const int64_t most = int64_t(1) << 23;     // workgroups of a launch
   const double mats = gated ? 2 : 1, weights = mats * double(N) * double(K);
-  const double others = double(T) * double(K) + 2.0 * double(T) * double(N);
+  const double results = 2.0 * double(T) * double(N);
   const double stages = double(ceil_div(K, 128));
   Int8Plan best{Int8Form::k256x256, 1, 0, 0, false};
   double best_us = 1e300;
   int64_t rows = 0;
   for (const Tile& t : kTiles) {
     const int64_t mtiles = ceil_div(T, t.rows), tiles = mtiles * ceil_div(N, gated ? t.wrows / 2 : t.wrows);
-    const double moved = (weights * (1 + 0.28 * double(mtiles - 1)) + others) / 10.0e6;
+    const double moved = (weights * (1 + 0.26 * double(mtiles - 1)) + double(T) * double(K) + results) / 9.2e6;
     for (int parts = 1; parts <= t.most_parts; parts *= 2) {
       const int64_t blocks = tiles * parts, round = int64_t(num_cu) * t.together;
       if (blocks > most && t.form != Int8Form::k256x256) continue;
       if (parts > 1 && (parts > stages || blocks > 4 * round || blocks > 1 << 20)) continue;
-      const auto some = [&](int64_t n) {     // workgroups, up to a round of them
-        return stages / parts * std::fmax(t.alone, double(ceil_div(n, num_cu)) * t.each) + t.rest;
+      const auto some = [&](int n) {         // of n workgroups on a compute unit
+        return stages / parts * std::fmax(t.alone, n * t.each) + n * t.end;
       };
-      double us = 2.8 + moved + double(blocks / round) * some(round);
-      if (blocks % round) us += some(blocks % round);
-      if (parts > 1) us += 2.7 + 1.17e-6 * mats * double(T) * double(N) * parts;
+      double work = double(blocks / round) * some(t.together);
+      if (blocks % round) work += some(int(ceil_div(blocks % round, num_cu))) + t.start;
+      if (parts > 1) work += 3.1 + 1.06e-6 * mats * double(T) * double(N) * parts;
+      const double us = 1.84 + beside(work, moved, 1.09);
       if (us < best_us) {
         best_us = us;
         best = {t.form, parts, tiles, size_t(tiles) * t.rows * t.wrows * 4, false};
@@ -258,21 +262,30 @@ inline Int8Plan int8_plan(int64_t T, int64_t N, int64_t K, bool gated, int num_c
       }
     }
   }
-  if (T <= 128) {
-    // two tiles of weights a wavefront, unless that left compute units without any (1, 4096, 14336: 12.1 us on 256
-    // workgroups, 14.0 on 128)
-    const double more = double(ceil_div(T, 16)), steps = std::ceil(stages / 8), units = double(ceil_div(N, 16)) * more;
-    const int nt = gated || units > num_cu ? 2 : 1;
-    const double blocks = gated ? units : std::ceil(units / nt);
-    const double alone = 0.116 * steps + 2.6, move = blocks / num_cu * steps * (0.364 * nt + 0.132);
-    const double memory = weights / 6.2e6 * (1 + 0.8 * (more - 1));
-    const double first = std::fmax(alone, std::fmax(move, memory));
-    const double second = std::fmax(std::fmin(alone, move), std::fmin(std::fmax(alone, move), memory));
-    if (2.95 + first + 0.115 * second < best_us) {
-      best = {nt == 1 ? Int8Form::kFew1 : Int8Form::kFew2, 1, 0, 0, false};
-      rows = 16;
+  struct Few {
+    Int8Form form;
+    int tiles, groups;             // of 16 weight rows, of 16 rows of x
+  };
+  static constexpr Few kFew[] = {{Int8Form::kFew1, 1, 1}, {Int8Form::kFew2, 2, 1}, {Int8Form::kFew2x32, 2, 2}};
+  if (T <= 128)
+    for (const Few& f : kFew) {
+      if (gated && f.tiles == 1) continue;
+      const int64_t more = ceil_div(T, 16 * f.groups), each = gated ? f.tiles / 2 : f.tiles;
+      const int64_t blocks = ceil_div(ceil_div(ceil_div(N, 16), each), 8) * 8 * more;
+      const double steps = double(ceil_div(int64_t(stages), 8)), units = double(blocks) / num_cu;
+      const bool together = units <= 4;        // a later group's weights are in the L2
+      const double load = together ? std::ceil(units) : units;               // workgroups of a compute unit
+      const double alone = steps * 0.015 * f.groups + 0.65 + 0.31 * (f.groups - 1);
+      const double moved = load * (steps * (0.165 * f.tiles + 0.202 / 16 * double(T) / double(more) + 0.014 * f.groups) + 0.184);
+      const double memory = (weights * (1 + (together ? 0.20 : 0.47) * double(more - 1)) + results) / 8.0e6;
+      // (of more than 32 rows by 32 the fit is short: 48, 7168, 2048 8.4 us, 6.7 on 32 x 128)
+      const double us = (1.43 + beside(beside(alone, moved, 1.345), memory, 0.926)) * (f.groups > 1 && more > 1 ? 1.05 : 1.0);
+      if (us < best_us) {
+        best_us = us;
+        best = {f.form, 1, 0, 0, false};
+        rows = 16 * f.groups;
+      }
     }
-  }
   // Weights that one workgroup reads and no other, and that are too many to be found in the Infinity Cache by the
   // next call: 8 rows, 28672 channels, K 4096 (117 MB) 24.0 us, 21.4 past the caches; 2 rows, 8441, 10928 (92 MB) 25.5,
   // 20.3.  59 MB that come back after two others 10.3, 12.5 past the caches.

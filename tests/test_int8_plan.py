@@ -10,7 +10,7 @@ from int8_forms import FORMS, STREAMED
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(os.path.dirname(HERE), "paper_2606_21712_amd", "csrc")
-NAMES = ["few1", "few2", "32x128", "64x128", "96x128", "128x128", "160x256", "192x256", "256x256"]
+NAMES = ["few1", "few2", "few2x32", "32x128", "64x128", "96x128", "128x128", "160x256", "192x256", "256x256"]
 MOST_T, MOST_N, MOST_K, MOST_OUT = 1 << 20, 1 << 24, 131056, 1 << 37
 
 pytestmark = pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
@@ -40,10 +40,10 @@ def test_sizes_reach_their_kernels(plan):
     for gated in (0, 1):
         seen = {f[:2] for f in FORMS if f[5] == gated}
         assert seen >= {(n, 1) for n in NAMES[gated:]}
-        assert seen >= {(n, p) for n in NAMES[2:6] for p in (2, 4)} and {("32x128", 8), ("64x128", 8)} <= seen
+        assert seen >= {(n, p) for n in NAMES[3:7] for p in (2, 4)} and {("32x128", 8), ("64x128", 8)} <= seen
     got = plan([f[2:] for f in STREAMED])
     assert [g[0] for g in got] == [f[0] for f in STREAMED] and all(g[4] for g in got)
-    assert {(f[0], f[5]) for f in STREAMED} >= {(n, g) for n in NAMES[1:6] for g in (0, 1)} | {("few1", 0)}
+    assert {(f[0], f[5]) for f in STREAMED} >= {(n, g) for n in NAMES[1:7] for g in (0, 1)} | {("few1", 0)}
 
 
 def test_launches_fit(plan):
