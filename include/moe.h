@@ -575,11 +575,11 @@ moe_status moe_kv8_attention(const void* q, int64_t T, int32_t q_heads, const mo
  *
  * Arithmetic is fp32, x' and z are rounded once; z is taken of x' before its rounding.  The codes of z
  * are those of x' (offset + w_pre), the norm's factor is in the scale alone.  Squares are summed in fp32:
- * rows of more than 2^60 in size overflow.  A NaN or infinity stays in its row.  The order of the sums depends on H, T
+ * rows whose squares sum to 2^128 or more overflow.  A NaN or infinity stays in its row.  The order of the sums depends on H, T
  * and the compute-unit budget (moe_set_cu_budget), on nothing else.
  * Errors: INVALID_ARGUMENT for H not a positive multiple of 8, T < 0, eps < 0, numbers that are not
  * finite, flags that are not 0 or 1, an unknown gate_kind, bad strides, arguments without the one they belong to,
- * null or misaligned pointers; UNSUPPORTED for H > 32768 or an unknown dtype.
+ * null or misaligned pointers; UNSUPPORTED for H > 32768, T > 2^31 or an unknown dtype.
  */
 typedef enum { MOE_GATE_NONE = 0, MOE_GATE_CHANNEL = 1, MOE_GATE_TOKEN = 2, MOE_GATE_FULL = 3 } moe_gate;
 moe_status moe_norm_join(const void* x, int64_t x_stride, moe_dtype dt, const void* y, int64_t y_stride, int32_t post,
@@ -594,7 +594,7 @@ moe_status moe_norm_join(const void* x, int64_t x_stride, moe_dtype dt, const vo
  *   codes   i8 [rows, K]  out;   scales  f32 [rows]  out
  *
  * Errors: INVALID_ARGUMENT for rows < 0, K not a positive multiple of 16, a bad stride, null or
- * misaligned pointers; UNSUPPORTED for K > 131056.
+ * misaligned pointers; UNSUPPORTED for K > 131056 or rows > 2^31.
  */
 moe_status moe_quantize_int8(const void* src, int64_t src_stride, int64_t rows, int32_t K, int8_t* codes, float* scales,
                              moe_stream stream);
