@@ -4,6 +4,8 @@
 //
 // The sums are exact in 32 bits (K <= kInt8MaxK), whatever their order, so how a product is cut up
 // does not show in its result.
+#include <type_traits>
+
 #include "int8_product.h"
 #include "launch_rules.h"
 
@@ -258,19 +260,23 @@ __global__ __launch_bounds__(256, A * B <= 16 ? 2 : 1) void int8_direct_kernel(I
 #pragma unroll
     for (int b = 0; b < B; ++b) acc[a][b] = i32x4{0, 0, 0, 0};
   u32x4 xf[2][A];
-  auto read = [&](const uint8_t* stage, int s, u32x4(&to)[A]) {
+  auto read = [&](const uint8_t* stage, int s, u32x4(&to)[A], int from = 0, int end = A) {
 #pragma unroll
-    for (int a = 0; a < A; ++a)
+    for (int a = from; a < end; ++a)
       to[a] = *reinterpret_cast<const u32x4*>(stage + xrow + a * 2048 + ((4 * s + quarter) ^ xswz) * 16);
   };
-  auto multiply = [&](const u32x4(&wf)[B], const u32x4(&x)[A]) {
+  auto multiply = [&](const u32x4(&wf)[B], const u32x4(&x)[A], int from = 0, int end = A) {
 #pragma unroll
-    for (int a = 0; a < A; ++a)
+    for (int a = from; a < end; ++a)
 #pragma unroll
       for (int b = 0; b < B; ++b) acc[a][b] = mfma_i8(wf[b], x[a], acc[a][b]);
   };
-  constexpr int kAhead = (2 * XS - 2) * B + (XS - 2) * Tile::kXLoads;        // loads issued after the next stage's x
-  constexpr int kFirst = (2 * XS - 1) * B + (XS - 1) * Tile::kXLoads;
+  // The waits leave as many loads in flight as were sent after the next stage's x, so scheduling barriers part x from the
+  // weights around it.
+  constexpr int kGroup = 2 * B + Tile::kXLoads;               // loads of a step
+  constexpr int kAhead = (XS - 2) * kGroup + 2 * B;
+  constexpr int kFirst = (XS - 1) * kGroup + B;
+  constexpr int kSplit = (A * Tile::kXLoads + B) / (B + Tile::kXLoads);      // rows of 16 that are multiplied while x is sent for
   // stage kt, whose steps are the slots 2 j and 2 j + 1
   auto step = [&](uint8_t* xcur, uint8_t* xnxt, u32x4(&wprev)[B], u32x4(&w0)[B], u32x4(&w1)[B], int kt) {
     read(xcur, 1, xf[1]);
@@ -281,17 +287,40 @@ __global__ __launch_bounds__(256, A * B <= 16 ? 2 : 1) void int8_direct_kernel(I
     __builtin_amdgcn_s_waitcnt(wait_all_but(kAhead));
     bare_barrier();
     __builtin_amdgcn_sched_barrier(0);
-    read(xnxt, 0, xf[0]);
+    read(xnxt, 0, xf[0], 0, kSplit);
     issue_x(xcur, kt + XS);
+    multiply(w1, xf[1], 0, kSplit);
+    Mix<kSplit * B, kSplit, Tile::kXLoads>::order();
+    __builtin_amdgcn_sched_barrier(0);
+    read(xnxt, 0, xf[0], kSplit, A);
     issue_w(w0, 2 * kt + kSlots);
+    multiply(w1, xf[1], kSplit, A);
+    Mix<(A - kSplit) * B, A - kSplit, B>::order();
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // The last steps, fewer than a ring: what they would load lies past the end.  They do not count on loads of weights
+  // that no step reads, which the compiler leaves out.
+  auto last_step = [&](auto which, uint8_t* xcur, uint8_t* xnxt, u32x4(&w0)[B], u32x4(&w1)[B]) {
+    constexpr int j = decltype(which)::value;
+    read(xcur, 1, xf[1]);
+    multiply(w0, xf[0]);
+    Mix<A * B, A, 0>::order();
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (j < XS - 2) {
+      __builtin_amdgcn_s_waitcnt(wait_all_but((XS - 2 - j) * kGroup));
+      bare_barrier();
+      __builtin_amdgcn_sched_barrier(0);
+      read(xnxt, 0, xf[0]);
+    }
     multiply(w1, xf[1]);
-    Mix<A * B, A, B + Tile::kXLoads>::order();
+    Mix<A * B, j < XS - 2 ? A : 0, 0>::order();
     __builtin_amdgcn_sched_barrier(0);
   };
   uint8_t* const xs[4] = {x0, x1, x2, x3};
 #pragma unroll
   for (int j = 0; j < XS; ++j) {
     issue_x(xs[j], first + j);
+    __builtin_amdgcn_sched_barrier(0);
     issue_w(w[2 * j], 2 * (first + j));
     if (j < XS - 1) issue_w(w[2 * j + 1], 2 * (first + j) + 1);
     __builtin_amdgcn_sched_barrier(0);
@@ -306,9 +335,11 @@ __global__ __launch_bounds__(256, A * B <= 16 ? 2 : 1) void int8_direct_kernel(I
     for (int j = 0; j < XS; ++j)
       step(xs[j], xs[(j + 1) % XS], w[(2 * j + kSlots - 1) % kSlots], w[2 * j], w[2 * j + 1], kt + j);
   }
-#pragma unroll
-  for (int j = 0; j < XS - 1; ++j)
-    if (kt + j < KT) step(xs[j], xs[(j + 1) % XS], w[(2 * j + kSlots - 1) % kSlots], w[2 * j], w[2 * j + 1], kt + j);
+  static_assert(XS == 3 || XS == 4, "last steps");
+  if (kt < KT) last_step(std::integral_constant<int, 0>{}, x0, x1, w[0], w[1]);
+  if (kt + 1 < KT) last_step(std::integral_constant<int, 1>{}, x1, x2, w[2], w[3]);
+  if constexpr (XS > 3)
+    if (kt + 2 < KT) last_step(std::integral_constant<int, 2>{}, x2, x3, w[4], w[5]);
 
   __builtin_amdgcn_s_waitcnt(wait_all_but(0));                // for the zeros that are on their way to LDS
   if constexpr (SPLIT) {
