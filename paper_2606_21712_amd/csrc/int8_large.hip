@@ -188,6 +188,7 @@ __global__ __launch_bounds__(256, 1) void int8_large_kernel(Int8Product p, int m
   issue_x(x0, 0, 1);
   issue_w(w0, 0, 0);
   issue_w(w0, 0, 1);
+  __builtin_amdgcn_sched_barrier(0);                         // the wait counts on the second stage's being the youngest
   issue_x(x1, 1, 0);
   issue_x(x1, 1, 1);
   issue_w(w1, 1, 0);

@@ -131,3 +131,16 @@ def test_the_walk_finds_late_stages():
         assert late(first + [("wait", n), ("barrier",)] + step, 2) == bad
     assert late(first + [("wait", 4), ("barrier",), ("wait", 2), ("barrier",), ("wait", 0), ("barrier",)], 2) == [(1, 2)]
     assert late(first + [("wait", 4), ("barrier",), ("wait", 1), ("barrier",), ("wait", 0), ("barrier",)], 2) == []
+
+
+def test_first_stages_of_the_large_tiles_are_pinned():
+    """The wait before the first reads counts the loads of the second stage as the youngest.  They go to other LDS
+    objects, so the scheduler may send them among the first stage's unless a barrier of its own stands between."""
+    with open(os.path.join(CSRC, "int8_large.hip")) as f:
+        text = re.sub(r"//[^\n]*", "", f.read())
+    first = [m for m in re.finditer(r"issue_([xw])\(\1(\d), (\d), (\d)\);", text)]
+    assert [(m.group(1), m.group(2), m.group(4)) for m in first] == [
+        ("x", "0", "0"), ("x", "0", "1"), ("w", "0", "0"), ("w", "0", "1"), ("x", "1", "0"), ("x", "1", "1"), ("w", "1", "0")]
+    for a, b in zip(first, first[1:]):
+        if a.group(2) != b.group(2):
+            assert "__builtin_amdgcn_sched_barrier(0);" in text[a.end():b.start()]
