@@ -577,8 +577,8 @@ moe_status moe_kv8_attention(const void* q, int64_t T, int32_t q_heads, const mo
  * are those of x' (offset + w_pre), the norm's factor is in the scale alone.  Squares are summed in fp32:
  * rows whose squares sum to 2^128 or more overflow.  A NaN or infinity stays in its row.  The order of the sums depends on H, T
  * and the compute-unit budget (moe_set_cu_budget), on nothing else.
- * Errors: INVALID_ARGUMENT for H not a positive multiple of 8, T < 0, eps < 0, numbers that are not
- * finite, flags that are not 0 or 1, an unknown gate_kind, bad strides, arguments without the one they belong to,
+ * Errors: INVALID_ARGUMENT for H not a positive multiple of 8, T < 0, eps < 0, an
+ * eps, alpha or offset beyond 1e30 or NaN, flags that are not 0 or 1, an unknown gate_kind, bad strides, arguments without the one they belong to,
  * null or misaligned pointers; UNSUPPORTED for H > 32768, T > 2^31 or an unknown dtype.
  */
 typedef enum { MOE_GATE_NONE = 0, MOE_GATE_CHANNEL = 1, MOE_GATE_TOKEN = 2, MOE_GATE_FULL = 3 } moe_gate;

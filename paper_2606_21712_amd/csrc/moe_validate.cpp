@@ -712,9 +712,10 @@ Check validate_norm_join(const void* x, int64_t x_stride, int x_dt, const void* 
   MOE_TRY(flag(fn, "sigmoid", sigmoid));
   MOE_TRY(flag(fn, "z_codes", z_codes));
   if (gate_kind < 0 || gate_kind > 3) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "unknown gate_kind=%lld", gate_kind);
-  if (!(eps >= 0.f) || eps > 1e30f) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "eps must be finite, and not negative");
-  if (!(alpha >= -1e30f && alpha <= 1e30f)) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "alpha must be finite");
-  if (!(offset >= -1e30f && offset <= 1e30f)) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "offset must be finite");
+  // with larger ones products on the way overflow where the results do not
+  if (!(eps >= 0.f && eps <= 1e30f)) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "eps must be 0 to 1e30");
+  if (!(alpha >= -1e30f && alpha <= 1e30f)) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "alpha must be -1e30 to 1e30");
+  if (!(offset >= -1e30f && offset <= 1e30f)) return fail(MOE_ERR_INVALID_ARGUMENT, fn, "offset must be -1e30 to 1e30");
   if (T == 0) return Check{};
   const int per16 = x_dt == MOE_DTYPE_F32 ? 4 : 8;
   MOE_TRY(ptr(fn, "x", x));

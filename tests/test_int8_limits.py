@@ -1,0 +1,33 @@
+"""The stated limits of the dense half in 8-bit integers, on a host without a GPU.  No call here reaches a kernel."""
+import os
+import re
+
+import pytest
+
+import paper_2606_21712_amd as moe
+
+INVALID = 1
+P = 0x10000          # a 16-byte aligned address that is never dereferenced
+NAN, INF = float("nan"), float("inf")
+HEADER = re.sub(r"\s*\n \*\s*", " ", open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "moe.h")).read())
+
+
+def join(eps=1e-6, alpha=1.0, offset=0.0):
+    """The checks of a call without rows, which come before its rows are looked at."""
+    return moe.lib().moe_norm_join(P, 64, moe.DTYPE_BF16, P, 64, 1, P, P, 64, 3, 0, alpha, P, offset, eps, 0, 64, P, 64, 0, P, None,
+                                   None)
+
+
+@pytest.mark.parametrize("name", ["eps", "alpha", "offset"])
+def test_norm_join_says_which_numbers_it_takes(name):
+    """Up to 1e30 in size; the message and the header give the limit, not that a finite number is none."""
+    signs = (1,) if name == "eps" else (1, -1)
+    for sign in signs:
+        for value in (0.0, 1e-30, 1.0, 1e30):
+            assert join(**{name: sign * value}) == 0, value
+    for value in [sign * v for sign in signs for v in (1.1e30, 3e38, INF)] + [NAN] + ([-1e-30] if name == "eps" else []):
+        assert join(**{name: value}) == INVALID, value
+        message = moe.lib().moe_last_error().decode()
+        assert name in message and "1e30" in message and "finite" not in message
+    contract = HEADER.split("moe_norm_join - ")[1].split("moe_status moe_norm_join(")[0]
+    assert "eps, alpha or offset beyond 1e30 or NaN" in contract
