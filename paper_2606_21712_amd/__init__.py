@@ -682,6 +682,11 @@ def moe_kv8_attention(q, cache, block_table, seq_lens, cu_tokens, max_new, max_l
 
 
 # --------------------------------------------------------------------------- the dense half in 8-bit integers
+def _too_wide(name, n):
+    """Of a size n with n >> 31 not 0: an argument of 32 bits would be what ctypes leaves of it."""
+    raise MoEError(2, f"{name}={n} does not fit 32 bits")
+
+
 class Int8:
     """A packed matrix [N, K] of 8-bit weights (include/moe.h): codes int8 in the library's tiled layout, scales
     f32 [N].  The tensors are looked over here, once, and stay."""
@@ -689,6 +694,8 @@ class Int8:
     def __init__(self, codes, scales, shape):
         self.codes, self.scales = codes, scales
         self.shape = N, K = tuple(shape)
+        if (N | K) >> 31:
+            _too_wide("weights", self.shape)
         if codes.dtype != torch.int8 or scales.dtype != torch.float32:
             raise TypeError("packed codes are int8, scales float32")
         if codes.numel() < moe_int8_code_bytes(N, K) or scales.shape != (N,):
@@ -698,7 +705,7 @@ class Int8:
 
 
 def moe_int8_code_bytes(rows, K) -> int:
-    return lib().moe_int8_code_bytes(rows, K)
+    return 0 if K >> 31 else lib().moe_int8_code_bytes(rows, K)
 
 
 _I8, _F32, _BF16 = torch.int8, torch.float32, torch.bfloat16
@@ -780,6 +787,8 @@ def moe_norm_join(x, y=None, post=None, gate=None, sigmoid=False, alpha=1.0, pre
     x_out may be slices with rows in one piece."""
     shape, dt, index = x.shape, x.dtype, x.get_device()
     T, H = shape
+    if H >> 31:
+        _too_wide("H", H)
     if dt is not _BF16 and dt is not _F32:
         raise TypeError("x must be bf16 or f32")
     if index < 0:
@@ -822,6 +831,8 @@ def moe_quantize_int8(src, codes=None, scales=None, stream=None):
     """bf16 [T, K], rows in one piece -> (codes int8 [T, K], scales f32 [T])."""
     shape, index = src.shape, src.get_device()
     T, K = shape
+    if K >> 31:
+        _too_wide("K", K)
     row = _matrix(src, "src", shape, index)
     codes = _like(codes, "codes", torch.int8, shape, src.device, stream)
     scales = _like(scales, "scales", torch.float32, (T,), src.device, stream)
@@ -835,6 +846,8 @@ def moe_pack_int8(codes, scales, stream=None):
     if codes.dtype != torch.int8:
         raise TypeError("moe_pack_int8 takes int8 codes")
     N, K = codes.shape
+    if (N | K) >> 31:
+        _too_wide("codes", (N, K))
     index = codes.get_device()
     _on(index, codes)
     out = Int8(_new(max(1, moe_int8_code_bytes(N, K)), torch.int8, codes.device, stream), scales, (N, K))
@@ -848,11 +861,11 @@ def quantize_weights_int8(w, stream=None):
 
 
 def moe_matmul_int8_workspace_bytes(T, N, K) -> int:
-    return lib().moe_matmul_int8_workspace_bytes(T, N, K)
+    return 0 if (N | K) >> 31 else lib().moe_matmul_int8_workspace_bytes(T, N, K)
 
 
 def moe_gated_int8_workspace_bytes(T, F, K) -> int:
-    return lib().moe_gated_int8_workspace_bytes(T, F, K)
+    return 0 if (F | K) >> 31 else lib().moe_gated_int8_workspace_bytes(T, F, K)
 
 
 def _int8_inputs(x, scales, w):

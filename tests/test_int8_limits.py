@@ -3,10 +3,11 @@ import os
 import re
 
 import pytest
+import torch
 
 import paper_2606_21712_amd as moe
 
-INVALID = 1
+INVALID, UNSUPPORTED = 1, 2
 P = 0x10000          # a 16-byte aligned address that is never dereferenced
 NAN, INF = float("nan"), float("inf")
 HEADER = re.sub(r"\s*\n \*\s*", " ", open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "moe.h")).read())
@@ -31,3 +32,33 @@ def test_norm_join_says_which_numbers_it_takes(name):
         assert name in message and "1e30" in message and "finite" not in message
     contract = HEADER.split("moe_norm_join - ")[1].split("moe_status moe_norm_join(")[0]
     assert "eps, alpha or offset beyond 1e30 or NaN" in contract
+
+
+WIDE = (1 << 32) + 64        # what a 32-bit argument would cut off to 64
+
+
+def meta(shape, dtype):
+    return torch.empty(shape, dtype=dtype, device="meta")
+
+
+def test_sizes_past_32_bits_are_not_cut_off():
+    """The library's columns and channels are 32 bits wide; more are refused, not taken as what is left of them."""
+    bf, i8 = torch.bfloat16, torch.int8
+    assert moe.moe_int8_code_bytes(16, 64) == 2048 and moe.moe_int8_code_bytes(16, WIDE) == 0
+    for size in (moe.moe_matmul_int8_workspace_bytes, moe.moe_gated_int8_workspace_bytes):
+        moe.set_cu_budget(256)
+        try:
+            need = size(128, 4096, 14336)
+            assert need > 0 and size(128, (1 << 32) + 4096, 14336) == 0 and size(128, 4096, (1 << 32) + 14336) == 0
+            assert size(128, -(1 << 32) + 4096, 14336) == 0
+        finally:
+            moe.set_cu_budget(0)
+    for call in (lambda: moe.Int8(torch.zeros(2048, dtype=i8), torch.ones(16), (16, WIDE)),
+                 lambda: moe.Int8(torch.zeros(2048, dtype=i8), meta(WIDE, torch.float32), (WIDE, 64)),
+                 lambda: moe.moe_pack_int8(meta((1, WIDE), i8), torch.ones(1)),
+                 lambda: moe.moe_quantize_int8(meta((1, WIDE), bf)),
+                 lambda: moe.moe_norm_join(meta((1, WIDE), bf), pre=True),
+                 lambda: moe.moe_norm_join(meta((1, WIDE), torch.float32), meta((1, WIDE), bf))):
+        with pytest.raises(moe.MoEError) as e:
+            call()
+        assert e.value.status == UNSUPPORTED
