@@ -62,3 +62,9 @@ def test_sizes_past_32_bits_are_not_cut_off():
         with pytest.raises(moe.MoEError) as e:
             call()
         assert e.value.status == UNSUPPORTED
+
+
+def test_norm_join_says_which_rows_it_takes():
+    """fp32 squares have an end on both sides."""
+    contract = HEADER.split("moe_norm_join - ")[1].split("moe_status moe_norm_join(")[0]
+    assert "sum to 2^128 or more" in contract and "eps below 2^-100" in contract and "below 2^-50" in contract
