@@ -614,7 +614,7 @@ moe_status moe_pack_int8(const int8_t* codes, int64_t rows, int32_t K, int8_t* o
  *   x, x_scales   row-major codes [T, K], f32 [T]
  *   w, w_scales   packed codes [N, K], f32 [N]
  *   bias          bf16 [N], or NULL
- *   y             bf16 [T, N]  out:  x_scales[t] * w_scales[n] * sum_k x[t][k] w[n][k] + bias[n]
+ *   y             bf16 [T, N]  out:  (sum_k x[t][k] w[n][k]) * x_scales[t] * w_scales[n] + bias[n]
  *   ws, ws_bytes  device scratch of at least moe_matmul_int8_workspace_bytes(); not to be shared by
  *                 calls that overlap
  *

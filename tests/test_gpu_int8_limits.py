@@ -6,7 +6,7 @@ import torch
 
 import paper_2606_21712_amd as moe
 from gpu_util import log
-from test_gpu_int8 import BF, check_join, gen, join
+from test_gpu_int8 import BF, bits, check_join, gen, join, random_int8, sums
 
 pytestmark = pytest.mark.gpu
 
@@ -40,3 +40,21 @@ def test_norms_of_the_shortest_and_longest_rows(H, int8):
         x = torch.randn(4, H, generator=gen(6)).to(BF)
         args = (x, rows.to(BF), w, None, False, 0.5, True, 0.0, eps, int8)       # as a block's output
         check_join(join(*args), *args)
+
+
+def forms():
+    """Rows, channels and columns that run on every kind of kernel: few rows, small tiles whole and in parts, large tiles."""
+    return [(5, 40, 256), (30, 3003, 1040), (90, 260, 1040), (150, 520, 8208), (700, 6000, 2064), (3000, 4100, 4112)]
+
+
+@pytest.mark.parametrize("T,N,K", forms())
+def test_scales_are_applied_one_after_the_other(T, N, K):
+    """The token's scale first, bit for bit, also where the product of the scales lies under the smallest fp32 number."""
+    log(f"[gpu] matmul int8: order of the scales, {T} x {N} x {K}")
+    x, _ = random_int8(T, K, 1)
+    w, _ = random_int8(N, K, 2)
+    s = sums(x, w)
+    for a, b in ((2.0 ** -75, 2.0 ** -75), (2.0 ** -40, 2.0 ** 50), (2.0 ** 20, 2.0 ** -140)):
+        y = moe.moe_matmul_int8(x.cuda(), torch.full((T,), a).cuda(), moe.moe_pack_int8(w.cuda(), torch.full((N,), b).cuda()))
+        want = (s.float() * torch.tensor(a) * torch.tensor(b)).to(BF)
+        assert torch.equal(bits(y.cpu()), bits(want)), (a, b)

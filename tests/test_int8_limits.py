@@ -68,3 +68,9 @@ def test_norm_join_says_which_rows_it_takes():
     """fp32 squares have an end on both sides."""
     contract = HEADER.split("moe_norm_join - ")[1].split("moe_status moe_norm_join(")[0]
     assert "sum to 2^128 or more" in contract and "eps below 2^-100" in contract and "below 2^-50" in contract
+
+
+def test_products_say_in_which_order_scales_are_applied():
+    """The sum times the token's scale comes first: the scales' own product may lie outside of fp32."""
+    contract = HEADER.split("moe_matmul_int8 - ")[1].split("moe_gated_int8 - ")[0]
+    assert "(sum_k x[t][k] w[n][k]) * x_scales[t] * w_scales[n] + bias[n]" in contract and "in this order" in contract
