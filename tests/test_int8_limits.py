@@ -74,3 +74,9 @@ def test_products_say_in_which_order_scales_are_applied():
     """The sum times the token's scale comes first: the scales' own product may lie outside of fp32."""
     contract = HEADER.split("moe_matmul_int8 - ")[1].split("moe_gated_int8 - ")[0]
     assert "(sum_k x[t][k] w[n][k]) * x_scales[t] * w_scales[n] + bias[n]" in contract and "in this order" in contract
+
+
+def test_norm_join_says_which_codes_a_product_takes():
+    """Codes come for every H that is a multiple of 8, products take multiples of 16."""
+    assert "H % 16 == 0" in HEADER.split("moe_norm_join - ")[1].split("moe_status moe_norm_join(")[0]
+    assert moe.lib().moe_matmul_int8(P, P, P, P, None, 1, 16, 72, P, None, 0, None) == INVALID
