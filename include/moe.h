@@ -574,11 +574,12 @@ moe_status moe_kv8_attention(const void* q, int64_t T, int32_t q_heads, const mo
  *   *_stride    elements from a row to the next, rows in whole 16-byte pieces
  *
  * Arithmetic is fp32, x' and z are rounded once; z is taken of x' before its rounding.  The codes of z
- * are those of x' (offset + w_pre), the norm's factor is in the scale alone; products take them where H % 16 == 0. 
+ * are those of x' (offset + w_pre), the norm's factor is in the scale alone; products take them where H % 16 == 0.
  * Squares are summed in fp32: a row (of y with post = 1, of x') whose squares sum to 2^128 or more counts as infinitely
- * long, its norm is 0; with an eps below 2^-100 a row whose largest magnitude is below 2^-50 is too short, its norm is
- * off, and from 2^-75 down infinite or NaN.  A NaN or infinity stays in its row.  The order of the
- * sums depends on H, T and the compute-unit budget (moe_set_cu_budget), on nothing else.
+ * long, its norm is 0, or NaN where a product with a weight overflows; with an eps below 2^-100 a row whose
+ * largest magnitude is below 2^-50 is too short, its norm is off, and from 2^-75 down infinite or NaN.  A NaN or
+ * infinity stays in its row.  The order of the sums depends on H, T and the compute-unit budget
+ * (moe_set_cu_budget), on nothing else.
  * Errors: INVALID_ARGUMENT for H not a positive multiple of 8, T < 0, eps < 0, an
  * eps, alpha or offset beyond 1e30 or NaN, flags that are not 0 or 1, an unknown gate_kind, bad strides, arguments without the one they belong to,
  * null or misaligned pointers; UNSUPPORTED for H > 32768, T > 2^31 or an unknown dtype.

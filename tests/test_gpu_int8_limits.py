@@ -6,7 +6,8 @@ import torch
 
 import paper_2606_21712_amd as moe
 from gpu_util import log
-from test_gpu_int8 import BF, bits, check_join, gen, join, random_int8, sums
+from int8_rings import ENDS
+from test_gpu_int8 import BF, bits, budget, check_join, check_product, gated_tolerance, gen, join, random_int8, sums      # noqa: F401 (budget is a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -42,6 +43,13 @@ def test_norms_of_the_shortest_and_longest_rows(H, int8):
         check_join(join(*args), *args)
 
 
+@pytest.mark.parametrize("form,parts,T,N,K,gated,cus", ENDS)
+def test_every_end_of_a_ring(budget, form, parts, T, N, K, gated, cus):            # noqa: F811
+    log(f"[gpu] int8 {form} in {parts}: {T} x {N} x {K} gated={gated}")
+    budget(cus)
+    check_product(T, N, K, gated)
+
+
 def forms():
     """Rows, channels and columns that run on every kind of kernel: few rows, small tiles whole and in parts, large tiles."""
     return [(5, 40, 256), (30, 3003, 1040), (90, 260, 1040), (150, 520, 8208), (700, 6000, 2064), (3000, 4100, 4112)]
@@ -58,3 +66,62 @@ def test_scales_are_applied_one_after_the_other(T, N, K):
         y = moe.moe_matmul_int8(x.cuda(), torch.full((T,), a).cuda(), moe.moe_pack_int8(w.cuda(), torch.full((N,), b).cuda()))
         want = (s.float() * torch.tensor(a) * torch.tensor(b)).to(BF)
         assert torch.equal(bits(y.cpu()), bits(want)), (a, b)
+
+
+@pytest.mark.parametrize("T,F,K", forms())
+def test_gated_products_keep_rows_and_channels_apart(T, F, K):
+    """A token's NaN scale shows in its row alone, a channel's infinite or NaN scale in its channel alone."""
+    log(f"[gpu] gated int8: scales that are not finite, {T} x {F} x {K}")
+    x, sx = random_int8(T, K, 5)
+    (wg, sg), (wu, su) = random_int8(F, K, 6), random_int8(F, K, 7)
+    run = lambda: moe.moe_gated_int8(x.cuda(), sx.cuda(), moe.moe_pack_int8(wg.cuda(), sg.cuda()),
+                                     moe.moe_pack_int8(wu.cuda(), su.cuda())).cpu()
+    want = run()
+    sx[1], sg[3], su[17], sg[F - 1] = float("nan"), float("inf"), float("-inf"), float("nan")
+    h = run()
+    rows, channels = torch.arange(T) != 1, torch.ones(F, dtype=torch.bool)
+    channels[[3, 17, F - 1]] = False
+    assert h[1].isnan().all() and h[:, F - 1].isnan().all()
+    assert not h[rows][:, 3].isfinite().any()
+    assert torch.equal(bits(h[rows][:, channels]), bits(want[rows][:, channels])) and want.isfinite().all()
+
+
+@pytest.mark.parametrize("T", [1, 40, 300])
+def test_gated_products_at_their_largest_sums(T):
+    """All codes -128 and K as long as it may be: both sums are 2^31 - 2^18, times 2^-31 just under 1."""
+    log(f"[gpu] gated int8: largest sums, T={T}")
+    K, F = 131056, 48
+    x = torch.full((T, K), -128, dtype=torch.int8, device="cuda")
+    w = moe.moe_pack_int8(torch.full((F, K), -128, dtype=torch.int8, device="cuda"), torch.full((F,), 2.0 ** -15, device="cuda"))
+    h = moe.moe_gated_int8(x, torch.full((T,), 2.0 ** -16, device="cuda"), w, w).cpu().double()
+    g = torch.full((T, F), K * 2.0 ** 14 * 2.0 ** -31, dtype=torch.float64)
+    ref = g * torch.sigmoid(g) * g
+    assert ((h - ref).abs() <= gated_tolerance(g, g, ref)).all()
+
+
+def test_a_projection_repeats_itself():
+    """A norm join to codes and the product on them, over and over between other work and on two streams at once: the
+    same bits every time."""
+    log("[gpu] norm_join and matmul int8: repeats")
+    T, N, H = 2003, 4608, 7168
+    g = gen(9)
+    x, y = (torch.randn(T, H, generator=g).to(BF).cuda() for _ in range(2))
+    gate, pre = (torch.randn(H, generator=g).to(BF).cuda() for _ in range(2))
+    w = moe.moe_pack_int8(*(t.cuda() for t in random_int8(N, H, 10)))
+
+    def project():
+        xo, z, s = moe.moe_norm_join(x, y, gate=gate, pre=pre, int8=True)
+        return xo, z, s, moe.moe_matmul_int8(z, s, w)
+    want = project()
+    noise = torch.randn(4096, 4096, device="cuda")
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = []
+    for i in range(6):
+        noise = noise * 1.0001
+        for st in streams:
+            with torch.cuda.stream(st):
+                got.append(project())
+    torch.cuda.synchronize()
+    for one in got:
+        assert all(torch.equal(bits(a), bits(b)) for a, b in zip(one, want))
