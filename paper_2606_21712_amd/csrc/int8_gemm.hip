@@ -50,7 +50,7 @@ __device__ __forceinline__ void store4(uint16_t* row, int n, int N, const float 
 // LDS; P steps are in flight.  More rows are other workgroups', which find the weights in the L2.
 //
 // Bound by the reads of the weights, after a launch and its ramp: one row, 4096 channels, K 14336 (59 MB) 10.0 us, 5.9
-// TB/s; eight rows gated, 2048, 7168 (29 MB) 7.5; eight rows, 28672, 4096 past the caches (117 MB) 21.4, 5.5 TB/s.  Two
+// TB/s; eight rows gated, 2048, 7168 (29 MB) 7.5; five rows, 6309, 16400 past the caches (103 MB) 20.2, 5.1 TB/s.  Two
 // tiles a wavefront halve the reads of x, eight wavefronts and two steps keep 32 KB of a tile in flight (four steps: 16
 // rows, 4096, 14336 14.4 us for 13.6).  Two groups read the weights once for both: 32 rows, 6144, 4096 8.0 us, 10.1 in
 // two workgroups; four were faster nowhere (64 rows 11.9 us, 10.0 on the tiles below).

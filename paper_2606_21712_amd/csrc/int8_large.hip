@@ -18,7 +18,8 @@ namespace {
 // ends.  The largest tile that registers hold moves the fewest bytes through LDS; 192 rows (813 us) fill the last
 // round better where that counts.  Measured against (16384, 4096, 14336): two stages of x 760 us; a stage's loads in
 // one of its groups, 832; workgroups that stay and load their next tile's first stages while this one's results
-// leave, 750 (gated 830, for 785 then): they need registers that the sums take, and spill.
+// leave, 750 (gated 830, for 785 then): they need registers that the sums take, and spill 20 (as it is, one of the gated
+// form's is spilled, before the loop and after it).
 __device__ __forceinline__ i32x16 mfma32_i8(u32x4 a, u32x4 b, i32x16 c) {
   return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
 }

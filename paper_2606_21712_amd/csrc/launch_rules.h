@@ -208,8 +208,12 @@ struct Int8Plan {
 
 // Which kernel: the one that a model of their times, fitted to 21000 measurements of 1950 sizes (1 to 16384 rows, 200 to
 // 30000 channels, K 256 to 16384, plain and gated, replayed in graphs), thinks the fastest.  On 400 sizes apart from
-// these, of up to 128 rows, its choice takes 0.9% more than the fastest of all kernels on average, at most 22%.  us; a
-// stage is 128 columns.
+// these, of up to 128 rows, its choice takes 0.9% more than the fastest of all kernels on average, at most 22%; on 147
+// fresh ones of more rows 17% on 129 to 160 rows (at most 87%), 5% on 161 to 512 (39%), 1% above (9%).  us; a stage is
+// 128 columns.
+//   The kernels for few rows end at 128 rows because their fit does.  With few channels they are the fastest up to
+//   some 220 rows (133 rows, 287 channels, K 2720: 7.3 on the 32 x 128 that is picked, 3.9 with one tile a wavefront; 221,
+//   236, 1616 gated: 5.3 and 3.9).
 //   Tiles: rounds of as many workgroups as run at once.  A stage takes what its operands take to pass
 //   through a compute unit, once for each workgroup there, and so does a tile's end; all operands and results move
 //   once besides, and the weights a quarter more for each further tile of rows.
@@ -287,8 +291,10 @@ inline Int8Plan int8_plan(int64_t T, int64_t N, int64_t K, bool gated, int num_c
       }
     }
   // Weights that one workgroup reads and no other, and that are too many to be found in the Infinity Cache by the
-  // next call: 8 rows, 28672 channels, K 4096 (117 MB) 24.0 us, 21.4 past the caches; 2 rows, 8441, 10928 (92 MB) 25.5,
-  // 20.3.  59 MB that come back after two others 10.3, 12.5 past the caches.
+  // next call: 8 rows, 28672 channels, K 4096 (117 MB, on 32 x 128) 22.7 us, 20.4 past the caches; 5 rows, 6309, 16400 (103
+  // MB, two tiles a wavefront) 22.0, 20.2; 2 rows, 8441, 10928 (92 MB, one) 22.3, 20.3.  59 MB that come back after two
+  // others 10.3, 12.5 past the caches.  (One row, 128256 channels, K 4096, beyond the channels of the fit: 80.0 on the 32 x
+  // 128 that is picked, 76.6 with two tiles a wavefront; 152064, 3584: 80.3 and 82.4.)
   best.stream = best.parts == 1 && T <= rows && T <= 128 && weights >= double(64 << 20);
   return best;
 }

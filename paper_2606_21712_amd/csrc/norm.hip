@@ -72,10 +72,13 @@ __device__ __forceinline__ void block_sum(float& sum, uint32_t& top, float (*slo
 
 // A workgroup walks rows; while it works on one, the next one's x and y are on their way.  Norm weights and a gate of
 // the channels stay in registers (read again for each row, from the L2, they cost a third: 9001 x 7168 133 us
-// against 102).  Rows of more than 16384 leave no registers for either.
+// against 102).  Rows of more than 16384 leave no registers for either, nor for the row ahead, and 8 to 40 registers of
+// theirs spill.
 //
 // Bound by memory: 9001 x 7168 with a post norm (516 MB) 98 us, 5.3 TB/s (without the row ahead 102), with codes
-// 85; 2003 x 7168 24.6 (30.9); one row of 4096 3.3 us, the latency of a load, two sums and a store.
+// 85; with a full gate (645 MB), which is read once its row is worked on, 122, 5.3 TB/s; an f32 stream (774 MB) 150, 5.2
+// TB/s.  2003 x 7168 24.6 (30.9); one row of 4096 3.3 us, the latency of a load, two sums and a store.  4000 x 32768 (1049
+// MB) 228 us, 4.6 TB/s, f32 344; 520 rows of it 44, 3.1 TB/s: a row at a time, two rounds and the last 8 rows.
 template <int NT, int V, bool F32, bool CODES>
 __global__ __launch_bounds__(NT) void norm_join_kernel(NormJoin a) {
   constexpr int kElt = F32 ? 4 : 2;
