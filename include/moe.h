@@ -628,6 +628,7 @@ moe_status moe_pack_int8(const int8_t* codes, int64_t rows, int32_t K, int8_t* o
  *
  * moe_gated_int8 - both projections of a gated block, its activation and product:
  *   h[t][f] = silu(g) * u,   g = x Wg^T, u = x Wu^T as above, in fp32; h bf16 [T, F], rounded once.
+ *   silu(g) = g / (1 + exp(-g)) is 0 for g below -87.3, where it is smaller than 1.03e-36
  *   wg, wu        packed codes [F, K]
  * Errors as moe_matmul_int8.
  */

@@ -86,6 +86,28 @@ def test_gated_products_keep_rows_and_channels_apart(T, F, K):
     assert torch.equal(bits(h[rows][:, channels]), bits(want[rows][:, channels])) and want.isfinite().all()
 
 
+@pytest.mark.parametrize("T", [15, 30, 100, 1000, 3000])
+def test_gated_products_of_gates_far_out(T):
+    """Gates from -100 to 100 with an up projection of 5000.  The quotient 1 / (1 + exp(-g)) is taken as 0 below the smallest
+    normal fp32 number, 2^-126: from g = -87.3 down h is off by up to 2^-126 |g u|, there and nowhere else."""
+    log(f"[gpu] gated int8: gates far out, T={T}")
+    F, K = 520, 64
+    x = torch.zeros(T, K, dtype=torch.int8)
+    x[:, 0] = 1
+    sx = torch.linspace(0.5, 1.0, T)
+    wg, wu = torch.zeros(F, K, dtype=torch.int8), torch.zeros(F, K, dtype=torch.int8)
+    wg[:, 0] = (torch.arange(F) % 255 - 127).to(torch.int8)
+    wu[:, 0] = 125
+    sg, su = torch.full((F,), 100 / 127), torch.full((F,), 40.0)
+    h = moe.moe_gated_int8(x.cuda(), sx.cuda(), moe.moe_pack_int8(wg.cuda(), sg.cuda()), moe.moe_pack_int8(wu.cuda(), su.cuda()))
+    g, u = (sums(x, w) * sx.double()[:, None] * s.double() for w, s in ((wg, sg), (wu, su)))
+    ref = g * torch.sigmoid(g) * u
+    far = g < -87.3
+    tol = gated_tolerance(g, u * 0, ref) + far * 2.0 ** -126 * (g * u).abs()      # u * 0: without the room for far gates
+    assert far.any() and (g > 87.3).any()
+    assert ((h.cpu().double() - ref).abs() <= tol).all()
+
+
 @pytest.mark.parametrize("T", [1, 40, 300])
 def test_gated_products_at_their_largest_sums(T):
     """All codes -128 and K as long as it may be: both sums are 2^31 - 2^18, times 2^-31 just under 1."""

@@ -80,3 +80,9 @@ def test_norm_join_says_which_codes_a_product_takes():
     """Codes come for every H that is a multiple of 8, products take multiples of 16."""
     assert "H % 16 == 0" in HEADER.split("moe_norm_join - ")[1].split("moe_status moe_norm_join(")[0]
     assert moe.lib().moe_matmul_int8(P, P, P, P, None, 1, 16, 72, P, None, 0, None) == INVALID
+
+
+def test_gated_products_say_where_their_gate_ends():
+    """1 / (1 + exp(-g)) is under the smallest normal fp32 number there, and the reciprocal gives 0."""
+    contract = HEADER.split("moe_gated_int8 - ")[1].split("size_t moe_matmul_int8_workspace_bytes")[0]
+    assert "g below -87.3" in contract
